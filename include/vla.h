@@ -459,6 +459,138 @@ int vla_debug_generate(uint64_t seed, const char* name, int64_t n, double mean, 
 int vla_debug_gemm_plan(int32_t dtype, int32_t M, int32_t N, int32_t K, int32_t kind, int32_t skinny,
                         int32_t plan_m, int32_t plan_batch, int32_t* out, int64_t* scratch_floats);
 
+/* ------------------------------------------------------------------------
+ * Paged KV cache: for a language model that answers token by token, or by
+ * drafted trees of tokens that it verifies in one pass. vla_ctx holds one
+ * frame's fixed prefix; the calls here work on a caller-owned cache whose
+ * sequences grow, branch and end. Each call is asynchronous on its stream,
+ * allocates nothing, keeps nothing between calls, reads lengths and tables on
+ * the device only and can be captured into a HIP graph (a replay works on
+ * what the arrays hold then). Calls on one cache must be ordered by their
+ * caller (one stream, or events); calls on different caches may overlap. Every
+ * array is device memory of the current device.
+ *
+ * A pool of n_pages pages serves every sequence; a page holds page_len slots
+ * (tokens) of every layer and KV head. Sequence s's slot i lies in page
+ * table[s][i / page_len]. Slots 0 .. lens[s] - 1 are committed; a step writes
+ * its rows (drafts) to the slots behind them and vla_pages_commit keeps the
+ * accepted ones. A page that several sequences hold (refs > 1) is full and
+ * committed, so no call writes to it.
+ * ------------------------------------------------------------------------ */
+typedef struct vla_pages {
+  int32_t dtype;     /* VLA_F32 or VLA_BF16: the cache and the rows of q, k, v, out  */
+  int32_t layers;
+  int32_t kv_heads;
+  int32_t head_dim;  /* a multiple of 32, <= 256 (fp32: <= 128)                      */
+  int32_t page_len;  /* 16, 32, 64, 128 or 256                                       */
+  int32_t n_pages;
+  int32_t n_seqs;    /* sequences the arrays below hold                              */
+  int32_t max_pages; /* pages a sequence can have                                    */
+  void* k;           /* [layers][n_pages][kv_heads][page_len][head_dim], 16-byte     */
+  void* v;           /*   aligned; likewise                                          */
+  int32_t* table;    /* [n_seqs][max_pages], -1 behind a sequence's pages            */
+  int32_t* lens;     /* [n_seqs] committed slots                                     */
+  int32_t* held;     /* [n_seqs] pages in the sequence's table                       */
+  int32_t* refs;     /* [n_pages] sequences that hold the page (0: free)             */
+  int32_t* status;   /* [1] VLA_PAGES_* bits, set by calls and never cleared by them */
+} vla_pages;
+
+/* status bits: what a call found on the device and left undone */
+#define VLA_PAGES_OUT 1 /* a page was missing: the pool or a table was full, or a slot */
+                        /*   without a page was to be written                       */
+#define VLA_PAGES_BAD 2 /* a position outside the rotation table, or an accepted list  */
+                        /*   that does not ascend within its drafts                 */
+
+/* The rows of one step: entry e's are start[e] .. start[e + 1] - 1 of the row
+ * buffers, row start[e] + i being draft i of sequence seqs[e] (slot
+ * lens + i). start is non-decreasing. An entry whose sequence is not in
+ * 0 .. n_seqs - 1 is padding: its rows are left as they are, and so are rows
+ * behind start[n_entries]. Sequences of one batch differ. */
+typedef struct vla_rows {
+  int32_t n_rows;       /* rows the buffers hold                            */
+  int32_t n_entries;
+  const int32_t* start; /* [n_entries + 1]                                  */
+  const int32_t* seqs;  /* [n_entries], or NULL: entry e is sequence e      */
+} vla_rows;
+
+/* How queries and keys are normed and rotated: y = RMSNorm(x) g per head (a
+ * NULL gain: no norm), then the first rot_dim elements rotated in pairs
+ * (i, i + rot_dim / 2) by the angle whose cosine and sine are row `position`
+ * of the tables. */
+typedef struct vla_rope_norm {
+  const float* q_gain;   /* fp32 [head_dim], 16-byte aligned, or NULL       */
+  const float* k_gain;
+  int32_t gain_plus_one; /* 1: the factor is 1 + gain                       */
+  float eps;             /* > 0 where there is a gain                       */
+  const float* cos_tab;  /* fp32 [n_pos][rot_dim / 2], 16-byte aligned      */
+  const float* sin_tab;
+  int32_t n_pos;
+  int32_t rot_dim;       /* a multiple of 16, <= head_dim; 0: no rotation   */
+} vla_rope_norm;
+
+/* Empty the cache: every page free, every table -1, lengths and status 0. k
+ * and v are not touched. */
+int vla_pages_init(const vla_pages* c, void* stream);
+
+/* Give every entry's sequence pages for lens + its rows slots, entries in
+ * order, free pages lowest first. When none is left (or a table is full) the
+ * rest goes without: VLA_PAGES_OUT. */
+int vla_pages_reserve(const vla_pages* c, const vla_rows* r, void* stream);
+
+/* Norm, rotate and store one layer's new rows: q [n_rows][nq heads], k and v
+ * [n_rows][kv_heads], rows ld* elements apart (a multiple of 16 bytes, as are
+ * the base addresses), so slices of a fused QKV product can be given. Queries
+ * go to q_out (which may be q itself with the same ldq), keys and values to
+ * the cache's slots. pos (int32 [n_rows]) holds the rows' positions; NULL: the
+ * slot. Norm, rotation and mean are fp32 and rounded once. A row whose
+ * position is outside the table is left out (VLA_PAGES_BAD); K and V of a slot
+ * without a page are not stored (VLA_PAGES_OUT). */
+int vla_qk_norm_rope(const vla_pages* c, int32_t layer, const vla_rows* r, const vla_rope_norm* p, const int32_t* pos,
+                     int32_t nq, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv,
+                     void* q_out, int64_t ldo, void* stream);
+
+/* Attention of one layer's rows over their sequences: out [n_rows][nq heads]
+ * = softmax(scale q K^T) V, query head h reading KV head h / (nq / kv_heads).
+ * Row i of an entry attends to every committed slot and to its own step's
+ * drafts: with mask (uint32 [n_rows][mask_words]) to draft j when bit j % 32
+ * of word j / 32 is set (drafts past 32 mask_words are not seen), without one
+ * to drafts 0 .. i. One row an entry and no mask is plain decoding, many rows
+ * and no mask a causal chunk of a prompt. The drafts' K and V have been stored
+ * before; slots without a page are not seen; a row that sees nothing is zero.
+ * Masked slots may hold anything, infinities and NaN among it. Sums and the
+ * softmax are fp32. q and out have rows ldq and ldo elements apart (base and
+ * rows on 16 bytes; out must not overlap q). scratch: scratch_bytes of device
+ * memory, at least what vla_tree_attention_scratch says, 16-byte aligned,
+ * contents of no matter; calls that may overlap need their own. The sums'
+ * order depends on the batch's lengths and shapes alone. */
+int vla_tree_attention(const vla_pages* c, int32_t layer, const vla_rows* r, const uint32_t* mask, int32_t mask_words,
+                       int32_t nq, float scale, const void* q, int64_t ldq, void* out, int64_t ldo, void* scratch,
+                       int64_t scratch_bytes, void* stream);
+
+/* Bytes of scratch for batches of these n_rows and n_entries (host only, but
+ * the size depends on the current device's CU count). */
+int vla_tree_attention_scratch(const vla_pages* c, const vla_rows* r, int32_t nq, int64_t* bytes);
+
+/* Branch: sequence dst[i] becomes a copy of src[i] (committed slots only).
+ * Full pages are shared, the used slots of the last page are copied in every
+ * layer to a page of the child's own. A pair is made (made[i] = 1) when dst[i]
+ * holds no page, is not dst of an earlier pair and src[i] is not dst of any
+ * pair; otherwise, or when no page is free (VLA_PAGES_OUT), made[i] = 0 and
+ * dst[i] stays empty or as it was. src, dst and made: int32 [n]. */
+int vla_pages_fork(const vla_pages* c, int32_t n, const int32_t* src, const int32_t* dst, int32_t* made, void* stream);
+
+/* Keep the accepted drafts of every entry: draft kept[start[e] + j] moves to
+ * slot lens + j in every layer, for j < n_kept[e], and lens grows by
+ * n_kept[e]. A list ascends. kept NULL: the first n_kept[e] drafts (nothing
+ * moves); n_kept NULL: all rows (kept must then be NULL). An entry whose list
+ * does not ascend within its drafts keeps none (VLA_PAGES_BAD). Pages stay
+ * with the sequence for its next drafts. */
+int vla_pages_commit(const vla_pages* c, const vla_rows* r, const int32_t* kept, const int32_t* n_kept, void* stream);
+
+/* Empty n sequences (int32 [n]; entries outside 0 .. n_seqs - 1 are skipped):
+ * pages that no other sequence holds are free again. */
+int vla_pages_release(const vla_pages* c, int32_t n, const int32_t* seqs, void* stream);
+
 /* Message for the last non-zero status on this thread ("" if none). */
 const char* vla_last_error(void);
 

@@ -69,6 +69,25 @@ class vla_debug_epi(ctypes.Structure):
                 ("gain", ctypes.c_void_p), ("plan_out", ctypes.c_void_p)]
 
 
+class vla_pages(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_int32) for f in ("dtype", "layers", "kv_heads", "head_dim", "page_len", "n_pages",
+                                              "n_seqs", "max_pages")] + \
+               [(f, ctypes.c_void_p) for f in ("k", "v", "table", "lens", "held", "refs", "status")]
+
+
+class vla_rows(ctypes.Structure):
+    _fields_ = [("n_rows", ctypes.c_int32), ("n_entries", ctypes.c_int32), ("start", ctypes.c_void_p),
+                ("seqs", ctypes.c_void_p)]
+
+
+class vla_rope_norm(ctypes.Structure):
+    _fields_ = [("q_gain", ctypes.c_void_p), ("k_gain", ctypes.c_void_p), ("gain_plus_one", ctypes.c_int32),
+                ("eps", ctypes.c_float), ("cos_tab", ctypes.c_void_p), ("sin_tab", ctypes.c_void_p),
+                ("n_pos", ctypes.c_int32), ("rot_dim", ctypes.c_int32)]
+
+
+PAGES_OUT, PAGES_BAD = 1, 2  # bits of a paged cache's status
+
 DEBUG_EPI = {"bias": 0, "t": 1, "gelu": 2, "swish": 3, "geglu": 4, "qkv_rope": 5, "qkv_plain": 6, "step": 7,
              "resid_norm": 8}
 
@@ -127,6 +146,14 @@ def _load():
         "vla_debug_gemm_plan": [I32, I32, I32, I32, I32, I32, I32, I32, P, ctypes.POINTER(I64)],
         "vla_debug_attention_cache": [I32, I32, I32, I32, I32, P, P, P, I32, P, P, I32, P, P],
         "vla_debug_norm": [I32, I32, I32, P, I32, P, I32, P, P, P, I32, P, I32, P, I32, P],
+        "vla_pages_init": [P, P],
+        "vla_pages_reserve": [P, P, P],
+        "vla_qk_norm_rope": [P, I32, P, P, P, I32, P, I64, P, I64, P, I64, P, I64, P],
+        "vla_tree_attention": [P, I32, P, P, I32, I32, ctypes.c_float, P, I64, P, I64, P, I64, P],
+        "vla_tree_attention_scratch": [P, P, I32, ctypes.POINTER(I64)],
+        "vla_pages_fork": [P, I32, P, P, P, P],
+        "vla_pages_commit": [P, P, P, P, P],
+        "vla_pages_release": [P, I32, P, P],
         "vla_kernel_timer": [P, ctypes.c_char_p],
         "vla_kernel_timer_read": [P, ctypes.POINTER(D), ctypes.POINTER(I64)],
     }
@@ -420,12 +447,211 @@ def vla_debug_gemm_plan(dtype: int, M: int, N: int, K: int, kind: int, skinny: b
             "scratch_floats": int(scratch.value)}
 
 
+# --------------------------------------------------------------------------
+# Paged KV cache (see vla.h). The descriptors below are made once from device
+# tensors, which they keep; the calls check their own operands against them.
+# Everything lies on one device, which must be the current one at a call.
+# --------------------------------------------------------------------------
+
+def _dev(x, what: str, dtype: str, shape=None):
+    """A contiguous device tensor of this type (and shape); its device."""
+    if x is None or not hasattr(x, "data_ptr"):
+        raise _einval(f"{what} must be a device (cuda) tensor")
+    n = 1
+    for d in (x.shape if shape is None else shape):
+        n *= int(d)
+    _check_buffer(x, what, n, dtype)
+    if shape is not None and tuple(x.shape) != tuple(shape):
+        raise _einval(f"{what} must have shape {tuple(shape)}, got {tuple(x.shape)}")
+    return x.device
+
+
+def _one_device(pairs):
+    first = None
+    for what, dev in pairs:
+        if first is None:
+            first = dev
+        elif dev != first:
+            raise _einval(f"{what} is on {dev}, other tensors on {first}")
+    return first
+
+
+def make_pages(k, v, table, lens, held, refs, status) -> vla_pages:
+    """A vla_pages from the cache's tensors: k and v [layers, n_pages,
+    kv_heads, page_len, head_dim] (bfloat16 or float32), table [n_seqs,
+    max_pages], lens and held [n_seqs], refs [n_pages], status [1] (int32)."""
+    kt = str(getattr(k, "dtype", "")).replace("torch.", "")
+    if kt not in ("bfloat16", "float32"):
+        raise _einval(f"k must be bfloat16 or float32, got {kt or type(k).__name__}")
+    if len(k.shape) != 5:
+        raise _einval("k must be [layers, n_pages, kv_heads, page_len, head_dim]")
+    if len(getattr(table, "shape", ())) != 2:
+        raise _einval("table must be [n_seqs, max_pages]")
+    layers, n_pages, nkv, page, hd = (int(d) for d in k.shape)
+    n_seqs, wide = (int(d) for d in table.shape)
+    dev = _one_device([("k", _dev(k, "k", kt)), ("v", _dev(v, "v", kt, k.shape)),
+                       ("table", _dev(table, "table", "int32")), ("lens", _dev(lens, "lens", "int32", (n_seqs,))),
+                       ("held", _dev(held, "held", "int32", (n_seqs,))),
+                       ("refs", _dev(refs, "refs", "int32", (n_pages,))),
+                       ("status", _dev(status, "status", "int32", (1,)))])
+    p = vla_pages(VLA_BF16 if kt == "bfloat16" else VLA_F32, layers, nkv, hd, page, n_pages, n_seqs, wide,
+                  *(_ptr(t) for t in (k, v, table, lens, held, refs, status)))
+    p._src = (k, v, table, lens, held, refs, status)
+    p._dev, p._type = dev, k.dtype
+    return p
+
+
+def make_rows(start, n_rows: int, seqs=None) -> vla_rows:
+    """A vla_rows from start [n_entries + 1] and seqs [n_entries] (int32, or
+    None: entry e is sequence e)."""
+    dev = _dev(start, "start", "int32")
+    if len(start.shape) != 1 or start.shape[0] < 1:
+        raise _einval("start must be [n_entries + 1]")
+    n = int(start.shape[0]) - 1
+    if seqs is not None:
+        _one_device([("start", dev), ("seqs", _dev(seqs, "seqs", "int32", (n,)))])
+    r = vla_rows(int(n_rows), n, _ptr(start), _ptr(seqs))
+    r._src, r._dev = (start, seqs), dev
+    return r
+
+
+def make_rope_norm(cos=None, sin=None, q_gain=None, k_gain=None, gain_plus_one: int = 0,
+                   eps: float = 1e-6) -> vla_rope_norm:
+    """A vla_rope_norm from the rotation's tables [n_pos, rot_dim / 2] and the
+    gains [head_dim] (float32; None: no rotation, no norm)."""
+    if (cos is None) != (sin is None):
+        raise _einval("a rotation needs both tables")
+    pairs, n_pos, rot = [], 0, 0
+    if cos is not None:
+        if len(cos.shape) != 2:
+            raise _einval("cos must be [n_pos, rot_dim / 2]")
+        pairs += [("cos", _dev(cos, "cos", "float32")), ("sin", _dev(sin, "sin", "float32", cos.shape))]
+        n_pos, rot = int(cos.shape[0]), 2 * int(cos.shape[1])
+    for what, g in (("q_gain", q_gain), ("k_gain", k_gain)):
+        if g is not None:
+            if len(g.shape) != 1:
+                raise _einval(f"{what} must be [head_dim]")
+            pairs.append((what, _dev(g, what, "float32")))
+    p = vla_rope_norm(_ptr(q_gain), _ptr(k_gain), 1 if gain_plus_one else 0, float(eps), _ptr(cos), _ptr(sin),
+                      n_pos, rot)
+    p._src, p._dev = (cos, sin, q_gain, k_gain), _one_device(pairs)
+    return p
+
+
+def _at(pages, *others) -> None:
+    """The current device holds the cache and the others' tensors."""
+    import torch
+    dev = pages._dev
+    for x in others:
+        if x is not None and x != dev:
+            raise _einval(f"a tensor is on {x}, the cache on {dev}")
+    if dev.index is not None and torch.cuda.current_device() != dev.index:
+        raise _einval(f"the cache is on {dev}, the current device is {torch.cuda.current_device()}")
+
+
+def _heads(x, what: str, pages, rows, heads=None):
+    """[n_rows, heads, head_dim] of the cache's type, heads side by side; its
+    row stride and heads."""
+    if not getattr(x, "is_cuda", False):
+        raise _einval(f"{what} must be a device (cuda) tensor")
+    if x.dtype != pages._type:
+        raise _einval(f"{what} must be {pages._type}, got {x.dtype}")
+    shape, stride = x.shape, x.stride()
+    hd = pages.head_dim
+    if len(shape) != 3 or shape[2] != hd or shape[0] != rows.n_rows or (heads is not None and shape[1] != heads):
+        raise _einval(f"{what} must be [{rows.n_rows}, {'heads' if heads is None else heads}, {hd}], got "
+                      f"{tuple(shape)}")
+    if stride[2] != 1 or (shape[1] > 1 and stride[1] != hd):
+        raise _einval(f"{what}: a row's heads must be contiguous")
+    # (a single row has no stride that counts)
+    return max(stride[0], shape[1] * hd) if shape[0] <= 1 else stride[0]
+
+
+def vla_pages_init(pages: vla_pages, stream: int = 0) -> None:
+    _at(pages)
+    _check(_lib.vla_pages_init(ctypes.byref(pages), stream or None))
+
+
+def vla_pages_reserve(pages: vla_pages, rows: vla_rows, stream: int = 0) -> None:
+    _at(pages, rows._dev)
+    _check(_lib.vla_pages_reserve(ctypes.byref(pages), ctypes.byref(rows), stream or None))
+
+
+def vla_qk_norm_rope(pages: vla_pages, layer: int, rows: vla_rows, rope: vla_rope_norm, q, k, v, q_out, pos=None,
+                     stream: int = 0) -> None:
+    """q, q_out [n_rows, nq, head_dim], k and v [n_rows, kv_heads, head_dim]
+    (rows may be strided: slices of one QKV tensor), pos int32 [n_rows]."""
+    nkv = pages.kv_heads
+    nq = int(q.shape[1]) if len(q.shape) == 3 else -1
+    ldq, ldk, ldv = _heads(q, "q", pages, rows), _heads(k, "k", pages, rows, nkv), _heads(v, "v", pages, rows, nkv)
+    ldo = _heads(q_out, "q_out", pages, rows, nq)
+    cos, _, qg, kg = rope._src
+    for what, g in (("q_gain", qg), ("k_gain", kg)):
+        if g is not None and g.shape[0] != pages.head_dim:
+            raise _einval(f"{what} holds {g.shape[0]} elements, head_dim is {pages.head_dim}")
+    _at(pages, rows._dev, rope._dev, q.device, k.device, v.device, q_out.device,
+        None if pos is None else _dev(pos, "pos", "int32", (rows.n_rows,)))
+    _check(_lib.vla_qk_norm_rope(ctypes.byref(pages), layer, ctypes.byref(rows), ctypes.byref(rope), _ptr(pos), nq,
+                                 q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, q_out.data_ptr(), ldo,
+                                 stream or None))
+
+
+def vla_tree_attention_scratch(pages: vla_pages, rows: vla_rows, nq: int) -> int:
+    n = ctypes.c_int64()
+    _at(pages, rows._dev)
+    _check(_lib.vla_tree_attention_scratch(ctypes.byref(pages), ctypes.byref(rows), int(nq), ctypes.byref(n)))
+    return n.value
+
+
+def vla_tree_attention(pages: vla_pages, layer: int, rows: vla_rows, q, out, scratch, mask=None, scale=None,
+                       stream: int = 0) -> None:
+    """q and out [n_rows, nq, head_dim] (rows may be strided), scratch uint8
+    (vla_tree_attention_scratch), mask int32 [n_rows, words] (the bits of
+    uint32) or None; scale None: 1 / sqrt(head_dim)."""
+    nq = int(q.shape[1]) if len(q.shape) == 3 else -1
+    ldq, ldo = _heads(q, "q", pages, rows), _heads(out, "out", pages, rows, nq)
+    words, mdev = 0, None
+    if mask is not None:
+        if len(mask.shape) != 2 or mask.shape[0] != rows.n_rows:
+            raise _einval(f"mask must be [{rows.n_rows}, words], got {tuple(mask.shape)}")
+        mdev, words = _dev(mask, "mask", "int32"), int(mask.shape[1])
+    _at(pages, rows._dev, q.device, out.device, _dev(scratch, "scratch", "uint8"), mdev)
+    _check(_lib.vla_tree_attention(ctypes.byref(pages), layer, ctypes.byref(rows), _ptr(mask), words, nq,
+                                   pages.head_dim ** -0.5 if scale is None else scale, q.data_ptr(), ldq,
+                                   out.data_ptr(), ldo, scratch.data_ptr(), scratch.numel(), stream or None))
+
+
+def vla_pages_fork(pages: vla_pages, src, dst, made, stream: int = 0) -> None:
+    """src, dst, made: int32 [n]."""
+    if len(src.shape) != 1:
+        raise _einval("src must be [n]")
+    _at(pages, _dev(src, "src", "int32"), _dev(dst, "dst", "int32", src.shape), _dev(made, "made", "int32", src.shape))
+    _check(_lib.vla_pages_fork(ctypes.byref(pages), int(src.shape[0]), _ptr(src), _ptr(dst), _ptr(made),
+                               stream or None))
+
+
+def vla_pages_commit(pages: vla_pages, rows: vla_rows, kept=None, n_kept=None, stream: int = 0) -> None:
+    """kept int32 [n_rows], n_kept int32 [n_entries] (None: see vla.h)."""
+    _at(pages, rows._dev, None if kept is None else _dev(kept, "kept", "int32", (rows.n_rows,)),
+        None if n_kept is None else _dev(n_kept, "n_kept", "int32", (rows.n_entries,)))
+    _check(_lib.vla_pages_commit(ctypes.byref(pages), ctypes.byref(rows), _ptr(kept), _ptr(n_kept), stream or None))
+
+
+def vla_pages_release(pages: vla_pages, seqs, stream: int = 0) -> None:
+    """seqs int32 [n]."""
+    if len(seqs.shape) != 1:
+        raise _einval("seqs must be [n]")
+    _at(pages, _dev(seqs, "seqs", "int32"))
+    _check(_lib.vla_pages_release(ctypes.byref(pages), int(seqs.shape[0]), _ptr(seqs), stream or None))
+
+
 def exported_symbols() -> Iterable[str]:
     """Names of the C entry points this binding wraps."""
     return ["vla_preset", "vla_validate", "vla_model_config", "vla_create", "vla_destroy", "vla_ctx_create",
             "vla_ctx_destroy", "vla_vlm_prefill", "vla_action_denoise", "vla_pipeline_run",
             "vla_param_count", "vla_param_info", "vla_export_param", "vla_ctx_export_kv", "vla_ctx_export_cross", "vla_ctx_export_cog", "vla_wavelog_enable", "vla_wavelog_read",
             "vla_debug_gemm", "vla_debug_gemm_epi", "vla_debug_gemm_fold", "vla_debug_gemm_ln", "vla_gemm_noalloc", "vla_debug_attention", "vla_debug_attention_cache", "vla_debug_norm", "vla_debug_generate",
-            "vla_debug_gemm_plan",
+            "vla_debug_gemm_plan", "vla_pages_init", "vla_pages_reserve", "vla_qk_norm_rope", "vla_tree_attention",
+            "vla_tree_attention_scratch", "vla_pages_fork", "vla_pages_commit", "vla_pages_release",
             "vla_kernel_timer",
             "vla_kernel_timer_read", "vla_last_error"]

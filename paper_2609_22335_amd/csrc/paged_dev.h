@@ -1,0 +1,110 @@
+// Device helpers of the paged cache's kernels.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "kernels.h"
+#include "paged.h"
+
+namespace vla {
+namespace pg {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+// A lane's chunk: 16 bytes of a row, VEC elements.
+template <typename T>
+struct El;
+template <>
+struct El<float> {
+  static constexpr int VEC = 4;
+};
+template <>
+struct El<uint16_t> {
+  static constexpr int VEC = 8;
+};
+
+// round to nearest, ties to even (the hardware conversion)
+__device__ __forceinline__ uint32_t bf2(float lo, float hi) {
+  return (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)lo) |
+         ((uint32_t)__builtin_bit_cast(uint16_t, (__bf16)hi) << 16);
+}
+__device__ __forceinline__ void unpack(uint4 u, float (&x)[8]) {
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = __uint_as_float(w[i] << 16);
+    x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+  }
+}
+__device__ __forceinline__ void unpack(uint4 u, float (&x)[4]) {
+  x[0] = __uint_as_float(u.x);
+  x[1] = __uint_as_float(u.y);
+  x[2] = __uint_as_float(u.z);
+  x[3] = __uint_as_float(u.w);
+}
+__device__ __forceinline__ uint4 pack(const float (&x)[8]) {
+  return make_uint4(bf2(x[0], x[1]), bf2(x[2], x[3]), bf2(x[4], x[5]), bf2(x[6], x[7]));
+}
+__device__ __forceinline__ uint4 pack(const float (&x)[4]) {
+  return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+}
+
+// The entry whose rows hold row t, by the whole wave: the largest e <= n with
+// start[e] <= t (start[0] is taken to be; n: t lies behind the last entry).
+// 64 entries a step, so 4,096 entries take two round trips. Every index stays
+// in [1, n] whatever the values are.
+__device__ __forceinline__ int wave_find(const int32_t* start, int n, int t) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, len = n;
+  while (len > 64) {
+    const int step = (len + 63) / 64;
+    const int i = (lane + 1) * step;
+    const int c = __popcll(__ballot(start[lo + (i < len ? i : len)] <= t));
+    if (c * step >= len) return lo + len;
+    lo += c * step;
+    len = len - c * step < step ? len - c * step : step;
+  }
+  return lo + __popcll(__ballot(lane < len && start[lo + (lane < len ? lane + 1 : len)] <= t));
+}
+
+// What an entry of a batch is: its sequence (-1: none), first row, rows,
+// committed slots and the slots that its pages hold. Rows and slots are
+// clamped so that whatever the arrays hold, rows lie in [0, n_rows) and slots
+// in the table.
+struct Entry {
+  int seq, row0, n, len, cap;
+};
+__device__ __forceinline__ Entry entry_of(const PagedCache& c, const PagedRows& r, int e) {
+  Entry x;
+  const int a = r.start[e], b = r.start[e + 1];
+  x.row0 = a < 0 ? 0 : a > r.n_rows ? r.n_rows : a;
+  const int end = b > r.n_rows ? r.n_rows : b;
+  x.n = end > x.row0 ? end - x.row0 : 0;
+  x.seq = r.seqs ? r.seqs[e] : e;
+  if (x.seq < 0 || x.seq >= c.n_seqs) {
+    x.seq = -1;
+    x.n = x.len = x.cap = 0;
+    return x;
+  }
+  int h = c.held[x.seq];
+  h = h < 0 ? 0 : h > c.max_pages ? c.max_pages : h;
+  x.cap = h << c.page_lg;
+  const int l = c.lens[x.seq];
+  x.len = l < 0 ? 0 : l > x.cap ? x.cap : l;
+  return x;
+}
+
+// The page of a slot of sequence s (-1: none).
+__device__ __forceinline__ int page_of(const PagedCache& c, int s, int slot, int cap) {
+  if (slot < 0 || slot >= cap) return -1;
+  const int p = c.table[(size_t)s * c.max_pages + (slot >> c.page_lg)];
+  return (unsigned)p < (unsigned)c.n_pages ? p : -1;
+}
+// Elements before slot `at` of KV head j in page p of a layer.
+__device__ __forceinline__ size_t slot_elem(const PagedCache& c, int layer, int p, int j, int at) {
+  return ((((size_t)layer * c.n_pages + p) * c.nkv + j) * c.page + at) * c.hd;
+}
+__device__ __forceinline__ void flag(const PagedCache& c, int bit) { atomicOr(c.status, bit); }
+
+}  // namespace pg
+}  // namespace vla

@@ -24,6 +24,7 @@
 #include "../../include/vla.h"
 #include "gen.h"
 #include "kernels.h"
+#include "paged.h"
 
 using namespace vla;
 
@@ -3247,6 +3248,245 @@ int vla_debug_generate(uint64_t seed, const char* name, int64_t n, double mean, 
     if (!name || !host_dst || n < 0) return fail(VLA_EINVAL, "bad argument");
     gen_normal(seed, name, (size_t)n, mean, stdv, host_dst);
     return VLA_OK;
+  })
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------------------
+// Paged cache: argument checks and descriptors of the calls on it
+// ---------------------------------------------------------------------------
+
+static bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
+// Device descriptor of a caller's cache. Limits keep every index that the
+// kernels form in 32 bits (slots, pages, table entries of a sequence) in range.
+static int paged_cache(const vla_pages* p, PagedCache* c) {
+  if (!p) return fail(VLA_EINVAL, "pages is NULL");
+  if (p->dtype != VLA_F32 && p->dtype != VLA_BF16) return fail(VLA_EINVAL, "pages: dtype");
+  if (p->layers <= 0 || p->kv_heads <= 0 || p->n_pages <= 0 || p->n_seqs <= 0 || p->max_pages <= 0)
+    return fail(VLA_EINVAL, "pages: every size must be positive");
+  if (p->head_dim <= 0 || p->head_dim % 32 || p->head_dim > (p->dtype == VLA_F32 ? 128 : 256))
+    return fail(VLA_EINVAL, "pages: head_dim must be a multiple of 32, at most 256 (fp32: 128)");
+  int lg = 4;
+  while (lg < 8 && (1 << lg) != p->page_len) ++lg;
+  if ((1 << lg) != p->page_len) return fail(VLA_EINVAL, "pages: page_len must be 16, 32, 64, 128 or 256");
+  if (p->n_pages > (1 << 28) || p->n_seqs > (1 << 24) || p->layers > (1 << 16) || p->kv_heads > (1 << 12) ||
+      (int64_t)p->max_pages * p->page_len > (1 << 30))
+    return fail(VLA_EINVAL, "pages: sizes above 2^28 pages, 2^24 sequences or 2^30 slots of a sequence");
+  if (!p->k || !p->v || !p->table || !p->lens || !p->held || !p->refs || !p->status)
+    return fail(VLA_EINVAL, "pages: NULL array");
+  if (!aligned16(p->k) || !aligned16(p->v)) return fail(VLA_EINVAL, "pages: k and v must be 16-byte aligned");
+  c->dtype = p->dtype == VLA_BF16 ? DT_BF16 : DT_F32;
+  c->layers = p->layers;
+  c->nkv = p->kv_heads;
+  c->hd = p->head_dim;
+  c->page = p->page_len;
+  c->page_lg = lg;
+  c->n_pages = p->n_pages;
+  c->n_seqs = p->n_seqs;
+  c->max_pages = p->max_pages;
+  c->k = p->k;
+  c->v = p->v;
+  c->table = p->table;
+  c->lens = p->lens;
+  c->held = p->held;
+  c->refs = p->refs;
+  c->status = p->status;
+  return VLA_OK;
+}
+
+static int paged_rows(const vla_rows* p, PagedRows* r) {
+  if (!p) return fail(VLA_EINVAL, "rows is NULL");
+  if (p->n_rows < 0 || p->n_rows > (1 << 28) || p->n_entries < 0 || p->n_entries > (1 << 24))
+    return fail(VLA_EINVAL, "rows: n_rows (at most 2^28) or n_entries (at most 2^24)");
+  if (p->n_entries > 0 && !p->start) return fail(VLA_EINVAL, "rows: start is NULL");
+  r->n_rows = p->n_rows;
+  r->n_ent = p->n_entries;
+  r->start = p->start;
+  r->seqs = p->seqs;
+  return VLA_OK;
+}
+
+// `heads` heads to a row, rows `ld` elements apart.
+static int paged_operand(const PagedCache& c, const char* what, const void* p, int64_t ld, int64_t heads) {
+  if (!p) return fail(VLA_EINVAL, std::string(what) + " is NULL");
+  const int esz = c.dtype == DT_BF16 ? 2 : 4;
+  if (!aligned16(p) || ld * esz % 16)
+    return fail(VLA_EINVAL, std::string(what) + ": base and rows must be 16-byte aligned");
+  if (ld < heads * c.hd || ld > ((int64_t)1 << 31)) return fail(VLA_EINVAL, std::string(what) + ": row stride");
+  return VLA_OK;
+}
+
+static int paged_layer(const PagedCache& c, int32_t layer, int32_t nq) {
+  if (layer < 0 || layer >= c.layers) return fail(VLA_EINVAL, "layer outside the cache");
+  if (nq <= 0 || nq % c.nkv || nq > (1 << 16)) return fail(VLA_EINVAL, "nq must be a multiple of kv_heads");
+  return VLA_OK;
+}
+
+static int paged_launch(const char* what, hipError_t e) {
+  if (e == hipErrorInvalidValue) return fail(VLA_EUNSUPPORTED, std::string(what) + ": more workgroups than a grid holds");
+  if (e != hipSuccess) return fail(VLA_EHIP, std::string(what) + ": " + hipGetErrorString(e));
+  return VLA_OK;
+}
+
+// CUs of the current device, looked up once per device.
+static int device_cus(int* out) {
+  static std::mutex mu;
+  static int known[NOALLOC_MAX_DEVICES] = {};
+  int dev = 0;
+  HIP_TRY(hipGetDevice(&dev));
+  if (dev < 0 || dev >= NOALLOC_MAX_DEVICES) return fail(VLA_EUNSUPPORTED, "device index above 63");
+  std::lock_guard<std::mutex> lock(mu);
+  if (!known[dev]) HIP_TRY(hipDeviceGetAttribute(&known[dev], hipDeviceAttributeMultiprocessorCount, dev));
+  *out = known[dev];
+  return VLA_OK;
+}
+
+extern "C" {
+
+int vla_pages_init(const vla_pages* p, void* stream) {
+  ABI_GUARD({
+    PagedCache c;
+    VLA_TRY(paged_cache(p, &c));
+    return paged_launch("pages init", launch_pages_init(c, (hipStream_t)stream));
+  })
+}
+
+int vla_pages_reserve(const vla_pages* p, const vla_rows* rows, void* stream) {
+  ABI_GUARD({
+    PagedCache c;
+    PagedRows r;
+    VLA_TRY(paged_cache(p, &c));
+    VLA_TRY(paged_rows(rows, &r));
+    return paged_launch("pages reserve", launch_pages_reserve(c, r, (hipStream_t)stream));
+  })
+}
+
+int vla_qk_norm_rope(const vla_pages* p, int32_t layer, const vla_rows* rows, const vla_rope_norm* n,
+                     const int32_t* pos, int32_t nq, const void* q, int64_t ldq, const void* k, int64_t ldk,
+                     const void* v, int64_t ldv, void* q_out, int64_t ldo, void* stream) {
+  ABI_GUARD({
+    RopeNormDesc d;
+    VLA_TRY(paged_cache(p, &d.c));
+    VLA_TRY(paged_rows(rows, &d.r));
+    VLA_TRY(paged_layer(d.c, layer, nq));
+    if (!n) return fail(VLA_EINVAL, "rope_norm is NULL");
+    if (n->rot_dim < 0 || n->rot_dim % 16 || n->rot_dim > d.c.hd)
+      return fail(VLA_EINVAL, "rot_dim must be a multiple of 16, at most head_dim");
+    if (n->rot_dim && (!n->cos_tab || !n->sin_tab || n->n_pos <= 0))
+      return fail(VLA_EINVAL, "a rotation needs both tables");
+    if ((n->q_gain || n->k_gain) && !(n->eps > 0.f)) return fail(VLA_EINVAL, "eps must be positive");
+    if (!aligned16(n->q_gain) || !aligned16(n->k_gain) || !aligned16(n->cos_tab) || !aligned16(n->sin_tab))
+      return fail(VLA_EINVAL, "gains and tables must be 16-byte aligned");
+    if (d.r.n_rows == 0 || d.r.n_ent == 0) return VLA_OK;  // nothing is read or written
+    VLA_TRY(paged_operand(d.c, "q", q, ldq, nq));
+    VLA_TRY(paged_operand(d.c, "k", k, ldk, d.c.nkv));
+    VLA_TRY(paged_operand(d.c, "v", v, ldv, d.c.nkv));
+    VLA_TRY(paged_operand(d.c, "q_out", q_out, ldo, nq));
+    if (q_out == q && ldo != ldq) return fail(VLA_EINVAL, "q_out may be q only with q's row stride");
+    d.layer = layer;
+    d.nq = nq;
+    d.q = q;
+    d.k = k;
+    d.v = v;
+    d.ldq = ldq;
+    d.ldk = ldk;
+    d.ldv = ldv;
+    d.q_out = q_out;
+    d.ldo = ldo;
+    d.q_gain = n->q_gain;
+    d.k_gain = n->k_gain;
+    d.gain_plus_one = n->gain_plus_one ? 1 : 0;
+    d.eps = n->eps;
+    d.cs = n->cos_tab;
+    d.sn = n->sin_tab;
+    d.n_pos = n->n_pos;
+    d.rot = n->rot_dim;
+    d.pos = pos;
+    return paged_launch("qk_norm_rope", launch_rope_norm(d, (hipStream_t)stream));
+  })
+}
+
+static int tree_desc(const vla_pages* p, const vla_rows* rows, int32_t layer, int32_t nq, TreeAttnDesc* d) {
+  VLA_TRY(paged_cache(p, &d->c));
+  VLA_TRY(paged_rows(rows, &d->r));
+  VLA_TRY(paged_layer(d->c, layer, nq));
+  if ((int64_t)d->r.n_rows * (nq / d->c.nkv) > (1 << 30))
+    return fail(VLA_EUNSUPPORTED, "more than 2^30 query rows to a KV head");
+  d->layer = layer;
+  d->nq = nq;
+  return device_cus(&d->cus);
+}
+
+int vla_tree_attention_scratch(const vla_pages* p, const vla_rows* rows, int32_t nq, int64_t* bytes) {
+  ABI_GUARD({
+    if (!bytes) return fail(VLA_EINVAL, "bytes is NULL");
+    TreeAttnDesc d;
+    VLA_TRY(tree_desc(p, rows, 0, nq, &d));
+    *bytes = (int64_t)tree_attn_scratch(d);
+    return VLA_OK;
+  })
+}
+
+int vla_tree_attention(const vla_pages* p, int32_t layer, const vla_rows* rows, const uint32_t* mask,
+                       int32_t mask_words, int32_t nq, float scale, const void* q, int64_t ldq, void* out,
+                       int64_t ldo, void* scratch, int64_t scratch_bytes, void* stream) {
+  ABI_GUARD({
+    TreeAttnDesc d;
+    VLA_TRY(tree_desc(p, rows, layer, nq, &d));
+    if (mask && (mask_words <= 0 || mask_words > (1 << 24))) return fail(VLA_EINVAL, "mask_words");
+    if (!(scale > 0.f) || !std::isfinite(scale)) return fail(VLA_EINVAL, "scale must be positive and finite");
+    if (d.r.n_rows == 0 || d.r.n_ent == 0) return VLA_OK;  // nothing is read or written
+    VLA_TRY(paged_operand(d.c, "q", q, ldq, nq));
+    VLA_TRY(paged_operand(d.c, "out", out, ldo, nq));
+    const size_t need = tree_attn_scratch(d);
+    if (!scratch || !aligned16(scratch) || scratch_bytes < 0 || (size_t)scratch_bytes < need)
+      return fail(VLA_EINVAL, "scratch: needs " + std::to_string(need) + " bytes, 16-byte aligned");
+    d.mask = mask;
+    d.mask_words = mask ? mask_words : 0;
+    d.scale = scale;
+    d.q = q;
+    d.ldq = ldq;
+    d.out = out;
+    d.ldo = ldo;
+    d.scratch = scratch;
+    return paged_launch("tree_attention", launch_tree_attn(d, (hipStream_t)stream));
+  })
+}
+
+int vla_pages_fork(const vla_pages* p, int32_t n, const int32_t* src, const int32_t* dst, int32_t* made,
+                   void* stream) {
+  ABI_GUARD({
+    PagedCache c;
+    VLA_TRY(paged_cache(p, &c));
+    if (n < 0 || n > (1 << 24)) return fail(VLA_EINVAL, "n must be in 0 .. 2^24");
+    if (n == 0) return VLA_OK;
+    if (!src || !dst || !made) return fail(VLA_EINVAL, "NULL argument");
+    return paged_launch("pages fork", launch_pages_fork(c, n, src, dst, made, (hipStream_t)stream));
+  })
+}
+
+int vla_pages_commit(const vla_pages* p, const vla_rows* rows, const int32_t* kept, const int32_t* n_kept,
+                     void* stream) {
+  ABI_GUARD({
+    PagedCache c;
+    PagedRows r;
+    VLA_TRY(paged_cache(p, &c));
+    VLA_TRY(paged_rows(rows, &r));
+    if (kept && !n_kept) return fail(VLA_EINVAL, "kept needs n_kept");
+    return paged_launch("pages commit", launch_pages_commit(c, r, kept, n_kept, (hipStream_t)stream));
+  })
+}
+
+int vla_pages_release(const vla_pages* p, int32_t n, const int32_t* seqs, void* stream) {
+  ABI_GUARD({
+    PagedCache c;
+    VLA_TRY(paged_cache(p, &c));
+    if (n < 0 || n > (1 << 24)) return fail(VLA_EINVAL, "n must be in 0 .. 2^24");
+    if (n == 0) return VLA_OK;
+    if (!seqs) return fail(VLA_EINVAL, "seqs is NULL");
+    return paged_launch("pages release", launch_pages_release(c, n, seqs, (hipStream_t)stream));
   })
 }
 
