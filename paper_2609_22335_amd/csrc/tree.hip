@@ -19,6 +19,12 @@ namespace {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+// Pointers into the LDS are typed as such: the compiler must not lose sight of
+// their address space.
+#define LDS_AS __attribute__((address_space(3)))
+typedef LDS_AS unsigned char LB;
 typedef __amdgpu_buffer_rsrc_t Rsrc;
 constexpr uint32_t OOB = 0x80000000u;
 constexpr float LOG2E = 1.4426950408889634f;
@@ -32,7 +38,7 @@ __device__ __forceinline__ void wait_vm() {
 }
 __device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 __device__ __forceinline__ void barrier() {
-  asm volatile("" ::: "memory");
+  wait_lds();  // (this wave's writes are in the LDS; loads into it may be on their way)
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
@@ -89,81 +95,103 @@ struct Geo {
   }
 };
 
-// What every workgroup works out for itself: all entries' blocks in a row,
-// dealt out in equal runs, so that uneven sequences load the chip evenly.
-// Lanes hold 64 entries at a time.
-template <int BM, int BN>
-struct Deal {
-  long long total = 0;
-  int chunk0 = 0;          // first entry of the lanes' chunk
-  long long base = 0;      // blocks before the chunk
-  long long incl = 0;      // inclusive prefix of the lane's entry in it
-  long long units = 0;     // the lane's entry's blocks
-  int persum = 0;          // of one head
-  Entry x;
+// A run of key blocks of one tile: what a workgroup does next. Worked out by
+// one wave, read by all.
+struct Seg {
+  int seq, row0, n, len, cap;  // the entry
+  int head, rt, b0, b1, nb;    // tile and its blocks [b0, b1) of nb
+  long long quota, total;
+};
 
-  __device__ __forceinline__ void load(const Args& a, int c0) {
-    const int e = c0 + (threadIdx.x & 63);
-    units = 0;
-    persum = 0;
-    x = Entry{-1, 0, 0, 0, 0};
-    if (e < a.r.n_ent) {
-      x = entry_of(a.c, a.r, e);
+// All entries' blocks stand in a row and are dealt out in equal runs, so that
+// uneven sequences load the chip evenly. Finds the run's segment at unit u (of
+// the run's end, u_end), or with u < 0 the length of a run. One wave; lanes
+// hold 64 entries at a time.
+template <int BM, int BN>
+__device__ __forceinline__ void deal(const Args& a, Seg* sg, long long u, long long u_end) {
+  const int lane = threadIdx.x & 63;
+  auto lane_of = [](long long v, int i) {
+    const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)v, i);
+    const uint32_t hi = __builtin_amdgcn_readlane((int)(v >> 32), i);
+    return (long long)(((unsigned long long)hi << 32) | lo);
+  };
+  long long base = 0;
+  for (int c0 = 0; c0 < a.r.n_ent; c0 += 64) {
+    long long units = 0;
+    int persum = 0;
+    Entry x{-1, 0, 0, 0, 0};
+    if (c0 + lane < a.r.n_ent) {
+      x = entry_of(a.c, a.r, c0 + lane);
       Geo<BM, BN> g;
       g.set(a, x);
       persum = g.sum();
       units = (long long)persum * a.c.nkv;
     }
-    incl = units;
+    long long incl = units;
 #pragma unroll
     for (int m = 1; m < 64; m *= 2) {
       const long long y = __shfl_up(incl, m);
-      if ((threadIdx.x & 63) >= m) incl += y;
+      if (lane >= m) incl += y;
     }
-    chunk0 = c0;
-  }
-  // lane i's value in every lane, in scalar registers
-  static __device__ __forceinline__ long long lane_of(long long v, int i) {
-    const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)v, i);
-    const int hi = __builtin_amdgcn_readlane((int)(v >> 32), i);
-    return (long long)(((unsigned long long)(uint32_t)hi << 32) | lo);
-  }
-  __device__ __forceinline__ void init(const Args& a) {
-    total = 0;
-    for (int c0 = 0; c0 < a.r.n_ent; c0 += 64) {
-      load(a, c0);
-      total += lane_of(incl, 63);
+    const long long all = lane_of(incl, 63);
+    if (u >= 0 && u < base + all) {
+      const int el = __ffsll(__ballot(base + incl > u)) - 1;
+      x.seq = __builtin_amdgcn_readlane(x.seq, el);
+      x.row0 = __builtin_amdgcn_readlane(x.row0, el);
+      x.n = __builtin_amdgcn_readlane(x.n, el);
+      x.len = __builtin_amdgcn_readlane(x.len, el);
+      x.cap = __builtin_amdgcn_readlane(x.cap, el);
+      persum = __builtin_amdgcn_readlane(persum, el);
+      const long long at = u - (base + lane_of(incl, el) - lane_of(units, el));
+      Geo<BM, BN> g;
+      g.set(a, x);
+      const int head = (int)(at / persum);
+      int rem = (int)(at - (long long)head * persum), rt = 0;
+      if (g.causal) {
+        while (rem >= g.nb(rt)) rem -= g.nb(rt), ++rt;
+      } else {
+        rt = rem / g.nb_all;
+        rem -= rt * g.nb_all;
+      }
+      if (lane == 0) {
+        sg->seq = x.seq;
+        sg->row0 = x.row0;
+        sg->n = x.n;
+        sg->len = x.len;
+        sg->cap = x.cap;
+        sg->head = head;
+        sg->rt = rt;
+        sg->nb = g.nb(rt);
+        sg->b0 = rem;
+        sg->b1 = (int)(sg->nb - rem < u_end - u ? sg->nb : rem + (u_end - u));
+      }
+      return;
     }
-    if (a.r.n_ent > 64) load(a, 0);
-    base = 0;
+    base += all;
   }
-  // The entry that holds unit u (chunks are only walked forward).
-  __device__ __forceinline__ int locate(const Args& a, long long u) {
-    long long all = lane_of(incl, 63);
-    while (u >= base + all) {
-      base += all;
-      load(a, chunk0 + 64);
-      all = lane_of(incl, 63);
-    }
-    return __ffsll(__ballot(base + incl > u)) - 1;
+  if (lane == 0) {
+    long long q = (base + a.wgs - 1) / a.wgs;
+    sg->quota = q < a.min_quota ? a.min_quota : q;
+    sg->total = base;
   }
-};
-
-// 16-byte chunk c of row r sits at position c ^ swz(r): rows that a fragment
-// read takes together start in different banks.
-template <typename T, int HDP>
-__device__ __forceinline__ constexpr int swz(int r) {
-  constexpr int RB = HDP * (int)sizeof(T);  // bytes of a row
-  if (sizeof(T) == 4) return RB >= 256 ? (((r >> 2) & 1) << 3) | ((r & 3) << 1) | ((r >> 3) & 1) : 0;
-  if (RB >= 256) return ((r & 3) << 2) | ((r >> 2) & 3);
-  return (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
+}
+__device__ __forceinline__ int uni(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ long long uni64(long long x) {
+  return (long long)(((unsigned long long)(uint32_t)uni((int)(x >> 32)) << 32) | (uint32_t)uni((int)(uint32_t)x));
 }
 
-__device__ __forceinline__ f32x16 mma(uint4 a, uint4 b, f32x16 c, uint16_t) {
+// 16-byte chunk c of row r of a tile sits at position c ^ swz(r). Eight rows
+// read at one chunk (K fragments) start in eight different 16-byte columns of
+// a 128-byte line, four rows read at two chunks (V, transposed) in four
+// different pairs; only the low three bits of c change, so that the rest of a
+// fragment's address is an immediate.
+__device__ __forceinline__ constexpr int swz(int r) { return ((r & 3) << 1) | ((r >> 2) & 1); }
+
+__device__ __forceinline__ f32x16 mma(u32x4 a, u32x4 b, f32x16 c, uint16_t) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0,
                                                  0);
 }
-__device__ __forceinline__ f32x16 mma(uint4 a, uint4 b, f32x16 c, float) {
+__device__ __forceinline__ f32x16 mma(u32x4 a, u32x4 b, f32x16 c, float) {
   c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.x), __uint_as_float(b.x), c, 0, 0, 0);
   c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.y), __uint_as_float(b.y), c, 0, 0, 0);
   c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.z), __uint_as_float(b.z), c, 0, 0, 0);
@@ -184,369 +212,560 @@ __device__ __forceinline__ float sum_x32(float x) {
 }
 __device__ __forceinline__ float ex2(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// RW row groups of 32 rows and KW = 4 / RW key groups of 32 keys to the four
-// waves: RW = 1 for few rows (each wave streams its own keys, the waves'
-// results are merged at the end), RW = 4 for many.
-template <typename T, int HDP, int RW>
-__global__ __launch_bounds__(256, 1) void k_tree(Args a) {
-  constexpr int KW = 4 / RW, BM = 32 * RW, BN = 32 * KW;
-  constexpr int ESZ = sizeof(T), RB = HDP * ESZ, CPR = RB / 16;  // row bytes, chunks
-  constexpr int RPI = 1024 / RB;                                 // rows of a load
-  constexpr int NI = 32 / RPI, NIW = NI / RW;                    // loads of a key group's tile, a wave's
-  constexpr int NQ = RB / 32, NDT = HDP / 32;
-  constexpr bool HALF = ESZ == 2;
-  static_assert(NIW >= 1 && 2 * NIW < 60, "loads in flight");
-  __shared__ __attribute__((aligned(1024))) unsigned char sK[KW][32 * RB];
-  __shared__ __attribute__((aligned(1024))) unsigned char sV[KW][32 * RB];
-  __shared__ float sM[4][32], sL[4][32];
+// What a lane knows of a segment's tile.
+struct Tile {
+  int seq, row0, len, cap, head, rt, b0, b1, nb;
+  int M, group, kend;
+  bool causal;
+};
+template <int BM, int BN>
+__device__ __forceinline__ Tile tile_of(const Args& a, const Seg& g) {
+  Tile t;
+  t.seq = uni(g.seq);
+  t.row0 = uni(g.row0);
+  t.len = uni(g.len);
+  t.cap = uni(g.cap);
+  t.head = uni(g.head);
+  t.rt = uni(g.rt);
+  t.b0 = uni(g.b0);
+  t.b1 = uni(g.b1);
+  t.nb = uni(g.nb);
+  Geo<BM, BN> geo;
+  geo.set(a, Entry{t.seq, t.row0, uni(g.n), t.len, t.cap});
+  t.M = geo.M;
+  t.group = geo.group;
+  t.causal = geo.causal;
+  t.kend = geo.tile_end(t.rt);
+  return t;
+}
 
-  const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int kg = RW == 1 ? wv : 0, rw = RW == 1 ? 0 : wv;
-  const int l32 = lane & 31, h = lane >> 5;
-  const int hd = a.c.hd;
-  // consecutive runs of blocks on one XCD (workgroups go round the eight)
-  const int w = (int)(blockIdx.x & 7) * (a.wgs >> 3) + (int)(blockIdx.x >> 3);
+// Loads of 32 keys' K or V into the LDS, by the part `part` of PARTS waves.
+// They reach at most one page's part of one head, from its base: slots behind
+// the last key and chunks behind the head dim lie out of the resource's range
+// and become zeros. Pages are scalar loads (ids), given by the caller.
+template <typename T, int HDP, int PARTS>
+struct Loader {
+  static constexpr int RB = HDP * (int)sizeof(T), CPR = RB / 16, RPI = 1024 / RB, NI = 32 / RPI;
+  int lrow, lchunk, hb;  // the lane's row and chunk of a load; bytes of a row in memory
+  size_t pbytes;         // a page's part of one KV head
+  uint32_t hoff;         // (the head's part, in pages)
+  const __attribute__((address_space(4))) int32_t* table;
 
-  Deal<BM, BN> deal;
-  deal.init(a);
-  long long quota = (deal.total + a.wgs - 1) / a.wgs;
-  if (quota < a.min_quota) quota = a.min_quota;
-  long long u = w * quota;
-  const long long u_end = u + quota < deal.total ? u + quota : deal.total;
-  int4 desc = make_int4(0, 0, 0, 0);
+  __device__ __forceinline__ void set(const Args& a, const Tile& t) {
+    const int lane = threadIdx.x & 63;
+    lrow = lane / CPR;
+    lchunk = (lane % CPR) ^ swz(lrow);
+    hb = a.c.hd * (int)sizeof(T);
+    pbytes = (size_t)a.c.page * hb;
+    hoff = t.head;
+    table = (const __attribute__((address_space(4))) int32_t*)(a.c.table + (size_t)t.seq * a.c.max_pages);
+  }
+  // pages of slots kb and kb + 16 (the two halves may lie in different ones)
+  __device__ __forceinline__ int2 ids(const Args& a, const Tile& t, int kb) const {
+    const int p0 = kb < t.kend ? table[kb >> a.c.page_lg] : -1;
+    const int p1 = kb + 16 < t.kend ? table[(kb + 16) >> a.c.page_lg] : -1;
+    return make_int2(p0, p1);
+  }
+  __device__ __forceinline__ void issue(const Args& a, const Tile& t, const char* src, LB* dst, int kb,
+                                        int2 id, int part) const {
+#pragma unroll
+    for (int hh = 0; hh < 2; ++hh) {
+      const int s0 = kb + 16 * hh, pid = hh ? id.y : id.x;
+      const bool ok = (unsigned)pid < (unsigned)a.c.n_pages;
+      const int at = s0 & (a.c.page - 1);
+      int have = t.kend - (s0 - at);  // keys from the page's first slot on
+      have = !ok || have < 0 ? 0 : have > a.c.page ? a.c.page : have;
+      const Rsrc rs = __builtin_amdgcn_make_buffer_rsrc(
+          const_cast<char*>(src) + ((size_t)(ok ? pid : 0) * a.c.nkv + hoff) * pbytes, (short)0, have * hb,
+          0x00020000);
+      constexpr int PER = NI / 2;  // loads of a half
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        const int idx = hh * PER + i;
+        if (PARTS > 1 && (NI >= PARTS ? idx % PARTS != part : idx != part)) continue;
+        const int r0 = idx * RPI;
+        const int ch = lchunk ^ swz(r0);
+        uint32_t off = (uint32_t)((at + (r0 & 15) + lrow) * hb + ch * 16);
+        if (HDP * (int)sizeof(T) != hb && ch * 16 >= hb) off = OOB;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (LDS_AS void*)(dst + idx * 1024), 16,
+                                                 off, 0, 0, 0);
+      }
+    }
+  }
+};
 
-  // the lane's part of a load: row and 16-byte chunk
-  const int lrow = lane / CPR, lpos = lane % CPR;
-  const int lchunk = lpos ^ swz<T, HDP>(lrow);
-
-  while (u < u_end) {
-    const int el = deal.locate(a, u);
-    Entry x;
-    x.seq = __builtin_amdgcn_readlane(deal.x.seq, el);
-    x.row0 = __builtin_amdgcn_readlane(deal.x.row0, el);
-    x.n = __builtin_amdgcn_readlane(deal.x.n, el);
-    x.len = __builtin_amdgcn_readlane(deal.x.len, el);
-    x.cap = __builtin_amdgcn_readlane(deal.x.cap, el);
-    const int persum = __builtin_amdgcn_readlane(deal.persum, el);
-    Geo<BM, BN> g;
-    g.set(a, x);
-    const long long first = deal.base + deal.lane_of(deal.incl, el) - deal.lane_of(deal.units, el);
-    const int head = (int)((u - first) / persum);
-    int rem = (int)(u - first - (long long)head * persum);
-    int rt = 0;
-    if (g.causal) {
-      while (rem >= g.nb(rt)) rem -= g.nb(rt), ++rt;
+// Bit i: this lane's query sees slot kb + i (kb + 32 may pass the last key).
+__device__ __forceinline__ uint32_t seen_bits(const Args& a, const Tile& t, int kb, int own, int row) {
+  const int n = own - kb;
+  uint32_t see = n >= 32 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << n) - 1u;
+  if (!t.causal && kb + 32 > t.len) {
+    const int j0 = kb - t.len;  // draft of bit 0
+    uint32_t bits;
+    const uint32_t* mw = a.mask + (size_t)row * a.mask_words;
+    if (j0 >= 0) {
+      const int wi = j0 >> 5, sh = j0 & 31;
+      const uint32_t lo = wi < a.mask_words ? mw[wi] : 0u, hi = wi + 1 < a.mask_words ? mw[wi + 1] : 0u;
+      bits = sh ? (lo >> sh) | (hi << (32 - sh)) : lo;
     } else {
-      rt = rem / g.nb_all;
-      rem -= rt * g.nb_all;
+      bits = (mw[0] << -j0) | ((1u << -j0) - 1u);
     }
-    const int nb = g.nb(rt), b0 = rem;
-    const int b1 = (int)(nb - b0 < u_end - u ? nb : b0 + (u_end - u));
-    const int kend = g.tile_end(rt);
+    see &= bits;
+  }
+  return see;
+}
 
-    // this lane's query
-    const int m = rt * BM + rw * 32 + l32;
-    const bool mine = m < g.M;
-    const int mc = mine ? m : g.M - 1;
-    const int tok = mc / g.group, row = x.row0 + tok;
-    uint4 qf[NQ];
-    {
-      const T* qp = (const T*)a.q + (size_t)row * (size_t)a.ldq +
-                    (size_t)(head * g.group + (mc - tok * g.group)) * hd;
+// S^T of 32 keys (rows) and the lane's query.
+template <typename T, int HDP, int NQ>
+__device__ __forceinline__ f32x16 scores(const LB* kt, const u32x4 (&qf)[NQ]) {
+  constexpr int RB = HDP * (int)sizeof(T);
+  const int l32 = threadIdx.x & 31, h = (threadIdx.x >> 5) & 1;
+  const LB* base = kt + l32 * RB;
+  const int x = (h ^ swz(l32)) * 16;
+  f32x16 s;
 #pragma unroll
-      for (int s = 0; s < NQ; ++s) {
-        const int d0 = (2 * s + h) * El<T>::VEC;
-        qf[s] = d0 < hd ? *(const uint4*)(qp + d0) : make_uint4(0, 0, 0, 0);
+  for (int j = 0; j < 16; ++j) s[j] = 0.f;
+#pragma unroll
+  for (int t = 0; t < NQ; ++t) {
+    const u32x4 kf = *(const LDS_AS u32x4*)(base + (x ^ ((t & 3) * 32)) + (t >> 2) * 128);
+    s = mma(kf, qf[t], s, T());
+  }
+  return s;
+}
+
+// Probabilities as operands of the second product: in bf16 rounded once, or
+// (TWO) as the sum of two bf16 values, where the matrix cores wait for memory
+// anyway.
+struct Probs {
+  u32x4 hi[2], lo[2];
+};
+template <bool TWO>
+__device__ __forceinline__ void round_probs(const f32x16& s, Probs& p) {
+#pragma unroll
+  for (int kk = 0; kk < 2; ++kk) {
+    uint32_t hw[4], lw[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float p0 = s[8 * kk + 2 * i], p1 = s[8 * kk + 2 * i + 1];
+      hw[i] = bf2(p0, p1);
+      if (TWO) lw[i] = bf2(p0 - __uint_as_float(hw[i] << 16), p1 - __uint_as_float(hw[i] & 0xFFFF0000u));
+    }
+    p.hi[kk] = u32x4{hw[0], hw[1], hw[2], hw[3]};
+    if (TWO) p.lo[kk] = u32x4{lw[0], lw[1], lw[2], lw[3]};
+  }
+}
+
+// O^T += V^T P^T over 32 keys.
+template <typename T, int HDP, bool TWO>
+__device__ __forceinline__ void add_values(const LB* vt, const f32x16& s, const Probs& p,
+                                           f32x16 (&o)[HDP / 32]) {
+  constexpr int RB = HDP * (int)sizeof(T), NDT = HDP / 32;
+  const int lane = threadIdx.x & 63, l32 = lane & 31, h = lane >> 5;
+  if constexpr (sizeof(T) == 2) {
+    // 16 lanes read four keys of 16 head-dim columns, transposed: lane i gets
+    // column i, the operand's keys 4 h .. + 3 and 8 + 4 h .. + 3 of each 16
+    const int il = lane & 15;
+    const LB* base = vt + (4 * h + (il >> 2)) * RB + 8 * (il & 1);
+    const int x = ((2 * ((lane >> 4) & 1) + ((il & 3) >> 1)) ^ swz(4 * h + (il >> 2))) * 16;
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+      for (int dt = 0; dt < NDT; ++dt) {
+        auto tr = [&](int k0) {
+          const LB* q = base + (x ^ ((dt & 1) * 64)) + (dt >> 1) * 128 + k0 * RB;
+          return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)q));
+        };
+        const u32x2 u0 = tr(16 * kk), u1 = tr(16 * kk + 8);
+        const u32x4 vf = {u0.x, u0.y, u1.x, u1.y};
+        o[dt] = mma(vf, p.hi[kk], o[dt], T());
+        if (TWO) o[dt] = mma(vf, p.lo[kk], o[dt], T());
+      }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      const int k0 = 8 * (j / 4) + j % 4, key = k0 + 4 * h;
+#pragma unroll
+      for (int dt = 0; dt < NDT; ++dt) {
+        const int d = 32 * dt + l32;
+        const float v = *(const LDS_AS float*)(vt + key * RB + (((d / 4) ^ swz(key)) * 16) + (d % 4) * 4);
+        o[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[j], o[dt], 0, 0, 0);
       }
     }
-    // slots below `own` are seen; the wave needs no mask below `safe`
-    const int own = g.causal ? (x.len + tok + 1 < kend ? x.len + tok + 1 : kend) : kend;
-    const int m0 = rt * BM + rw * 32;
-    const int safe0 = g.causal ? x.len + (m0 < g.M ? m0 : g.M - 1) / g.group + 1 : x.len;
-    const int safe = safe0 < kend ? safe0 : kend;
+  }
+}
 
-    const int32_t* table = a.c.table + (size_t)x.seq * a.c.max_pages;
-    const size_t pbytes = (size_t)a.c.page * hd * ESZ;  // a page's part of one KV head
-    // K or V of block b into the LDS. Loads reach at most one page's part of
-    // one head, from its base; slots behind the last key and chunks behind the
-    // head dim lie out of the resource's range and become zeros.
-    auto issue = [&](const char* src, unsigned char* dst, int b) {
-      const int kb = b * BN + kg * 32;
+// A masked key's V may hold anything, and 0 x inf is not 0. In blocks of which
+// a row may be masked, values that are not finite are replaced by zeros before
+// the product (clean_values, by PARTS waves; true when there was one), and
+// added afterwards to the rows that see them (add_odd_values): a weight is
+// positive, so the sum is what the value alone makes it.
+__device__ __forceinline__ uint32_t odd_bits(uint32_t w, uint16_t) {
+  return ((w & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u) | ((w & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u);
+}
+__device__ __forceinline__ uint32_t odd_bits(uint32_t w, float) {
+  return (w & 0x7F800000u) == 0x7F800000u ? 0xFFFFFFFFu : 0u;
+}
+template <typename T, int HDP, int PARTS>
+__device__ __forceinline__ bool clean_values(LB* vt, int part) {
+  constexpr int NI = HDP * (int)sizeof(T) * 32 / 1024;
+  bool odd = false;
+#pragma unroll 1
+  for (int i = part; i < NI; i += PARTS) {
+    LDS_AS u32x4* at = (LDS_AS u32x4*)(vt + i * 1024 + (threadIdx.x & 63) * 16);
+    u32x4 c = *at;
+    const u32x4 b = {odd_bits(c.x, T()), odd_bits(c.y, T()), odd_bits(c.z, T()), odd_bits(c.w, T())};
+    if (b.x | b.y | b.z | b.w) {
+      *at = c & ~b;
+      odd = true;
+    }
+  }
+  return __any(odd);
+}
+// Slots kb .. kb + 31, of which the lane's query sees `see`.
+template <typename T, int HDP>
+__device__ __forceinline__ void add_odd_values(const Args& a, const Tile& t, int kb, uint32_t see,
+                                               f32x16 (&o)[HDP / 32]) {
+  const int h = (threadIdx.x >> 5) & 1, hd = a.c.hd;
+#pragma unroll 1
+  for (int kk = 0; kk < 32; ++kk) {
+    if (kb + kk >= t.kend) return;
+    const int p = a.c.table[(size_t)t.seq * a.c.max_pages + ((kb + kk) >> a.c.page_lg)];
+    if ((unsigned)p >= (unsigned)a.c.n_pages) continue;
+    const T* row = (const T*)a.v + (((size_t)p * a.c.nkv + t.head) * a.c.page + ((kb + kk) & (a.c.page - 1))) * hd;
 #pragma unroll
-      for (int hh = 0; hh < 2; ++hh) {
-        const int s0 = kb + 16 * hh;
-        const int pid = s0 < kend ? ((const __attribute__((address_space(4))) int32_t*)table)[s0 >> a.c.page_lg] : -1;
-        const bool ok = (unsigned)pid < (unsigned)a.c.n_pages;
-        const int at = s0 & (a.c.page - 1);
-        int have = kend - (s0 - at);  // keys from the page's first slot on
-        have = !ok || have < 0 ? 0 : have > a.c.page ? a.c.page : have;
-        const Rsrc rs = __builtin_amdgcn_make_buffer_rsrc(
-            const_cast<char*>(src) + ((size_t)(ok ? pid : 0) * a.c.nkv + head) * pbytes, (short)0, have * hd * ESZ,
-            0x00020000);
+    for (int dt = 0; dt < HDP / 32; ++dt) {
+      asm volatile("" ::: "memory");  // few loads at a time: this path is rare, its registers are not
 #pragma unroll
-        for (int i = 0; i < NI / 2; ++i) {
-          const int idx = hh * (NI / 2) + i;  // rows idx RPI .. + RPI - 1 of the tile
-          if (RW > 1 && idx % RW != rw) continue;
-          const int r0 = idx * RPI;
-          const int ch = lchunk ^ swz<T, HDP>(r0);
-          const uint32_t off = (uint32_t)((at + (r0 & 15) + lrow) * hd * ESZ + ch * 16);
-          __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void*)(dst + idx * 1024), 16,
-                                                   HDP != hd && ch * 16 >= hd * ESZ ? OOB : off, 0, 0, 0);
+      for (int j4 = 0; j4 < 4; ++j4) {
+        const int d = 32 * dt + 8 * j4 + 4 * h;
+        if (d >= hd) continue;
+        uint32_t v[4];
+        if constexpr (sizeof(T) == 2) {
+          const u32x2 u = *(const u32x2*)(row + d);
+          v[0] = u.x << 16, v[1] = u.x & 0xFFFF0000u, v[2] = u.y << 16, v[3] = u.y & 0xFFFF0000u;
+        } else {
+          const u32x4 u = *(const u32x4*)(row + d);
+          v[0] = u.x, v[1] = u.y, v[2] = u.z, v[3] = u.w;
         }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (((see >> kk) & 1u) && (v[i] & 0x7F800000u) == 0x7F800000u) o[dt][4 * j4 + i] += __uint_as_float(v[i]);
       }
-    };
+    }
+  }
+}
 
+// One step of the running softmax over NS x 32 keys: s becomes the
+// probabilities, o and l are rescaled when a row's maximum has grown by 2^8
+// or more (sums of probabilities up to 2^8 lose nothing).
+template <int NDT, int NS>
+__device__ __forceinline__ void soften(f32x16 (&s)[NS], float c2, float& mx, float& l, f32x16 (&o)[NDT]) {
+  float bm = s[0][0];
+#pragma unroll
+  for (int n = 0; n < NS; ++n)
+#pragma unroll
+    for (int j = 0; j < 16; ++j) bm = fmaxf(bm, s[n][j]);
+  bm = max_x32(bm) * c2;
+  if (__any(bm > mx + 8.f)) {
+    const float mn = fmaxf(mx, bm);
+    const float f = mn == -INFINITY ? 1.f : ex2(mx - mn);
+    mx = mn;
+    l *= f;
+#pragma unroll
+    for (int i = 0; i < NDT; ++i)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) o[i][j] *= f;
+  }
+  const float ref = mx == -INFINITY ? 0.f : mx;
+#pragma unroll
+  for (int n = 0; n < NS; ++n)
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      s[n][j] = ex2(__builtin_fmaf(s[n][j], c2, -ref));
+      l += s[n][j];
+    }
+}
+
+__device__ __forceinline__ void hide(f32x16& s, uint32_t see) {
+  const uint32_t half = see >> (4 * ((threadIdx.x >> 5) & 1));
+#pragma unroll
+  for (int j = 0; j < 16; ++j) s[j] = (half >> (8 * (j / 4) + j % 4)) & 1u ? s[j] : -INFINITY;
+}
+
+// The lane's query (row m of the tile's rows, clamped to the last).
+template <typename T, int NQ>
+__device__ __forceinline__ void load_query(const Args& a, const Tile& t, int mc, u32x4 (&qf)[NQ]) {
+  const int tok = mc / t.group, h = (threadIdx.x >> 5) & 1, hd = a.c.hd;
+  const T* qp = (const T*)a.q + (size_t)(t.row0 + tok) * (size_t)a.ldq +
+                (size_t)(t.head * t.group + (mc - tok * t.group)) * hd;
+#pragma unroll
+  for (int s = 0; s < NQ; ++s) {
+    const int d0 = (2 * s + h) * El<T>::VEC;
+    qf[s] = d0 < hd ? *(const u32x4*)(qp + d0) : u32x4{0, 0, 0, 0};
+  }
+}
+
+// Four results (d .. d + 3) of row mm of the tile, to the output.
+template <typename T>
+__device__ __forceinline__ void put_out(const Args& a, const Tile& t, int mm, int d, float inv, const float (&v)[4]) {
+  if (mm >= t.M || d >= a.c.hd) return;
+  const int tk = mm / t.group;
+  T* dst = (T*)a.out + (size_t)(t.row0 + tk) * (size_t)a.ldo +
+           (size_t)(t.head * t.group + (mm - tk * t.group)) * a.c.hd + d;
+  if constexpr (sizeof(T) == 2) *(uint2*)dst = make_uint2(bf2(v[0] * inv, v[1] * inv), bf2(v[2] * inv, v[3] * inv));
+  else *(f32x4*)dst = f32x4{v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv};
+}
+__device__ __forceinline__ float inverse(float l) { return l > 0.f || l != l ? 1.f / l : 0.f; }
+
+// The workgroup's run of blocks: calls f(tile, whole, slot) for each segment;
+// what other workgroups hold of the last tile is written down for the join.
+template <int BM, int BN, typename F>
+__device__ __forceinline__ void for_segments(const Args& a, Seg* sg, F&& f) {
+  const int wv = uni(threadIdx.x >> 6);
+  // consecutive runs on one XCD (workgroups go round the eight)
+  const int w = (int)(blockIdx.x & 7) * (a.wgs >> 3) + (int)(blockIdx.x >> 3);
+  if (wv == 0) deal<BM, BN>(a, sg, -1, 0);
+  __syncthreads();
+  const long long quota = uni64(sg->quota), total = uni64(sg->total);
+  long long u = w * quota;
+  const long long u_end = u + quota < total ? u + quota : total;
+  int4 desc = make_int4(0, 0, 0, 0);
+  while (u < u_end) {
+    if (wv == 0) deal<BM, BN>(a, sg, u, u_end);
+    __syncthreads();
+    const Tile t = tile_of<BM, BN>(a, *sg);
+    const bool whole = t.b0 == 0 && t.b1 == t.nb;
+    if (!whole && t.b0 == 0) desc = make_int4((int)((u + t.nb - 1) / quota - w) + 1, t.row0, t.head, t.rt);
+    f(t, whole, 2 * w + (t.b0 == 0 ? 1 : 0));
+    u += t.b1 - t.b0;
+    wait_vm<0>();  // no store of this tile in the next one's counts
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) a.desc[w] = desc;
+}
+
+// Few rows to a sequence: tiles of 32 rows, bound by the cache's bandwidth.
+// Each wave streams its own 32 keys of a block of 128 through its own part of
+// the LDS, without a barrier: the next K is on its way during softmax and
+// P V, the next V during the next scores. The four waves' results are merged
+// at the end.
+template <typename T, int HDP>
+__global__ __launch_bounds__(256, 1) void k_tree_few(Args a) {
+  constexpr int BM = 32, BN = 128;
+  constexpr int RB = HDP * (int)sizeof(T), NQ = RB / 32, NDT = HDP / 32;
+  typedef Loader<T, HDP, 1> Ld;
+  static_assert(2 * Ld::NI < 60, "loads in flight");
+  __shared__ __attribute__((aligned(1024))) unsigned char sK[4][32 * RB];
+  __shared__ __attribute__((aligned(1024))) unsigned char sV[4][32 * RB];
+  __shared__ float sM[4][32], sL[4][32];
+  __shared__ Seg sg;
+  for_segments<BM, BN>(a, &sg, [&](const Tile& t, bool whole, int slot) {
+    const int tid = threadIdx.x, lane = tid & 63, wv = uni(tid >> 6), l32 = lane & 31, h = lane >> 5;
+    Ld ld;
+    ld.set(a, t);
+    const int kb0 = t.b0 * BN + wv * 32;
+    LB *kl = (LB*)sK[wv], *vl = (LB*)sV[wv];
+    int2 id = ld.ids(a, t, kb0);
+    ld.issue(a, t, a.k, kl, kb0, id, 0);
+    ld.issue(a, t, a.v, vl, kb0, id, 0);
+    const int m = t.rt * BM + l32, mc = m < t.M ? m : t.M - 1, tok = mc / t.group, row = t.row0 + tok;
+    u32x4 qf[NQ];
+    load_query<T, NQ>(a, t, mc, qf);
+    // slots below `own` are seen; the tile needs no mask below `safe`
+    const int own = t.causal && t.len + tok + 1 < t.kend ? t.len + tok + 1 : t.kend;
+    const int safe0 = t.causal ? t.len + t.rt * BM / t.group + 1 : t.len;
+    const int safe = safe0 < t.kend ? safe0 : t.kend;
     f32x16 o[NDT];
 #pragma unroll
     for (int i = 0; i < NDT; ++i)
 #pragma unroll
       for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
     float mx = -INFINITY, l = 0.f;
-
-    wait_vm<0>();  // stores of the last tile are out of the count
-    barrier();     // and its use of the LDS is over
-    issue(a.k, sK[kg], b0);
-    issue(a.v, sV[kg], b0);
-    for (int b = b0; b < b1; ++b) {
-      const int kb = b * BN + kg * 32;
-      const bool more = b + 1 < b1;
-      wait_vm<NIW>();  // K is here, V may be on its way
-      if (RW > 1) barrier();
-      f32x16 s;
-#pragma unroll
-      for (int j = 0; j < 16; ++j) s[j] = 0.f;
-#pragma unroll
-      for (int t = 0; t < NQ; ++t) {
-        const uint4 kf = *(const uint4*)(sK[kg] + l32 * RB + (((2 * t + h) ^ swz<T, HDP>(l32)) * 16));
-        s = mma(kf, qf[t], s, T());
-      }
+    bool odd = false;
+    wait_vm<0>();  // (the first block waits for the query as well)
+    for (int b = t.b0; b < t.b1; ++b) {
+      const int kb = b * BN + wv * 32;
+      const bool more = b + 1 < t.b1;
+      if (b > t.b0) wait_vm<Ld::NI>();  // K is here, V may be on its way
+      f32x16 s[1] = {scores<T, HDP, NQ>(kl, qf)};
       wait_lds();
-      if (RW > 1) barrier();
-      if (more) issue(a.k, sK[kg], b + 1);
-
-      // masks: bit i of `see` is key kb + i for this lane's query
+      if (more) {
+        id = ld.ids(a, t, kb + BN);
+        ld.issue(a, t, a.k, kl, kb + BN, id, 0);
+      }
       const bool masked = kb + 32 > safe;
-      uint32_t see = 0xFFFFFFFFu;
-      if (masked) {
-        const int n = own - kb;
-        see = n >= 32 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << n) - 1u;
-        if (!g.causal && kb + 32 > x.len) {
-          const int j0 = kb - x.len;  // draft of bit 0
-          uint32_t bits;
-          const uint32_t* mw = a.mask + (size_t)row * a.mask_words;
-          if (j0 >= 0) {
-            const int wi = j0 >> 5, sh = j0 & 31;
-            const uint32_t lo = wi < a.mask_words ? mw[wi] : 0u, hi = wi + 1 < a.mask_words ? mw[wi + 1] : 0u;
-            bits = sh ? (lo >> sh) | (hi << (32 - sh)) : lo;
-          } else {
-            bits = (mw[0] << -j0) | ((1u << -j0) - 1u);
-          }
-          see &= bits;
-        }
-        const uint32_t half = see >> (4 * h);
-#pragma unroll
-        for (int j = 0; j < 16; ++j) s[j] = (half >> (8 * (j / 4) + j % 4)) & 1u ? s[j] : -INFINITY;
-      }
-
-      // running maximum and sum
-      float bm = s[0];
-#pragma unroll
-      for (int j = 1; j < 16; ++j) bm = fmaxf(bm, s[j]);
-      bm = max_x32(bm) * a.c2;
-      // rescale only when a row's maximum has grown by 2^8 or more: sums of
-      // probabilities up to 2^8 lose nothing
-      if (__any(bm > mx + 8.f)) {
-        const float mn = fmaxf(mx, bm);
-        const float f = mn == -INFINITY ? 1.f : ex2(mx - mn);
-        mx = mn;
-        l *= f;
-#pragma unroll
-        for (int i = 0; i < NDT; ++i)
-#pragma unroll
-          for (int j = 0; j < 16; ++j) o[i][j] *= f;
-      }
-      const float ref = mx == -INFINITY ? 0.f : mx;
-#pragma unroll
-      for (int j = 0; j < 16; ++j) s[j] = ex2(__builtin_fmaf(s[j], a.c2, -ref));
-      uint4 ph[2], pl[2];
-      if constexpr (HALF) {
-        // P as the sum of two bf16 values where the matrix cores wait for
-        // memory anyway (few rows), else rounded once
-#pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-          uint32_t hw[4], lw[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float p0 = s[8 * kk + 2 * i], p1 = s[8 * kk + 2 * i + 1];
-            hw[i] = bf2(p0, p1);
-            const float r0 = __uint_as_float(hw[i] << 16), r1 = __uint_as_float(hw[i] & 0xFFFF0000u);
-            if (RW == 1) {
-              lw[i] = bf2(p0 - r0, p1 - r1);
-              l += p0 + p1;
-            } else {
-              l += r0 + r1;
-            }
-          }
-          ph[kk] = make_uint4(hw[0], hw[1], hw[2], hw[3]);
-          if (RW == 1) pl[kk] = make_uint4(lw[0], lw[1], lw[2], lw[3]);
-        }
-      } else {
-#pragma unroll
-        for (int j = 0; j < 16; ++j) l += s[j];
-      }
-
-      if (more) wait_vm<NIW>();  // V is here, the next K may be on its way
+      if (masked) hide(s[0], seen_bits(a, t, kb, own, row));
+      soften<NDT, 1>(s, a.c2, mx, l, o);
+      Probs p;
+      if constexpr (sizeof(T) == 2) round_probs<true>(s[0], p);
+      if (more) wait_vm<Ld::NI>();  // V is here, the next K may be on its way
       else wait_vm<0>();
-      if (RW > 1) barrier();
-      const unsigned char* vt = sV[kg];
-      // A masked key's V may hold anything, and 0 x inf is not 0: such a
-      // block is added key by key.
-      bool odd = false;
       if (masked) {
-#pragma unroll
-        for (int i = 0; i < NI; ++i) {
-          const uint4 c4 = *(const uint4*)(vt + i * 1024 + lane * 16);
-          const uint32_t wd[4] = {c4.x, c4.y, c4.z, c4.w};
-#pragma unroll
-          for (int t = 0; t < 4; ++t) {
-            if (HALF) odd |= (wd[t] & 0x7F80u) == 0x7F80u || (wd[t] & 0x7F800000u) == 0x7F800000u;
-            else odd |= (wd[t] & 0x7F800000u) == 0x7F800000u;
-          }
-        }
-        odd = __any(odd);
+        odd |= clean_values<T, HDP, 1>(vl, 0);
+        wait_lds();
       }
-      if (odd) {
-        for (int kk = 0; kk < 32; ++kk) {
-          const int jj = (kk >> 3) * 4 + (kk & 3);
-          float p = s[0];
-#pragma unroll
-          for (int j = 1; j < 16; ++j) p = jj == j ? s[j] : p;
-          p = __shfl(p, l32 + 32 * ((kk >> 2) & 1));
-          const bool seen = (see >> kk) & 1u;
-#pragma unroll
-          for (int dt = 0; dt < NDT; ++dt)
-#pragma unroll
-            for (int j = 0; j < 16; ++j) {
-              const int d = 32 * dt + 8 * (j / 4) + 4 * h + j % 4;
-              const int ch = (d * ESZ / 16) ^ swz<T, HDP>(kk);
-              const unsigned char* vp = vt + kk * RB + ch * 16 + (d * ESZ) % 16;
-              const float v = HALF ? __uint_as_float((uint32_t) * (const uint16_t*)vp << 16) : *(const float*)vp;
-              if (seen) o[dt][j] = __builtin_fmaf(p, v, o[dt][j]);
-            }
-        }
-      } else if constexpr (HALF) {
-#pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-          // 16 lanes read four keys of 16 head-dim columns, transposed
-          const int il = lane & 15, key = 16 * kk + 4 * h + (il >> 2);
-#pragma unroll
-          for (int dt = 0; dt < NDT; ++dt) {
-            const int ch = 4 * dt + 2 * ((lane >> 4) & 1) + ((il & 3) >> 1);
-            auto tr = [&](int k0) {
-              const unsigned char* p = vt + k0 * RB + ((ch ^ swz<T, HDP>(k0)) * 16) + 8 * (il & 1);
-              return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p);
-            };
-            const s16x4 v0 = tr(key), v1 = tr(key + 8);
-            const uint2 u0 = __builtin_bit_cast(uint2, v0), u1 = __builtin_bit_cast(uint2, v1);
-            const uint4 vf = make_uint4(u0.x, u0.y, u1.x, u1.y);
-            o[dt] = mma(vf, ph[kk], o[dt], T());
-            if (RW == 1) o[dt] = mma(vf, pl[kk], o[dt], T());
-          }
-        }
-      } else {
-#pragma unroll
-        for (int j = 0; j < 16; ++j) {
-          const int key = 8 * (j / 4) + 4 * h + j % 4;
-#pragma unroll
-          for (int dt = 0; dt < NDT; ++dt) {
-            const int d = 32 * dt + l32;
-            const float v = *(const float*)(vt + key * RB + (((d / 4) ^ swz<T, HDP>(key)) * 16) + (d % 4) * 4);
-            o[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[j], o[dt], 0, 0, 0);
-          }
-        }
-      }
+      add_values<T, HDP, true>(vl, s[0], p, o);
       wait_lds();
-      if (RW > 1) barrier();
-      if (more) issue(a.v, sV[kg], b + 1);
+      if (more) ld.issue(a, t, a.v, vl, kb + BN, id, 0);
     }
     l = sum_x32(l);
-
-    const bool whole = b0 == 0 && b1 == nb;
-    const long long slot = 2ll * w + (b0 == 0 ? 1 : 0);
-    if (!whole && b0 == 0) {
-      const long long last = (u + nb - 1) / quota;  // the run that holds the tile's last block
-      desc = make_int4((int)(last - w) + 1, x.row0, head, rt);
-    }
-    float* po = a.part + slot * BM * HDP;
-    float* pm = a.part + 2ll * a.wgs * BM * HDP + slot * BM * 2;
-    // four results of one row: to the output, or the partial
-    auto put = [&](int lm, int d, float inv, const float (&v)[4]) {
-      if (whole) {
-        const int mm = rt * BM + lm;
-        if (mm >= g.M || d >= hd) return;
-        const int tk = mm / g.group;
-        T* dst = (T*)a.out + (size_t)(x.row0 + tk) * (size_t)a.ldo +
-                 (size_t)(head * g.group + (mm - tk * g.group)) * hd + d;
-        if constexpr (HALF) *(uint2*)dst = make_uint2(bf2(v[0] * inv, v[1] * inv), bf2(v[2] * inv, v[3] * inv));
-        else *(f32x4*)dst = f32x4{v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv};
-      } else {
-        *(f32x4*)(po + (size_t)lm * HDP + d) = f32x4{v[0], v[1], v[2], v[3]};
+    if (odd)
+      for (int b = t.b0; b < t.b1; ++b) {
+        const int kb = b * BN + wv * 32;
+        if (kb + 32 > safe) add_odd_values<T, HDP>(a, t, kb, seen_bits(a, t, kb, own, row), o);
       }
+    // the four waves' results, half of the columns at a time
+    if (h == 0) sM[wv][l32] = mx, sL[wv][l32] = l;
+    __syncthreads();
+    const float top = fmaxf(fmaxf(sM[0][l32], sM[1][l32]), fmaxf(sM[2][l32], sM[3][l32]));
+    const float f = mx == -INFINITY ? 0.f : ex2(mx - top);
+    float* so = (float*)sK;
+    float* po = a.part + (size_t)slot * BM * HDP;
+    float* pm = a.part + 2ll * a.wgs * BM * HDP + (size_t)slot * BM * 2;
+    constexpr int HC = HDP / 2;  // columns of a half
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf) {
+#pragma unroll
+      for (int dt = 0; dt < NDT / 2; ++dt)
+#pragma unroll
+        for (int j4 = 0; j4 < 4; ++j4) {
+          const f32x16& oo = o[hf * (NDT / 2) + dt];
+          const int c4 = 8 * dt + 2 * j4 + h;  // four columns
+          *(f32x4*)(so + ((wv * 32 + l32) * HC) + ((c4 ^ (l32 & 7)) * 4)) =
+              f32x4{oo[4 * j4] * f, oo[4 * j4 + 1] * f, oo[4 * j4 + 2] * f, oo[4 * j4 + 3] * f};
+        }
+      __syncthreads();
+      const int rows = t.M - t.rt * BM < 32 ? t.M - t.rt * BM : 32;
+      for (int i = tid; i < rows * (HC / 4); i += 256) {
+        const int lm = i / (HC / 4), c4 = i % (HC / 4);
+        float v[4] = {0.f, 0.f, 0.f, 0.f};
+        const float t4 = fmaxf(fmaxf(sM[0][lm], sM[1][lm]), fmaxf(sM[2][lm], sM[3][lm]));
+        float den = 0.f;
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) {
+          const f32x4 y = *(const f32x4*)(so + ((q4 * 32 + lm) * HC) + ((c4 ^ (lm & 7)) * 4));
+#pragma unroll
+          for (int u = 0; u < 4; ++u) v[u] += y[u];
+          den += sM[q4][lm] == -INFINITY ? 0.f : sL[q4][lm] * ex2(sM[q4][lm] - t4);
+        }
+        if (whole) {
+          put_out<T>(a, t, t.rt * BM + lm, hf * HC + c4 * 4, inverse(den), v);
+        } else {
+          *(f32x4*)(po + (size_t)lm * HDP + hf * HC + c4 * 4) = f32x4{v[0], v[1], v[2], v[3]};
+          if (hf == 0 && c4 == 0) pm[2 * lm] = t4, pm[2 * lm + 1] = den;
+        }
+      }
+      __syncthreads();
+    }
+  });
+}
+
+// Keys of a block of the many-row kernel: two tiles of 32 while two
+// workgroups' rings fit on a CU.
+template <typename T, int HDP>
+constexpr int many_keys() {
+  return HDP * (int)sizeof(T) <= 256 ? 64 : 32;
+}
+
+// Many rows to a sequence: tiles of 128 rows, 32 to a wave, bound by the
+// matrix cores. The four waves share a ring of two blocks in the LDS, the
+// next one on its way while one is worked on: one barrier to a block.
+template <typename T, int HDP>
+__global__ __launch_bounds__(256, 2) void k_tree_many(Args a) {
+  constexpr int BM = 128, BN = many_keys<T, HDP>(), NS = BN / 32;
+  constexpr int RB = HDP * (int)sizeof(T), NQ = RB / 32, NDT = HDP / 32;
+  typedef Loader<T, HDP, 4> Ld;
+  __shared__ __attribute__((aligned(1024))) unsigned char sK0[NS * 32 * RB], sK1[NS * 32 * RB];
+  __shared__ __attribute__((aligned(1024))) unsigned char sV0[NS * 32 * RB], sV1[NS * 32 * RB];
+  __shared__ Seg sg;
+  __shared__ int sOdd;
+  for_segments<BM, BN>(a, &sg, [&](const Tile& t, bool whole, int slot) {
+    const int tid = threadIdx.x, lane = tid & 63, wv = uni(tid >> 6), l32 = lane & 31, h = lane >> 5;
+    if (tid == 0) sOdd = 0;  // (a barrier of the first block follows)
+    Ld ld;
+    ld.set(a, t);
+    int2 id[NS];
+    auto look = [&](int b) {
+#pragma unroll
+      for (int n = 0; n < NS; ++n) id[n] = ld.ids(a, t, b * BN + 32 * n);
     };
-    if constexpr (RW == 1) {
-      // the four waves' results, half of the columns at a time
-      if (h == 0) sM[wv][l32] = mx, sL[wv][l32] = l;
-      wait_lds();
-      barrier();
-      float top = fmaxf(fmaxf(sM[0][l32], sM[1][l32]), fmaxf(sM[2][l32], sM[3][l32]));
-      const float f = mx == -INFINITY ? 0.f : ex2(mx - top);
-      float* so = (float*)sK;
-      constexpr int HC = HDP / 2;  // columns of a half
+    auto issue = [&](LB* kd, LB* vd, int b) {
 #pragma unroll
-      for (int hf = 0; hf < 2; ++hf) {
+      for (int n = 0; n < NS; ++n) ld.issue(a, t, a.k, kd + n * 32 * RB, b * BN + 32 * n, id[n], wv);
 #pragma unroll
-        for (int dt = 0; dt < NDT / 2; ++dt)
+      for (int n = 0; n < NS; ++n) ld.issue(a, t, a.v, vd + n * 32 * RB, b * BN + 32 * n, id[n], wv);
+    };
+    look(t.b0);
+    LB *k0 = (LB*)sK0, *k1 = (LB*)sK1, *v0 = (LB*)sV0, *v1 = (LB*)sV1;
+    issue(k0, v0, t.b0);
+    const int m = t.rt * BM + wv * 32 + l32, mc = m < t.M ? m : t.M - 1, tok = mc / t.group, row = t.row0 + tok;
+    u32x4 qf[NQ];
+    load_query<T, NQ>(a, t, mc, qf);
+    const int own = t.causal && t.len + tok + 1 < t.kend ? t.len + tok + 1 : t.kend;
+    // (of the tile's first row: the waves clean V together)
+    const int safe0 = t.causal ? t.len + t.rt * BM / t.group + 1 : t.len;
+    const int safe = safe0 < t.kend ? safe0 : t.kend;
+    f32x16 o[NDT];
 #pragma unroll
-          for (int j4 = 0; j4 < 4; ++j4) {
-            const f32x16& oo = o[hf * (NDT / 2) + dt];
-            const int c4 = 8 * dt + 2 * j4 + h;  // four columns
-            *(f32x4*)(so + ((wv * 32 + l32) * HC) + ((c4 ^ (l32 & 7)) * 4)) =
-                f32x4{oo[4 * j4] * f, oo[4 * j4 + 1] * f, oo[4 * j4 + 2] * f, oo[4 * j4 + 3] * f};
-          }
-        wait_lds();
-        barrier();
-        for (int i = tid; i < 32 * (HC / 4); i += 256) {
-          const int lm = i / (HC / 4), c4 = i % (HC / 4);
-          float v[4] = {0.f, 0.f, 0.f, 0.f};
-          const float t4 = fmaxf(fmaxf(sM[0][lm], sM[1][lm]), fmaxf(sM[2][lm], sM[3][lm]));
-          float den = 0.f;
+    for (int i = 0; i < NDT; ++i)
 #pragma unroll
-          for (int q4 = 0; q4 < 4; ++q4) {
-            const f32x4 y = *(const f32x4*)(so + ((q4 * 32 + lm) * HC) + ((c4 ^ (lm & 7)) * 4));
+      for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
+    float mx = -INFINITY, l = 0.f;
+    look(t.b0 + 1);
+    auto step = [&](const LB* kt, LB* vt, LB* kn, LB* vn, int b) {
+      wait_vm<0>();  // this wave's part of the block is here,
+      barrier();     // so are the others', and the other block is worked off
+      if (b + 1 < t.b1) issue(kn, vn, b + 1);
+      look(b + 2);
+      const int kb = b * BN;
+      f32x16 s[NS];
 #pragma unroll
-            for (int t = 0; t < 4; ++t) v[t] += y[t];
-            den += sM[q4][lm] == -INFINITY ? 0.f : sL[q4][lm] * ex2(sM[q4][lm] - t4);
-          }
-          put(lm, hf * HC + c4 * 4, den > 0.f || den != den ? 1.f / den : 0.f, v);
-          if (!whole && hf == 0 && c4 == 0) pm[2 * lm] = t4, pm[2 * lm + 1] = den;
+      for (int n = 0; n < NS; ++n) s[n] = scores<T, HDP, NQ>(kt + n * 32 * RB, qf);
+      if (kb + BN > safe) {
+#pragma unroll
+        for (int n = 0; n < NS; ++n) {
+          hide(s[n], seen_bits(a, t, kb + 32 * n, own, row));
+          if (clean_values<T, HDP, 4>(vt + n * 32 * RB, wv)) sOdd = 1;
         }
         wait_lds();
         barrier();
       }
-    } else {
-      const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+      soften<NDT, NS>(s, a.c2, mx, l, o);
+#pragma unroll
+      for (int n = 0; n < NS; ++n) {
+        Probs p;
+        if constexpr (sizeof(T) == 2) round_probs<false>(s[n], p);
+        add_values<T, HDP, false>(vt + n * 32 * RB, s[n], p, o);
+      }
+    };
+    for (int b = t.b0; b < t.b1; b += 2) {
+      step(k0, v0, k1, v1, b);
+      if (b + 1 < t.b1) step(k1, v1, k0, v0, b + 1);
+    }
+    l = sum_x32(l);
+    if (sOdd)  // (written before the last block's barrier)
+      for (int kb = t.b0 * BN; kb < t.b1 * BN; kb += 32)
+        if (kb + 32 > safe) add_odd_values<T, HDP>(a, t, kb, seen_bits(a, t, kb, own, row), o);
+    float* po = a.part + (size_t)slot * BM * HDP;
+    float* pm = a.part + 2ll * a.wgs * BM * HDP + (size_t)slot * BM * 2;
+    const float inv = inverse(l);
+    if (whole) {
 #pragma unroll
       for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
         for (int j4 = 0; j4 < 4; ++j4) {
           const float v[4] = {o[dt][4 * j4], o[dt][4 * j4 + 1], o[dt][4 * j4 + 2], o[dt][4 * j4 + 3]};
-          put(rw * 32 + l32, 32 * dt + 8 * j4 + 4 * h, inv, v);
+          put_out<T>(a, t, m, 32 * dt + 8 * j4 + 4 * h, inv, v);
         }
-      if (!whole && h == 0) pm[2 * (rw * 32 + l32)] = mx, pm[2 * (rw * 32 + l32) + 1] = l;
+    } else if (m < t.M) {
+#pragma unroll
+      for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+        for (int j4 = 0; j4 < 4; ++j4)
+          *(f32x4*)(po + (size_t)(wv * 32 + l32) * HDP + 32 * dt + 8 * j4 + 4 * h) =
+              f32x4{o[dt][4 * j4], o[dt][4 * j4 + 1], o[dt][4 * j4 + 2], o[dt][4 * j4 + 3]};
+      if (h == 0) pm[2 * (wv * 32 + l32)] = mx, pm[2 * (wv * 32 + l32) + 1] = l;
     }
-    u += b1 - b0;
-  }
-  if (tid == 0) a.desc[w] = desc;
+  });
 }
 
 // Tiles whose keys several workgroups shared out: their partials, in order. A
@@ -589,7 +808,7 @@ __global__ __launch_bounds__(256) void k_tree_join(Args a) {
         den += __shfl(ld, i);
         const float* po = a.part + (slot(i0 + i) * BM + lm) * HDP + lane * C;
 #pragma unroll
-        for (int t = 0; t < C; ++t) o[t] += fi == 0.f ? 0.f : fi * po[t];
+        for (int t = 0; t < C; ++t) o[t] = __builtin_fmaf(fi, po[t], o[t]);
       }
     }
     const float inv = den > 0.f || den != den ? 1.f / den : 0.f;
@@ -612,14 +831,22 @@ int tile_rows(const TreeAttnDesc& d) {
   const long long rows = (long long)d.r.n_rows * (d.nq / d.c.nkv);
   return rows > 64ll * d.r.n_ent ? 128 : 32;
 }
-int tree_wgs(const TreeAttnDesc& d) { return std::max(8, d.cus / 8 * 8); }
+// Workgroups, each with a run of blocks: as many as the CUs hold.
+int tree_wgs(const TreeAttnDesc& d) {
+  const int esz = d.c.dtype == DT_BF16 ? 2 : 4;
+  const int per = pad_hd(d.c.dtype, d.c.hd) * esz <= 256 ? 2 : 1;
+  return std::max(8, d.cus / 8 * 8) * per;
+}
 
-template <typename T, int HDP, int RW>
+template <typename T, int HDP>
 hipError_t run(const TreeAttnDesc& d, const Args& a, hipStream_t st) {
-  hipLaunchKernelGGL((k_tree<T, HDP, RW>), dim3(a.wgs), dim3(256), 0, st, a);
+  const int rows = tile_rows(d);
+  if (rows == 32) hipLaunchKernelGGL((k_tree_few<T, HDP>), dim3(a.wgs), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((k_tree_many<T, HDP>), dim3(a.wgs), dim3(256), 0, st, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((k_tree_join<T, HDP, 32 * RW>), dim3(a.wgs, 4 * RW), dim3(256), 0, st, a);
+  if (rows == 32) hipLaunchKernelGGL((k_tree_join<T, HDP, 32>), dim3(a.wgs, 4), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((k_tree_join<T, HDP, 128>), dim3(a.wgs, 16), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 
@@ -651,18 +878,12 @@ hipError_t launch_tree_attn(const TreeAttnDesc& d, hipStream_t st) {
   a.desc = (int4*)d.scratch;
   a.part = (float*)((char*)d.scratch + (size_t)a.wgs * 16);
   a.min_quota = 1;
-  const int hdp = pad_hd(d.c.dtype, d.c.hd), rows = tile_rows(d);
-  if (d.c.dtype == DT_BF16) {
-    if (rows == 32) {
-      return hdp == 64 ? run<uint16_t, 64, 1>(d, a, st) : hdp == 128 ? run<uint16_t, 128, 1>(d, a, st)
-                                                                     : run<uint16_t, 256, 1>(d, a, st);
-    }
-    return hdp == 64 ? run<uint16_t, 64, 4>(d, a, st) : hdp == 128 ? run<uint16_t, 128, 4>(d, a, st)
-                                                                   : run<uint16_t, 256, 4>(d, a, st);
-  }
+  const int hdp = pad_hd(d.c.dtype, d.c.hd);
+  if (d.c.dtype == DT_BF16)
+    return hdp == 64 ? run<uint16_t, 64>(d, a, st) : hdp == 128 ? run<uint16_t, 128>(d, a, st)
+                                                                : run<uint16_t, 256>(d, a, st);
   if (hdp > 128) return hipErrorInvalidValue;
-  if (rows == 32) return hdp == 64 ? run<float, 64, 1>(d, a, st) : run<float, 128, 1>(d, a, st);
-  return hdp == 64 ? run<float, 64, 4>(d, a, st) : run<float, 128, 4>(d, a, st);
+  return hdp == 64 ? run<float, 64>(d, a, st) : run<float, 128>(d, a, st);
 }
 
 }  // namespace vla
