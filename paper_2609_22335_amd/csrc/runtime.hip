@@ -3272,8 +3272,9 @@ static int paged_cache(const vla_pages* p, PagedCache* c) {
   while (lg < 8 && (1 << lg) != p->page_len) ++lg;
   if ((1 << lg) != p->page_len) return fail(VLA_EINVAL, "pages: page_len must be 16, 32, 64, 128 or 256");
   if (p->n_pages > (1 << 28) || p->n_seqs > (1 << 24) || p->layers > (1 << 16) || p->kv_heads > (1 << 12) ||
-      (int64_t)p->max_pages * p->page_len > (1 << 30))
-    return fail(VLA_EINVAL, "pages: sizes above 2^28 pages, 2^24 sequences or 2^30 slots of a sequence");
+      (int64_t)p->n_pages * p->kv_heads > (1 << 30) || (int64_t)p->max_pages * p->page_len > (1 << 30))
+    return fail(VLA_EINVAL, "pages: sizes above 2^28 pages, 2^30 pages of single heads, 2^24 sequences or 2^30 slots of "
+                            "a sequence");
   if (!p->k || !p->v || !p->table || !p->lens || !p->held || !p->refs || !p->status)
     return fail(VLA_EINVAL, "pages: NULL array");
   if (!aligned16(p->k) || !aligned16(p->v)) return fail(VLA_EINVAL, "pages: k and v must be 16-byte aligned");

@@ -61,6 +61,14 @@ struct Args {
   int min_quota;
 };
 
+// The kernel's arguments, loaded anew: what a rare or late part of a kernel
+// reads need not stand in scalar registers throughout its loop.
+__device__ __forceinline__ const Args& fresh() {
+  auto p = (const __attribute__((address_space(4))) Args*)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return *(const Args*)p;
+}
+
 // Tiles of an entry: BM rows by blocks of BN keys.
 template <int BM, int BN>
 struct Geo {
@@ -108,7 +116,8 @@ struct Seg {
 // the run's end, u_end), or with u < 0 the length of a run. One wave; lanes
 // hold 64 entries at a time.
 template <int BM, int BN>
-__device__ __forceinline__ void deal(const Args& a, Seg* sg, long long u, long long u_end) {
+__device__ __forceinline__ void deal(Seg* sg, long long u, long long u_end) {
+  const Args& a = fresh();
   const int lane = threadIdx.x & 63;
   auto lane_of = [](long long v, int i) {
     const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)v, i);
@@ -219,7 +228,8 @@ struct Tile {
   bool causal;
 };
 template <int BM, int BN>
-__device__ __forceinline__ Tile tile_of(const Args& a, const Seg& g) {
+__device__ __forceinline__ Tile tile_of(const Seg& g) {
+  const Args& a = fresh();
   Tile t;
   t.seq = uni(g.seq);
   t.row0 = uni(g.row0);
@@ -239,66 +249,77 @@ __device__ __forceinline__ Tile tile_of(const Args& a, const Seg& g) {
   return t;
 }
 
+// Where 16 slots lie: their first row in the cache's bytes from the layer's
+// base, and the bytes from there on that may be read (to the page's end, the
+// last key at most; 0 without a page).
+struct Place {
+  uint32_t lo, hi, bytes;
+};
+
 // Loads of 32 keys' K or V into the LDS, by the part `part` of PARTS waves.
-// They reach at most one page's part of one head, from its base: slots behind
-// the last key and chunks behind the head dim lie out of the resource's range
-// and become zeros. Pages are scalar loads (ids), given by the caller.
+// A buffer resource spans what is left of one page of one head: slots behind
+// the last key and chunks behind the head dim lie out of its range and become
+// zeros.
 template <typename T, int HDP, int PARTS>
 struct Loader {
   static constexpr int RB = HDP * (int)sizeof(T), CPR = RB / 16, RPI = 1024 / RB, NI = 32 / RPI;
   int lrow, lchunk, hb;  // the lane's row and chunk of a load; bytes of a row in memory
-  size_t pbytes;         // a page's part of one KV head
-  uint32_t hoff;         // (the head's part, in pages)
+  uint32_t pbytes;       // a page's part of one KV head
   const __attribute__((address_space(4))) int32_t* table;
+  int page, page_lg, n_pages, nkv, head, kend;
 
-  __device__ __forceinline__ void set(const Args& a, const Tile& t) {
+  __device__ __forceinline__ void set(const Tile& t) {
+    const Args& a = fresh();
     const int lane = threadIdx.x & 63;
     lrow = lane / CPR;
     lchunk = (lane % CPR) ^ swz(lrow);
     hb = a.c.hd * (int)sizeof(T);
-    pbytes = (size_t)a.c.page * hb;
-    hoff = t.head;
+    pbytes = (uint32_t)(a.c.page * hb);
     table = (const __attribute__((address_space(4))) int32_t*)(a.c.table + (size_t)t.seq * a.c.max_pages);
+    page = a.c.page, page_lg = a.c.page_lg, n_pages = a.c.n_pages, nkv = a.c.nkv, head = t.head, kend = t.kend;
   }
-  // pages of slots kb and kb + 16 (the two halves may lie in different ones)
-  __device__ __forceinline__ int2 ids(const Args& a, const Tile& t, int kb) const {
-    const int p0 = kb < t.kend ? table[kb >> a.c.page_lg] : -1;
-    const int p1 = kb + 16 < t.kend ? table[(kb + 16) >> a.c.page_lg] : -1;
-    return make_int2(p0, p1);
+  __device__ __forceinline__ Place place(int s0) const {
+    const int left = kend - s0;
+    const int id = left > 0 ? table[s0 >> page_lg] : -1;
+    const bool ok = (unsigned)id < (unsigned)n_pages;
+    const int at = s0 & (page - 1), room = page - at;
+    const unsigned long long off =
+        (unsigned long long)(uint32_t)((ok ? id : 0) * nkv + head) * pbytes + (uint32_t)(at * hb);
+    return Place{(uint32_t)off, (uint32_t)(off >> 32), ok ? (uint32_t)((left < room ? left : room) * hb) : 0u};
   }
-  __device__ __forceinline__ void issue(const Args& a, const Tile& t, const char* src, LB* dst, int kb,
-                                        int2 id, int part) const {
+  // the places of slots kb and kb + 16 (which may lie in different pages)
+  __device__ __forceinline__ void look(int kb, Place (&p)[2]) const {
+    p[0] = place(kb);
+    p[1] = place(kb + 16);
+  }
+  __device__ __forceinline__ void issue(const char* src, LB* dst, const Place (&p)[2], int part) const {
 #pragma unroll
     for (int hh = 0; hh < 2; ++hh) {
-      const int s0 = kb + 16 * hh, pid = hh ? id.y : id.x;
-      const bool ok = (unsigned)pid < (unsigned)a.c.n_pages;
-      const int at = s0 & (a.c.page - 1);
-      int have = t.kend - (s0 - at);  // keys from the page's first slot on
-      have = !ok || have < 0 ? 0 : have > a.c.page ? a.c.page : have;
       const Rsrc rs = __builtin_amdgcn_make_buffer_rsrc(
-          const_cast<char*>(src) + ((size_t)(ok ? pid : 0) * a.c.nkv + hoff) * pbytes, (short)0, have * hb,
+          const_cast<char*>(src) + (((unsigned long long)p[hh].hi << 32) | p[hh].lo), (short)0, (int)p[hh].bytes,
           0x00020000);
-      constexpr int PER = NI / 2;  // loads of a half
+      constexpr int PER = NI / 2;  // loads of a half, dealt out to the parts
 #pragma unroll
-      for (int i = 0; i < PER; ++i) {
-        const int idx = hh * PER + i;
-        if (PARTS > 1 && (NI >= PARTS ? idx % PARTS != part : idx != part)) continue;
-        const int r0 = idx * RPI;
+      for (int i = 0; i < PER; i += PER >= PARTS ? PARTS : 1) {
+        // (with fewer loads than parts, the halves go to different parts)
+        if (PER < PARTS && hh * PER + i != part) continue;
+        const int in = PER >= PARTS ? i + part : i;  // the load's place in its half
+        const int r0 = in * RPI, idx = hh * PER + in;
         const int ch = lchunk ^ swz(r0);
-        uint32_t off = (uint32_t)((at + (r0 & 15) + lrow) * hb + ch * 16);
+        uint32_t off = (uint32_t)((r0 + lrow) * hb + ch * 16);
         if (HDP * (int)sizeof(T) != hb && ch * 16 >= hb) off = OOB;
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (LDS_AS void*)(dst + idx * 1024), 16,
-                                                 off, 0, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (LDS_AS void*)(dst + idx * 1024), 16, off, 0, 0, 0);
       }
     }
   }
 };
 
 // Bit i: this lane's query sees slot kb + i (kb + 32 may pass the last key).
-__device__ __forceinline__ uint32_t seen_bits(const Args& a, const Tile& t, int kb, int own, int row) {
+__device__ __forceinline__ uint32_t seen_bits(const Tile& t, int kb, int own, int row) {
   const int n = own - kb;
   uint32_t see = n >= 32 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << n) - 1u;
   if (!t.causal && kb + 32 > t.len) {
+    const Args& a = fresh();
     const int j0 = kb - t.len;  // draft of bit 0
     uint32_t bits;
     const uint32_t* mw = a.mask + (size_t)row * a.mask_words;
@@ -314,22 +335,35 @@ __device__ __forceinline__ uint32_t seen_bits(const Args& a, const Tile& t, int 
   return see;
 }
 
-// S^T of 32 keys (rows) and the lane's query.
-template <typename T, int HDP, int NQ>
-__device__ __forceinline__ f32x16 scores(const LB* kt, const u32x4 (&qf)[NQ]) {
-  constexpr int RB = HDP * (int)sizeof(T);
+// S^T of NS x 32 keys (rows) and the lane's query. Fragments are read a set of
+// four ahead of the products that use them: the compiler would wait for each
+// read in turn.
+template <typename T, int HDP, int NS, int NQ>
+__device__ __forceinline__ void scores(const LB* kt, const u32x4 (&qf)[NQ], f32x16 (&s)[NS]) {
+  constexpr int RB = HDP * (int)sizeof(T), SETS = NS * NQ / 4;
   const int l32 = threadIdx.x & 31, h = (threadIdx.x >> 5) & 1;
   const LB* base = kt + l32 * RB;
   const int x = (h ^ swz(l32)) * 16;
-  f32x16 s;
+  u32x4 kf[2][4];
+  auto read = [&](int set) {
 #pragma unroll
-  for (int j = 0; j < 16; ++j) s[j] = 0.f;
+    for (int i = 0; i < 4; ++i)
+      kf[set & 1][i] = *(const LDS_AS u32x4*)(base + (x ^ (i * 32)) + (set % (NQ / 4)) * 128 +
+                                             set / (NQ / 4) * 32 * RB);
+  };
 #pragma unroll
-  for (int t = 0; t < NQ; ++t) {
-    const u32x4 kf = *(const LDS_AS u32x4*)(base + (x ^ ((t & 3) * 32)) + (t >> 2) * 128);
-    s = mma(kf, qf[t], s, T());
+  for (int n = 0; n < NS; ++n)
+#pragma unroll
+    for (int j = 0; j < 16; ++j) s[n][j] = 0.f;
+  read(0);
+#pragma unroll
+  for (int set = 0; set < SETS; ++set) {
+    if (set + 1 < SETS) read(set + 1);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      s[set / (NQ / 4)] = mma(kf[set & 1][i], qf[set % (NQ / 4) * 4 + i], s[set / (NQ / 4)], T());
   }
-  return s;
 }
 
 // Probabilities as operands of the second product: in bf16 rounded once, or
@@ -354,44 +388,72 @@ __device__ __forceinline__ void round_probs(const f32x16& s, Probs& p) {
   }
 }
 
-// O^T += V^T P^T over 32 keys.
-template <typename T, int HDP, bool TWO>
-__device__ __forceinline__ void add_values(const LB* vt, const f32x16& s, const Probs& p,
-                                           f32x16 (&o)[HDP / 32]) {
-  constexpr int RB = HDP * (int)sizeof(T), NDT = HDP / 32;
-  const int lane = threadIdx.x & 63, l32 = lane & 31, h = lane >> 5;
-  if constexpr (sizeof(T) == 2) {
-    // 16 lanes read four keys of 16 head-dim columns, transposed: lane i gets
-    // column i, the operand's keys 4 h .. + 3 and 8 + 4 h .. + 3 of each 16
-    const int il = lane & 15;
-    const LB* base = vt + (4 * h + (il >> 2)) * RB + 8 * (il & 1);
-    const int x = ((2 * ((lane >> 4) & 1) + ((il & 3) >> 1)) ^ swz(4 * h + (il >> 2))) * 16;
-#pragma unroll
-    for (int kk = 0; kk < 2; ++kk)
+// O^T += V^T P^T over NS x 32 keys. The first set of V's fragments (16 keys,
+// every column) is read by first(), before the softmax; each further set
+// before the products of the one ahead of it.
+template <typename T, int HDP, int NS, bool TWO>
+struct Values {
+  static constexpr int RB = HDP * (int)sizeof(T), NDT = HDP / 32;
+  u32x4 vf[2][sizeof(T) == 2 ? NDT : 1];
+  const LB* base;
+  int x;
+
+  __device__ __forceinline__ void read(int set) {
+    if constexpr (sizeof(T) == 2) {
+      // 16 lanes read four keys of 16 head-dim columns, transposed: lane i
+      // gets column i, the operand's keys 4 h .. + 3 and 8 + 4 h .. + 3
 #pragma unroll
       for (int dt = 0; dt < NDT; ++dt) {
         auto tr = [&](int k0) {
           const LB* q = base + (x ^ ((dt & 1) * 64)) + (dt >> 1) * 128 + k0 * RB;
           return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)q));
         };
-        const u32x2 u0 = tr(16 * kk), u1 = tr(16 * kk + 8);
-        const u32x4 vf = {u0.x, u0.y, u1.x, u1.y};
-        o[dt] = mma(vf, p.hi[kk], o[dt], T());
-        if (TWO) o[dt] = mma(vf, p.lo[kk], o[dt], T());
-      }
-  } else {
-#pragma unroll
-    for (int j = 0; j < 16; ++j) {
-      const int k0 = 8 * (j / 4) + j % 4, key = k0 + 4 * h;
-#pragma unroll
-      for (int dt = 0; dt < NDT; ++dt) {
-        const int d = 32 * dt + l32;
-        const float v = *(const LDS_AS float*)(vt + key * RB + (((d / 4) ^ swz(key)) * 16) + (d % 4) * 4);
-        o[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[j], o[dt], 0, 0, 0);
+        const u32x2 u0 = tr(16 * set), u1 = tr(16 * set + 8);
+        vf[set & 1][dt] = u32x4{u0.x, u0.y, u1.x, u1.y};
       }
     }
   }
-}
+  __device__ __forceinline__ void first(const LB* vt) {
+    const int lane = threadIdx.x & 63, h = lane >> 5, il = lane & 15;
+    if constexpr (sizeof(T) == 2) {
+      base = vt + (4 * h + (il >> 2)) * RB + 8 * (il & 1);
+      x = ((2 * ((lane >> 4) & 1) + ((il & 3) >> 1)) ^ swz(4 * h + (il >> 2))) * 16;
+    } else {
+      base = vt;
+      x = 0;
+    }
+    read(0);
+  }
+  __device__ __forceinline__ void add(const f32x16 (&s)[NS], const Probs (&p)[NS], f32x16 (&o)[NDT]) {
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int set = 0; set < 2 * NS; ++set) {
+        if (set + 1 < 2 * NS) read(set + 1);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int dt = 0; dt < NDT; ++dt) o[dt] = mma(vf[set & 1][dt], p[set >> 1].hi[set & 1], o[dt], T());
+        if (TWO) {
+#pragma unroll
+          for (int dt = 0; dt < NDT; ++dt) o[dt] = mma(vf[set & 1][dt], p[set >> 1].lo[set & 1], o[dt], T());
+        }
+      }
+    } else {
+      const int lane = threadIdx.x & 63, l32 = lane & 31, h = lane >> 5;
+#pragma unroll
+      for (int n = 0; n < NS; ++n)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          const int key = 8 * (j / 4) + j % 4 + 4 * h;
+#pragma unroll
+          for (int dt = 0; dt < NDT; ++dt) {
+            const int d = 32 * dt + l32;
+            const float v = *(const LDS_AS float*)(base + (32 * n + key) * RB + (((d / 4) ^ swz(key)) * 16) + (d % 4) * 4);
+            o[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[n][j], o[dt], 0, 0, 0);
+          }
+        }
+    }
+  }
+};
 
 // A masked key's V may hold anything, and 0 x inf is not 0. In blocks of which
 // a row may be masked, values that are not finite are replaced by zeros before
@@ -422,8 +484,8 @@ __device__ __forceinline__ bool clean_values(LB* vt, int part) {
 }
 // Slots kb .. kb + 31, of which the lane's query sees `see`.
 template <typename T, int HDP>
-__device__ __forceinline__ void add_odd_values(const Args& a, const Tile& t, int kb, uint32_t see,
-                                               f32x16 (&o)[HDP / 32]) {
+__device__ __forceinline__ void add_odd_values(const Tile& t, int kb, uint32_t see, f32x16 (&o)[HDP / 32]) {
+  const Args& a = fresh();
   const int h = (threadIdx.x >> 5) & 1, hd = a.c.hd;
 #pragma unroll 1
   for (int kk = 0; kk < 32; ++kk) {
@@ -493,7 +555,8 @@ __device__ __forceinline__ void hide(f32x16& s, uint32_t see) {
 
 // The lane's query (row m of the tile's rows, clamped to the last).
 template <typename T, int NQ>
-__device__ __forceinline__ void load_query(const Args& a, const Tile& t, int mc, u32x4 (&qf)[NQ]) {
+__device__ __forceinline__ void load_query(const Tile& t, int mc, u32x4 (&qf)[NQ]) {
+  const Args& a = fresh();
   const int tok = mc / t.group, h = (threadIdx.x >> 5) & 1, hd = a.c.hd;
   const T* qp = (const T*)a.q + (size_t)(t.row0 + tok) * (size_t)a.ldq +
                 (size_t)(t.head * t.group + (mc - tok * t.group)) * hd;
@@ -519,20 +582,20 @@ __device__ __forceinline__ float inverse(float l) { return l > 0.f || l != l ? 1
 // The workgroup's run of blocks: calls f(tile, whole, slot) for each segment;
 // what other workgroups hold of the last tile is written down for the join.
 template <int BM, int BN, typename F>
-__device__ __forceinline__ void for_segments(const Args& a, Seg* sg, F&& f) {
+__device__ __forceinline__ void for_segments(int wgs, Seg* sg, F&& f) {
   const int wv = uni(threadIdx.x >> 6);
   // consecutive runs on one XCD (workgroups go round the eight)
-  const int w = (int)(blockIdx.x & 7) * (a.wgs >> 3) + (int)(blockIdx.x >> 3);
-  if (wv == 0) deal<BM, BN>(a, sg, -1, 0);
+  const int w = (int)(blockIdx.x & 7) * (wgs >> 3) + (int)(blockIdx.x >> 3);
+  if (wv == 0) deal<BM, BN>(sg, -1, 0);
   __syncthreads();
   const long long quota = uni64(sg->quota), total = uni64(sg->total);
   long long u = w * quota;
   const long long u_end = u + quota < total ? u + quota : total;
   int4 desc = make_int4(0, 0, 0, 0);
   while (u < u_end) {
-    if (wv == 0) deal<BM, BN>(a, sg, u, u_end);
+    if (wv == 0) deal<BM, BN>(sg, u, u_end);
     __syncthreads();
-    const Tile t = tile_of<BM, BN>(a, *sg);
+    const Tile t = tile_of<BM, BN>(*sg);
     const bool whole = t.b0 == 0 && t.b1 == t.nb;
     if (!whole && t.b0 == 0) desc = make_int4((int)((u + t.nb - 1) / quota - w) + 1, t.row0, t.head, t.rt);
     f(t, whole, 2 * w + (t.b0 == 0 ? 1 : 0));
@@ -540,7 +603,13 @@ __device__ __forceinline__ void for_segments(const Args& a, Seg* sg, F&& f) {
     wait_vm<0>();  // no store of this tile in the next one's counts
     __syncthreads();
   }
-  if (threadIdx.x == 0) a.desc[w] = desc;
+  if (threadIdx.x == 0) fresh().desc[w] = desc;
+}
+
+// Waves per SIMD (workgroups per CU) that a kernel's registers are to leave room for.
+template <typename T, int HDP>
+constexpr int many_waves() {
+  return HDP * (int)sizeof(T) <= 256 ? 2 : 1;
 }
 
 // Few rows to a sequence: tiles of 32 rows, bound by the cache's bandwidth.
@@ -549,7 +618,7 @@ __device__ __forceinline__ void for_segments(const Args& a, Seg* sg, F&& f) {
 // P V, the next V during the next scores. The four waves' results are merged
 // at the end.
 template <typename T, int HDP>
-__global__ __launch_bounds__(256, 1) void k_tree_few(Args a) {
+__global__ __launch_bounds__(256, (many_waves<T, HDP>())) void k_tree_few(Args a) {
   constexpr int BM = 32, BN = 128;
   constexpr int RB = HDP * (int)sizeof(T), NQ = RB / 32, NDT = HDP / 32;
   typedef Loader<T, HDP, 1> Ld;
@@ -558,18 +627,19 @@ __global__ __launch_bounds__(256, 1) void k_tree_few(Args a) {
   __shared__ __attribute__((aligned(1024))) unsigned char sV[4][32 * RB];
   __shared__ float sM[4][32], sL[4][32];
   __shared__ Seg sg;
-  for_segments<BM, BN>(a, &sg, [&](const Tile& t, bool whole, int slot) {
+  for_segments<BM, BN>(a.wgs, &sg, [&](const Tile& t, bool whole, int slot) {
     const int tid = threadIdx.x, lane = tid & 63, wv = uni(tid >> 6), l32 = lane & 31, h = lane >> 5;
     Ld ld;
-    ld.set(a, t);
+    ld.set(t);
     const int kb0 = t.b0 * BN + wv * 32;
     LB *kl = (LB*)sK[wv], *vl = (LB*)sV[wv];
-    int2 id = ld.ids(a, t, kb0);
-    ld.issue(a, t, a.k, kl, kb0, id, 0);
-    ld.issue(a, t, a.v, vl, kb0, id, 0);
+    Place at[2];
+    ld.look(kb0, at);
+    ld.issue(a.k, kl, at, 0);
+    ld.issue(a.v, vl, at, 0);
     const int m = t.rt * BM + l32, mc = m < t.M ? m : t.M - 1, tok = mc / t.group, row = t.row0 + tok;
     u32x4 qf[NQ];
-    load_query<T, NQ>(a, t, mc, qf);
+    load_query<T, NQ>(t, mc, qf);
     // slots below `own` are seen; the tile needs no mask below `safe`
     const int own = t.causal && t.len + tok + 1 < t.kend ? t.len + tok + 1 : t.kend;
     const int safe0 = t.causal ? t.len + t.rt * BM / t.group + 1 : t.len;
@@ -586,32 +656,35 @@ __global__ __launch_bounds__(256, 1) void k_tree_few(Args a) {
       const int kb = b * BN + wv * 32;
       const bool more = b + 1 < t.b1;
       if (b > t.b0) wait_vm<Ld::NI>();  // K is here, V may be on its way
-      f32x16 s[1] = {scores<T, HDP, NQ>(kl, qf)};
+      f32x16 s[1];
+      scores<T, HDP, 1, NQ>(kl, qf, s);
       wait_lds();
       if (more) {
-        id = ld.ids(a, t, kb + BN);
-        ld.issue(a, t, a.k, kl, kb + BN, id, 0);
+        ld.look(kb + BN, at);
+        ld.issue(a.k, kl, at, 0);
       }
       const bool masked = kb + 32 > safe;
-      if (masked) hide(s[0], seen_bits(a, t, kb, own, row));
+      if (masked) hide(s[0], seen_bits(t, kb, own, row));
       soften<NDT, 1>(s, a.c2, mx, l, o);
-      Probs p;
-      if constexpr (sizeof(T) == 2) round_probs<true>(s[0], p);
+      Probs p[1];
+      if constexpr (sizeof(T) == 2) round_probs<true>(s[0], p[0]);
       if (more) wait_vm<Ld::NI>();  // V is here, the next K may be on its way
       else wait_vm<0>();
       if (masked) {
         odd |= clean_values<T, HDP, 1>(vl, 0);
         wait_lds();
       }
-      add_values<T, HDP, true>(vl, s[0], p, o);
+      Values<T, HDP, 1, true> vv;
+      vv.first(vl);
+      vv.add(s, p, o);
       wait_lds();
-      if (more) ld.issue(a, t, a.v, vl, kb + BN, id, 0);
+      if (more) ld.issue(a.v, vl, at, 0);
     }
     l = sum_x32(l);
     if (odd)
       for (int b = t.b0; b < t.b1; ++b) {
         const int kb = b * BN + wv * 32;
-        if (kb + 32 > safe) add_odd_values<T, HDP>(a, t, kb, seen_bits(a, t, kb, own, row), o);
+        if (kb + 32 > safe) add_odd_values<T, HDP>(t, kb, seen_bits(t, kb, own, row), o);
       }
     // the four waves' results, half of the columns at a time
     if (h == 0) sM[wv][l32] = mx, sL[wv][l32] = l;
@@ -619,8 +692,9 @@ __global__ __launch_bounds__(256, 1) void k_tree_few(Args a) {
     const float top = fmaxf(fmaxf(sM[0][l32], sM[1][l32]), fmaxf(sM[2][l32], sM[3][l32]));
     const float f = mx == -INFINITY ? 0.f : ex2(mx - top);
     float* so = (float*)sK;
-    float* po = a.part + (size_t)slot * BM * HDP;
-    float* pm = a.part + 2ll * a.wgs * BM * HDP + (size_t)slot * BM * 2;
+    const Args& z = fresh();
+    float* po = z.part + (size_t)slot * BM * HDP;
+    float* pm = z.part + 2ll * z.wgs * BM * HDP + (size_t)slot * BM * 2;
     constexpr int HC = HDP / 2;  // columns of a half
 #pragma unroll
     for (int hf = 0; hf < 2; ++hf) {
@@ -648,7 +722,7 @@ __global__ __launch_bounds__(256, 1) void k_tree_few(Args a) {
           den += sM[q4][lm] == -INFINITY ? 0.f : sL[q4][lm] * ex2(sM[q4][lm] - t4);
         }
         if (whole) {
-          put_out<T>(a, t, t.rt * BM + lm, hf * HC + c4 * 4, inverse(den), v);
+          put_out<T>(z, t, t.rt * BM + lm, hf * HC + c4 * 4, inverse(den), v);
         } else {
           *(f32x4*)(po + (size_t)lm * HDP + hf * HC + c4 * 4) = f32x4{v[0], v[1], v[2], v[3]};
           if (hf == 0 && c4 == 0) pm[2 * lm] = t4, pm[2 * lm + 1] = den;
@@ -670,7 +744,7 @@ constexpr int many_keys() {
 // matrix cores. The four waves share a ring of two blocks in the LDS, the
 // next one on its way while one is worked on: one barrier to a block.
 template <typename T, int HDP>
-__global__ __launch_bounds__(256, 2) void k_tree_many(Args a) {
+__global__ __launch_bounds__(256, (many_waves<T, HDP>())) void k_tree_many(Args a) {
   constexpr int BM = 128, BN = many_keys<T, HDP>(), NS = BN / 32;
   constexpr int RB = HDP * (int)sizeof(T), NQ = RB / 32, NDT = HDP / 32;
   typedef Loader<T, HDP, 4> Ld;
@@ -678,28 +752,28 @@ __global__ __launch_bounds__(256, 2) void k_tree_many(Args a) {
   __shared__ __attribute__((aligned(1024))) unsigned char sV0[NS * 32 * RB], sV1[NS * 32 * RB];
   __shared__ Seg sg;
   __shared__ int sOdd;
-  for_segments<BM, BN>(a, &sg, [&](const Tile& t, bool whole, int slot) {
+  for_segments<BM, BN>(a.wgs, &sg, [&](const Tile& t, bool whole, int slot) {
     const int tid = threadIdx.x, lane = tid & 63, wv = uni(tid >> 6), l32 = lane & 31, h = lane >> 5;
     if (tid == 0) sOdd = 0;  // (a barrier of the first block follows)
     Ld ld;
-    ld.set(a, t);
-    int2 id[NS];
+    ld.set(t);
+    Place at[NS][2];
     auto look = [&](int b) {
 #pragma unroll
-      for (int n = 0; n < NS; ++n) id[n] = ld.ids(a, t, b * BN + 32 * n);
+      for (int n = 0; n < NS; ++n) ld.look(b * BN + 32 * n, at[n]);
     };
-    auto issue = [&](LB* kd, LB* vd, int b) {
+    auto issue = [&](LB* kd, LB* vd) {
 #pragma unroll
-      for (int n = 0; n < NS; ++n) ld.issue(a, t, a.k, kd + n * 32 * RB, b * BN + 32 * n, id[n], wv);
+      for (int n = 0; n < NS; ++n) ld.issue(a.k, kd + n * 32 * RB, at[n], wv);
 #pragma unroll
-      for (int n = 0; n < NS; ++n) ld.issue(a, t, a.v, vd + n * 32 * RB, b * BN + 32 * n, id[n], wv);
+      for (int n = 0; n < NS; ++n) ld.issue(a.v, vd + n * 32 * RB, at[n], wv);
     };
     look(t.b0);
     LB *k0 = (LB*)sK0, *k1 = (LB*)sK1, *v0 = (LB*)sV0, *v1 = (LB*)sV1;
-    issue(k0, v0, t.b0);
+    issue(k0, v0);
     const int m = t.rt * BM + wv * 32 + l32, mc = m < t.M ? m : t.M - 1, tok = mc / t.group, row = t.row0 + tok;
     u32x4 qf[NQ];
-    load_query<T, NQ>(a, t, mc, qf);
+    load_query<T, NQ>(t, mc, qf);
     const int own = t.causal && t.len + tok + 1 < t.kend ? t.len + tok + 1 : t.kend;
     // (of the tile's first row: the waves clean V together)
     const int safe0 = t.causal ? t.len + t.rt * BM / t.group + 1 : t.len;
@@ -714,28 +788,29 @@ __global__ __launch_bounds__(256, 2) void k_tree_many(Args a) {
     auto step = [&](const LB* kt, LB* vt, LB* kn, LB* vn, int b) {
       wait_vm<0>();  // this wave's part of the block is here,
       barrier();     // so are the others', and the other block is worked off
-      if (b + 1 < t.b1) issue(kn, vn, b + 1);
+      if (b + 1 < t.b1) issue(kn, vn);
       look(b + 2);
       const int kb = b * BN;
       f32x16 s[NS];
-#pragma unroll
-      for (int n = 0; n < NS; ++n) s[n] = scores<T, HDP, NQ>(kt + n * 32 * RB, qf);
+      scores<T, HDP, NS, NQ>(kt, qf, s);
       if (kb + BN > safe) {
 #pragma unroll
         for (int n = 0; n < NS; ++n) {
-          hide(s[n], seen_bits(a, t, kb + 32 * n, own, row));
+          hide(s[n], seen_bits(t, kb + 32 * n, own, row));
           if (clean_values<T, HDP, 4>(vt + n * 32 * RB, wv)) sOdd = 1;
         }
         wait_lds();
         barrier();
       }
+      Values<T, HDP, NS, false> vv;
+      vv.first(vt);
       soften<NDT, NS>(s, a.c2, mx, l, o);
+      Probs p[NS];
+      if constexpr (sizeof(T) == 2) {
 #pragma unroll
-      for (int n = 0; n < NS; ++n) {
-        Probs p;
-        if constexpr (sizeof(T) == 2) round_probs<false>(s[n], p);
-        add_values<T, HDP, false>(vt + n * 32 * RB, s[n], p, o);
+        for (int n = 0; n < NS; ++n) round_probs<false>(s[n], p[n]);
       }
+      vv.add(s, p, o);
     };
     for (int b = t.b0; b < t.b1; b += 2) {
       step(k0, v0, k1, v1, b);
@@ -744,9 +819,10 @@ __global__ __launch_bounds__(256, 2) void k_tree_many(Args a) {
     l = sum_x32(l);
     if (sOdd)  // (written before the last block's barrier)
       for (int kb = t.b0 * BN; kb < t.b1 * BN; kb += 32)
-        if (kb + 32 > safe) add_odd_values<T, HDP>(a, t, kb, seen_bits(a, t, kb, own, row), o);
-    float* po = a.part + (size_t)slot * BM * HDP;
-    float* pm = a.part + 2ll * a.wgs * BM * HDP + (size_t)slot * BM * 2;
+        if (kb + 32 > safe) add_odd_values<T, HDP>(t, kb, seen_bits(t, kb, own, row), o);
+    const Args& z = fresh();
+    float* po = z.part + (size_t)slot * BM * HDP;
+    float* pm = z.part + 2ll * z.wgs * BM * HDP + (size_t)slot * BM * 2;
     const float inv = inverse(l);
     if (whole) {
 #pragma unroll
@@ -754,7 +830,7 @@ __global__ __launch_bounds__(256, 2) void k_tree_many(Args a) {
 #pragma unroll
         for (int j4 = 0; j4 < 4; ++j4) {
           const float v[4] = {o[dt][4 * j4], o[dt][4 * j4 + 1], o[dt][4 * j4 + 2], o[dt][4 * j4 + 3]};
-          put_out<T>(a, t, m, 32 * dt + 8 * j4 + 4 * h, inv, v);
+          put_out<T>(z, t, m, 32 * dt + 8 * j4 + 4 * h, inv, v);
         }
     } else if (m < t.M) {
 #pragma unroll
