@@ -76,21 +76,17 @@ struct Entry {
   int seq, row0, n, len, cap;
 };
 __device__ __forceinline__ Entry entry_of(const PagedCache& c, const PagedRows& r, int e) {
+  // (every load is issued at once: an entry without a sequence reads the first)
+  const int q = r.seqs ? r.seqs[e] : e;
+  const bool in = q >= 0 && q < c.n_seqs;
+  const int at = in ? q : 0;
+  const int a = r.start[e], b = r.start[e + 1], h = c.held[at], l = c.lens[at];
   Entry x;
-  const int a = r.start[e], b = r.start[e + 1];
+  x.seq = in ? q : -1;
   x.row0 = a < 0 ? 0 : a > r.n_rows ? r.n_rows : a;
   const int end = b > r.n_rows ? r.n_rows : b;
-  x.n = end > x.row0 ? end - x.row0 : 0;
-  x.seq = r.seqs ? r.seqs[e] : e;
-  if (x.seq < 0 || x.seq >= c.n_seqs) {
-    x.seq = -1;
-    x.n = x.len = x.cap = 0;
-    return x;
-  }
-  int h = c.held[x.seq];
-  h = h < 0 ? 0 : h > c.max_pages ? c.max_pages : h;
-  x.cap = h << c.page_lg;
-  const int l = c.lens[x.seq];
+  x.n = in && end > x.row0 ? end - x.row0 : 0;
+  x.cap = (h < 0 || !in ? 0 : h > c.max_pages ? c.max_pages : h) << c.page_lg;
   x.len = l < 0 ? 0 : l > x.cap ? x.cap : l;
   return x;
 }

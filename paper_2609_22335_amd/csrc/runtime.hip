@@ -3413,8 +3413,11 @@ static int tree_desc(const vla_pages* p, const vla_rows* rows, int32_t layer, in
   VLA_TRY(paged_cache(p, &d->c));
   VLA_TRY(paged_rows(rows, &d->r));
   VLA_TRY(paged_layer(d->c, layer, nq));
-  if ((int64_t)d->r.n_rows * (nq / d->c.nkv) > (1 << 30))
-    return fail(VLA_EUNSUPPORTED, "more than 2^30 query rows to a KV head");
+  // the blocks of one entry and KV head are counted in 31 bits
+  const int64_t group = nq / d->c.nkv, slots = (int64_t)d->c.max_pages * d->c.page;
+  if (d->r.n_rows * group > (1 << 29) || group * slots > (1 << 29) ||
+      (d->r.n_rows * group / 32 + 1) * (slots / 32 + 1) > ((int64_t)1 << 31) - 1)
+    return fail(VLA_EUNSUPPORTED, "more than 2^29 query rows or grouped slots, or 2^31 blocks of scores, to a KV head");
   d->layer = layer;
   d->nq = nq;
   return device_cus(&d->cus);

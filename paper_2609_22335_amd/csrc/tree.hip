@@ -8,6 +8,7 @@
 // lane, and the probabilities are, without leaving their registers, the right
 // operand of O^T += V^T P^T.
 #include <algorithm>
+#include <type_traits>
 
 #include "paged_dev.h"
 
@@ -56,9 +57,8 @@ struct Args {
   const char* k;  // the layer's K and V
   const char* v;
   float* part;   // [2 W][rows][hd], then [2 W][rows][2]
-  int4* desc;    // [W]
+  int4* desc;    // [W][2]: what the join reads
   int wgs;       // W
-  int min_quota;
 };
 
 // The kernel's arguments, loaded anew: what a rare or late part of a kernel
@@ -69,125 +69,214 @@ __device__ __forceinline__ const Args& fresh() {
   return *(const Args*)p;
 }
 
-// Tiles of an entry: BM rows by blocks of BN keys.
-template <int BM, int BN>
+// sum over i < n of floor((a i + b) / m), by Euclid's steps
+__device__ __forceinline__ uint32_t floor_sum(uint32_t n, uint32_t m, uint32_t a, uint32_t b) {
+  uint32_t sum = 0;
+  while (n > 0) {
+    if (a >= m) {
+      sum += (uint32_t)((unsigned long long)(n - 1) * n / 2) * (a / m);
+      a %= m;
+    }
+    if (b >= m) {
+      sum += n * (b / m);
+      b %= m;
+    }
+    const uint32_t y = a * n + b;
+    if (y < m) break;
+    n = y / m;
+    b = y % m;
+    const uint32_t t = m;
+    m = a;
+    a = t;
+  }
+  return sum;
+}
+
+// The tiles of an entry and one KV head: BM rows by units of `unit` keys. A
+// causal tile ends with its last row's own slot, so tile rt has
+// ceil((len + 1 + floor((BM (rt + 1) - 1) / group)) / unit) units, which is
+// floor((BM rt + BM - 1 + group (len + unit)) / (group unit)).
+template <int BM>
 struct Geo {
-  int tiles, nb_all;  // row tiles of a head; blocks of a tile with every key
-  int end, len, M, group;
-  bool causal;
-  __device__ __forceinline__ void set(const Args& a, const Entry& x) {
-    group = a.group;
+  int tiles, M, group, len, end, unit;
+  bool flat;  // every tile reads all keys
+  __device__ __forceinline__ void set(int group_, bool causal, const Entry& x, int unit_) {
+    group = group_;
+    unit = unit_;
     M = x.n * group;
     tiles = (M + BM - 1) / BM;
     len = x.len;
     const long long e = (long long)x.len + x.n;
     end = e < x.cap ? (int)e : x.cap;
-    causal = a.mask == nullptr;
-    nb_all = blocks(end);
+    flat = !causal || e > x.cap;  // (drafts without pages: no row sees them)
   }
-  // (a tile without keys has one block, which writes its zeros)
-  static __device__ __forceinline__ int blocks(int keys) { return keys > 0 ? (keys + BN - 1) / BN : 1; }
+  // (a tile without keys has one unit, which writes its zeros)
+  __device__ __forceinline__ int all() const { return end > 0 ? (end + unit - 1) / unit : 1; }
   __device__ __forceinline__ int tile_end(int rt) const {
-    if (!causal) return end;
+    if (flat) return end;
     const int last = (rt + 1) * BM < M ? (rt + 1) * BM - 1 : M - 1;
-    const int e = len + last / group + 1;
-    return e < end ? e : end;
+    return len + last / group + 1;
   }
-  __device__ __forceinline__ int nb(int rt) const { return causal ? blocks(tile_end(rt)) : nb_all; }
-  // blocks of one head's tiles
-  __device__ __forceinline__ int sum() const {
-    if (!causal || tiles == 0) return tiles * nb_all;
-    int s = 0;
-    for (int rt = 0; rt < tiles; ++rt) s += nb(rt);
-    return s;
+  __device__ __forceinline__ int units(int rt) const { return flat ? all() : (tile_end(rt) + unit - 1) / unit; }
+  // units of the tiles before rt (rt < tiles)
+  __device__ __forceinline__ int before(int rt) const {
+    if (flat) return rt * all();
+    return (int)floor_sum(rt, group * unit, BM, BM - 1 + group * (len + unit));
+  }
+  __device__ __forceinline__ int sum() const { return tiles == 0 ? 0 : before(tiles - 1) + units(tiles - 1); }
+  // the tile that holds unit u of the head's
+  __device__ __forceinline__ int find(int u) const {
+    if (flat) return u / all();
+    int lo = 0, hi = tiles - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) / 2;
+      if (before(mid) <= u) lo = mid;
+      else hi = mid - 1;
+    }
+    return lo;
   }
 };
 
-// A run of key blocks of one tile: what a workgroup does next. Worked out by
-// one wave, read by all.
-struct Seg {
-  int seq, row0, n, len, cap;  // the entry
-  int head, rt, b0, b1, nb;    // tile and its blocks [b0, b1) of nb
-  long long quota, total;
+// Inclusive sum over the wave's lanes, by shifts inside rows of 16 lanes and
+// broadcasts of their last ones (no LDS round trips).
+template <int CTRL, int ROWS>
+__device__ __forceinline__ void scan_step(int& v) {
+  v += __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false);
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ void scan_step(long long& v) {
+  const int lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CTRL, ROWS, 0xf, false);
+  const int hi = __builtin_amdgcn_update_dpp(0, (int)(v >> 32), CTRL, ROWS, 0xf, false);
+  v += (long long)(((unsigned long long)(uint32_t)hi << 32) | (uint32_t)lo);
+}
+template <typename I>
+__device__ __forceinline__ I wave_scan(I v) {
+  scan_step<0x111, 0xf>(v);  // row_shr 1, 2, 4, 8
+  scan_step<0x112, 0xf>(v);
+  scan_step<0x114, 0xf>(v);
+  scan_step<0x118, 0xf>(v);
+  scan_step<0x142, 0xa>(v);  // row_bcast 15 to rows 1 and 3
+  scan_step<0x143, 0xc>(v);  // row_bcast 31 to rows 2 and 3
+  return v;
+}
+__device__ __forceinline__ long long lane_of(long long v, int i) {
+  const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)v, i);
+  const uint32_t hi = __builtin_amdgcn_readlane((int)(v >> 32), i);
+  return (long long)(((unsigned long long)hi << 32) | lo);
+}
+
+// (64-bit divisions are long: most counts are short)
+__device__ __forceinline__ long long ceil_div(long long a, int b) {
+  return a >> 31 ? (a + b - 1) / b : (long long)(((uint32_t)a + (uint32_t)b - 1) / (uint32_t)b);
+}
+
+// What a wave knows of its workgroup's run and of the tile it works on: the
+// same in every lane.
+struct Tile {
+  int seq, row0, len, head, rt;
+  int b0, b1;         // blocks of the tile to work on
+  int M, group, kend;
+  int parts;          // with the first of several parts: how many, else 0
+  bool whole, causal;
+};
+struct Run {
+  long long u, u_end;  // this run's next and last unit
+  long long quota;     // units of a run
+  int per;             // blocks of a unit
 };
 
-// All entries' blocks stand in a row and are dealt out in equal runs, so that
-// uneven sequences load the chip evenly. Finds the run's segment at unit u (of
-// the run's end, u_end), or with u < 0 the length of a run. One wave; lanes
-// hold 64 entries at a time.
+// All entries' units stand in a row and are dealt out in equal runs, so that
+// uneven sequences load the chip evenly. A unit is a block of keys of a tile,
+// and a run may begin and end inside tiles: at most two of its tiles are
+// shared with other runs. Where there are few tiles (at most half as many as
+// workgroups), a unit is as many blocks of one tile as give every workgroup at
+// most one unit: a run that crossed into another tile would start twice for
+// a few blocks each. deal() finds the tile at r.u; with `first` set it works
+// out the run of workgroup w before. Every wave does so for itself; lanes hold
+// 64 entries at a time.
 template <int BM, int BN>
-__device__ __forceinline__ void deal(Seg* sg, long long u, long long u_end) {
+__device__ __forceinline__ Tile deal(Run& r, bool first, int w) {
   const Args& a = fresh();
-  const int lane = threadIdx.x & 63;
-  auto lane_of = [](long long v, int i) {
-    const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)v, i);
-    const uint32_t hi = __builtin_amdgcn_readlane((int)(v >> 32), i);
-    return (long long)(((unsigned long long)hi << 32) | lo);
-  };
-  long long base = 0;
-  for (int c0 = 0; c0 < a.r.n_ent; c0 += 64) {
-    long long units = 0;
-    int persum = 0;
-    Entry x{-1, 0, 0, 0, 0};
-    if (c0 + lane < a.r.n_ent) {
-      x = entry_of(a.c, a.r, c0 + lane);
-      Geo<BM, BN> g;
-      g.set(a, x);
-      persum = g.sum();
-      units = (long long)persum * a.c.nkv;
+  const int lane = threadIdx.x & 63, n_ent = a.r.n_ent, nkv = a.c.nkv;
+  const bool causal = a.mask == nullptr;
+  Entry x;
+  Geo<BM> g;
+  int persum;
+  long long units, incl, base = 0, total = 0;
+  // One loop over the entries, in passes: 0 counts blocks and tiles, 1 counts
+  // units of several blocks, 2 finds the unit. (One copy of the code: what a
+  // short call waits for most is instructions.)
+  int pass = first ? 0 : 2, tiles = 0, per = first ? 1 : r.per;
+  for (int c0 = 0;;) {
+    if (c0 == 0 ? pass == 0 || pass == 2 : true) {
+      x = Entry{-1, 0, 0, 0, 0};
+      if (c0 + lane < n_ent) x = entry_of(a.c, a.r, c0 + lane);
     }
-    long long incl = units;
-#pragma unroll
-    for (int m = 1; m < 64; m *= 2) {
-      const long long y = __shfl_up(incl, m);
-      if (lane >= m) incl += y;
-    }
+    g.set(a.group, causal, x, BN * per);
+    persum = g.sum();
+    units = (long long)persum * nkv;
+    incl = wave_scan(units);
     const long long all = lane_of(incl, 63);
-    if (u >= 0 && u < base + all) {
-      const int el = __ffsll(__ballot(base + incl > u)) - 1;
-      x.seq = __builtin_amdgcn_readlane(x.seq, el);
-      x.row0 = __builtin_amdgcn_readlane(x.row0, el);
-      x.n = __builtin_amdgcn_readlane(x.n, el);
-      x.len = __builtin_amdgcn_readlane(x.len, el);
-      x.cap = __builtin_amdgcn_readlane(x.cap, el);
-      persum = __builtin_amdgcn_readlane(persum, el);
-      const long long at = u - (base + lane_of(incl, el) - lane_of(units, el));
-      Geo<BM, BN> g;
-      g.set(a, x);
-      const int head = (int)(at / persum);
-      int rem = (int)(at - (long long)head * persum), rt = 0;
-      if (g.causal) {
-        while (rem >= g.nb(rt)) rem -= g.nb(rt), ++rt;
-      } else {
-        rt = rem / g.nb_all;
-        rem -= rt * g.nb_all;
-      }
-      if (lane == 0) {
-        sg->seq = x.seq;
-        sg->row0 = x.row0;
-        sg->n = x.n;
-        sg->len = x.len;
-        sg->cap = x.cap;
-        sg->head = head;
-        sg->rt = rt;
-        sg->nb = g.nb(rt);
-        sg->b0 = rem;
-        sg->b1 = (int)(sg->nb - rem < u_end - u ? sg->nb : rem + (u_end - u));
-      }
-      return;
+    if (pass == 2) {
+      if (r.u < base + all) break;
+      base += all;
+      c0 += 64;
+      continue;
     }
-    base += all;
+    total += all;
+    if (pass == 0) tiles += __builtin_amdgcn_readlane(wave_scan(g.tiles), 63) * nkv;
+    c0 += 64;
+    if (c0 < n_ent) continue;
+    c0 = 0;
+    if (pass == 0 && 2 * tiles <= a.wgs) {
+      per = (int)ceil_div(total, a.wgs - tiles);
+      pass = 1;
+      if (per > 1) {
+        total = 0;
+        continue;
+      }
+      per = 1;
+    }
+    r.per = per;
+    r.quota = pass == 1 || total <= a.wgs ? 1 : ceil_div(total, a.wgs);
+    r.u = w * r.quota;
+    r.u_end = r.u + r.quota < total ? r.u + r.quota : total;
+    if (r.u >= r.u_end) return Tile{};
+    if (n_ent <= 64) break;
+    pass = 2;
   }
-  if (lane == 0) {
-    long long q = (base + a.wgs - 1) / a.wgs;
-    sg->quota = q < a.min_quota ? a.min_quota : q;
-    sg->total = base;
-  }
+  const int el = __ffsll(__ballot(base + incl > r.u)) - 1;
+  x.seq = __builtin_amdgcn_readlane(x.seq, el);
+  x.row0 = __builtin_amdgcn_readlane(x.row0, el);
+  x.n = __builtin_amdgcn_readlane(x.n, el);
+  x.len = __builtin_amdgcn_readlane(x.len, el);
+  x.cap = __builtin_amdgcn_readlane(x.cap, el);
+  persum = __builtin_amdgcn_readlane(persum, el);
+  const long long at = r.u - (base + lane_of(incl, el) - lane_of(units, el));
+  g.set(a.group, causal, x, BN * per);
+  Tile t{};
+  // (a head's units fit 31 bits; most entries' do as well)
+  t.head = at >> 31 ? (int)(at / persum) : (int)((uint32_t)at / (uint32_t)persum);
+  const int rem = (int)(at - (long long)t.head * persum);
+  t.rt = g.find(rem);
+  const int u0 = rem - g.before(t.rt), nu = g.units(t.rt);
+  const int u1 = (int)(nu - u0 < r.u_end - r.u ? nu : u0 + (r.u_end - r.u));
+  t.seq = x.seq;
+  t.row0 = x.row0;
+  t.len = x.len;
+  t.M = g.M;
+  t.group = g.group;
+  t.causal = causal;
+  t.kend = g.tile_end(t.rt);
+  t.b0 = u0 * per;
+  const int nb = t.kend > 0 ? (t.kend + BN - 1) / BN : 1;
+  t.b1 = u1 * per < nb ? u1 * per : nb;
+  t.whole = u0 == 0 && u1 == nu;
+  t.parts = t.whole || u0 > 0 ? 0 : (int)(r.quota == 1 ? r.u + nu - 1 : (r.u + nu - 1) / r.quota) - w + 1;
+  r.u += u1 - u0;
+  return t;
 }
 __device__ __forceinline__ int uni(int x) { return __builtin_amdgcn_readfirstlane(x); }
-__device__ __forceinline__ long long uni64(long long x) {
-  return (long long)(((unsigned long long)(uint32_t)uni((int)(x >> 32)) << 32) | (uint32_t)uni((int)(uint32_t)x));
-}
 
 // 16-byte chunk c of row r of a tile sits at position c ^ swz(r). Eight rows
 // read at one chunk (K fragments) start in eight different 16-byte columns of
@@ -220,34 +309,6 @@ __device__ __forceinline__ float sum_x32(float x) {
   return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 __device__ __forceinline__ float ex2(float x) { return __builtin_amdgcn_exp2f(x); }
-
-// What a lane knows of a segment's tile.
-struct Tile {
-  int seq, row0, len, cap, head, rt, b0, b1, nb;
-  int M, group, kend;
-  bool causal;
-};
-template <int BM, int BN>
-__device__ __forceinline__ Tile tile_of(const Seg& g) {
-  const Args& a = fresh();
-  Tile t;
-  t.seq = uni(g.seq);
-  t.row0 = uni(g.row0);
-  t.len = uni(g.len);
-  t.cap = uni(g.cap);
-  t.head = uni(g.head);
-  t.rt = uni(g.rt);
-  t.b0 = uni(g.b0);
-  t.b1 = uni(g.b1);
-  t.nb = uni(g.nb);
-  Geo<BM, BN> geo;
-  geo.set(a, Entry{t.seq, t.row0, uni(g.n), t.len, t.cap});
-  t.M = geo.M;
-  t.group = geo.group;
-  t.causal = geo.causal;
-  t.kend = geo.tile_end(t.rt);
-  return t;
-}
 
 // Where 16 slots lie: their first row in the cache's bytes from the layer's
 // base, and the bytes from there on that may be read (to the page's end, the
@@ -579,31 +640,36 @@ __device__ __forceinline__ void put_out(const Args& a, const Tile& t, int mm, in
 }
 __device__ __forceinline__ float inverse(float l) { return l > 0.f || l != l ? 1.f / l : 0.f; }
 
-// The workgroup's run of blocks: calls f(tile, whole, slot) for each segment;
-// what other workgroups hold of the last tile is written down for the join.
+// The run of this workgroup: consecutive runs on one XCD (workgroups go round
+// the eight), so that its L2 serves K and V of neighbouring tiles once, and
+// the joins what was written there.
+__device__ __forceinline__ int run_of(int wgs) { return (int)(blockIdx.x & 7) * (wgs >> 3) + (int)(blockIdx.x >> 3); }
+
+// The workgroup's run of blocks: calls f(tile, slot) for each of its tiles,
+// slot being where a shared tile's part goes; what other workgroups hold of the last one is written down for the
+// join.
 template <int BM, int BN, typename F>
-__device__ __forceinline__ void for_segments(int wgs, Seg* sg, F&& f) {
-  const int wv = uni(threadIdx.x >> 6);
-  // consecutive runs on one XCD (workgroups go round the eight)
-  const int w = (int)(blockIdx.x & 7) * (wgs >> 3) + (int)(blockIdx.x >> 3);
-  if (wv == 0) deal<BM, BN>(sg, -1, 0);
-  __syncthreads();
-  const long long quota = uni64(sg->quota), total = uni64(sg->total);
-  long long u = w * quota;
-  const long long u_end = u + quota < total ? u + quota : total;
-  int4 desc = make_int4(0, 0, 0, 0);
-  while (u < u_end) {
-    if (wv == 0) deal<BM, BN>(sg, u, u_end);
-    __syncthreads();
-    const Tile t = tile_of<BM, BN>(*sg);
-    const bool whole = t.b0 == 0 && t.b1 == t.nb;
-    if (!whole && t.b0 == 0) desc = make_int4((int)((u + t.nb - 1) / quota - w) + 1, t.row0, t.head, t.rt);
-    f(t, whole, 2 * w + (t.b0 == 0 ? 1 : 0));
-    u += t.b1 - t.b0;
+__device__ __forceinline__ void for_tiles(int wgs, F&& f) {
+  const int w = run_of(wgs);
+  Run r;
+  Tile t = deal<BM, BN>(r, true, w);
+  int4 desc = make_int4(0, 0, 0, 0), more = desc;
+  while (t.b1 > t.b0) {
+    if (t.parts) {
+      desc = make_int4(t.parts, t.row0, t.head * t.group, t.rt);
+      more = make_int4(t.M, t.group, 0, 0);
+    }
+    f(t, 2 * w + (t.b0 == 0 ? 1 : 0));
+    if (r.u >= r.u_end) break;
     wait_vm<0>();  // no store of this tile in the next one's counts
     __syncthreads();
+    t = deal<BM, BN>(r, false, w);
   }
-  if (threadIdx.x == 0) fresh().desc[w] = desc;
+  if (threadIdx.x == 0) {
+    int4* to = fresh().desc + 2 * w;
+    to[0] = desc;
+    to[1] = more;
+  }
 }
 
 // Waves per SIMD (workgroups per CU) that a kernel's registers are to leave room for.
@@ -626,20 +692,19 @@ __global__ __launch_bounds__(256, (many_waves<T, HDP>())) void k_tree_few(Args a
   __shared__ __attribute__((aligned(1024))) unsigned char sK[4][32 * RB];
   __shared__ __attribute__((aligned(1024))) unsigned char sV[4][32 * RB];
   __shared__ float sM[4][32], sL[4][32];
-  __shared__ Seg sg;
-  for_segments<BM, BN>(a.wgs, &sg, [&](const Tile& t, bool whole, int slot) {
+  for_tiles<BM, BN>(a.wgs, [&](const Tile& t, int slot) {
     const int tid = threadIdx.x, lane = tid & 63, wv = uni(tid >> 6), l32 = lane & 31, h = lane >> 5;
     Ld ld;
     ld.set(t);
     const int kb0 = t.b0 * BN + wv * 32;
     LB *kl = (LB*)sK[wv], *vl = (LB*)sV[wv];
     Place at[2];
-    ld.look(kb0, at);
-    ld.issue(a.k, kl, at, 0);
-    ld.issue(a.v, vl, at, 0);
     const int m = t.rt * BM + l32, mc = m < t.M ? m : t.M - 1, tok = mc / t.group, row = t.row0 + tok;
     u32x4 qf[NQ];
     load_query<T, NQ>(t, mc, qf);
+    ld.look(kb0, at);
+    ld.issue(a.k, kl, at, 0);
+    ld.issue(a.v, vl, at, 0);
     // slots below `own` are seen; the tile needs no mask below `safe`
     const int own = t.causal && t.len + tok + 1 < t.kend ? t.len + tok + 1 : t.kend;
     const int safe0 = t.causal ? t.len + t.rt * BM / t.group + 1 : t.len;
@@ -686,49 +751,48 @@ __global__ __launch_bounds__(256, (many_waves<T, HDP>())) void k_tree_few(Args a
         const int kb = b * BN + wv * 32;
         if (kb + 32 > safe) add_odd_values<T, HDP>(t, kb, seen_bits(t, kb, own, row), o);
       }
-    // the four waves' results, half of the columns at a time
+    // the four waves' results: each puts its own into the LDS (columns of the
+    // first half where K was, the others where V was), then 256 threads add
+    // four columns of a row each
+    constexpr int HC = HDP / 2;
+    const int rows = t.M - t.rt * BM < 32 ? t.M - t.rt * BM : 32;
+    barrier();  // (every wave is done with K and V)
     if (h == 0) sM[wv][l32] = mx, sL[wv][l32] = l;
-    __syncthreads();
-    const float top = fmaxf(fmaxf(sM[0][l32], sM[1][l32]), fmaxf(sM[2][l32], sM[3][l32]));
-    const float f = mx == -INFINITY ? 0.f : ex2(mx - top);
-    float* so = (float*)sK;
-    const Args& z = fresh();
-    float* po = z.part + (size_t)slot * BM * HDP;
-    float* pm = z.part + 2ll * z.wgs * BM * HDP + (size_t)slot * BM * 2;
-    constexpr int HC = HDP / 2;  // columns of a half
+    if (l32 < rows) {
 #pragma unroll
-    for (int hf = 0; hf < 2; ++hf) {
-#pragma unroll
-      for (int dt = 0; dt < NDT / 2; ++dt)
+      for (int dt = 0; dt < NDT; ++dt) {
+        LDS_AS float* so = dt < NDT / 2 ? (LDS_AS float*)sK : (LDS_AS float*)sV;
 #pragma unroll
         for (int j4 = 0; j4 < 4; ++j4) {
-          const f32x16& oo = o[hf * (NDT / 2) + dt];
-          const int c4 = 8 * dt + 2 * j4 + h;  // four columns
-          *(f32x4*)(so + ((wv * 32 + l32) * HC) + ((c4 ^ (l32 & 7)) * 4)) =
-              f32x4{oo[4 * j4] * f, oo[4 * j4 + 1] * f, oo[4 * j4 + 2] * f, oo[4 * j4 + 3] * f};
-        }
-      __syncthreads();
-      const int rows = t.M - t.rt * BM < 32 ? t.M - t.rt * BM : 32;
-      for (int i = tid; i < rows * (HC / 4); i += 256) {
-        const int lm = i / (HC / 4), c4 = i % (HC / 4);
-        float v[4] = {0.f, 0.f, 0.f, 0.f};
-        const float t4 = fmaxf(fmaxf(sM[0][lm], sM[1][lm]), fmaxf(sM[2][lm], sM[3][lm]));
-        float den = 0.f;
-#pragma unroll
-        for (int q4 = 0; q4 < 4; ++q4) {
-          const f32x4 y = *(const f32x4*)(so + ((q4 * 32 + lm) * HC) + ((c4 ^ (lm & 7)) * 4));
-#pragma unroll
-          for (int u = 0; u < 4; ++u) v[u] += y[u];
-          den += sM[q4][lm] == -INFINITY ? 0.f : sL[q4][lm] * ex2(sM[q4][lm] - t4);
-        }
-        if (whole) {
-          put_out<T>(z, t, t.rt * BM + lm, hf * HC + c4 * 4, inverse(den), v);
-        } else {
-          *(f32x4*)(po + (size_t)lm * HDP + hf * HC + c4 * 4) = f32x4{v[0], v[1], v[2], v[3]};
-          if (hf == 0 && c4 == 0) pm[2 * lm] = t4, pm[2 * lm + 1] = den;
+          const int c4 = (8 * dt + 2 * j4 + h) % (HC / 4);  // four columns
+          *(LDS_AS f32x4*)(so + ((wv * 32 + l32) * HC) + ((c4 ^ (l32 & 7)) * 4)) =
+              f32x4{o[dt][4 * j4], o[dt][4 * j4 + 1], o[dt][4 * j4 + 2], o[dt][4 * j4 + 3]};
         }
       }
-      __syncthreads();
+    }
+    barrier();
+    const Args& z = fresh();
+#pragma unroll 1
+    for (int i = tid; i < rows * (HDP / 4); i += 256) {
+      const int lm = i / (HDP / 4), col = i % (HDP / 4) * 4, c4 = col % HC / 4;
+      const LDS_AS float* so = col < HC ? (const LDS_AS float*)sK : (const LDS_AS float*)sV;
+      const float top = fmaxf(fmaxf(sM[0][lm], sM[1][lm]), fmaxf(sM[2][lm], sM[3][lm]));
+      float v[4] = {0.f, 0.f, 0.f, 0.f}, den = 0.f;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float f = sM[k][lm] == -INFINITY ? 0.f : ex2(sM[k][lm] - top);
+        const f32x4 y = *(const LDS_AS f32x4*)(so + ((k * 32 + lm) * HC) + ((c4 ^ (lm & 7)) * 4));
+#pragma unroll
+        for (int u = 0; u < 4; ++u) v[u] = __builtin_fmaf(f, y[u], v[u]);
+        den = __builtin_fmaf(f, sL[k][lm], den);
+      }
+      if (t.whole) {
+        put_out<T>(z, t, t.rt * BM + lm, col, inverse(den), v);
+      } else {
+        float* pm = z.part + 2ll * z.wgs * BM * HDP + (size_t)slot * BM * 2;
+        *(f32x4*)(z.part + ((size_t)slot * BM + lm) * HDP + col) = f32x4{v[0], v[1], v[2], v[3]};
+        if (col == 0) pm[2 * lm] = top, pm[2 * lm + 1] = den;
+      }
     }
   });
 }
@@ -750,9 +814,8 @@ __global__ __launch_bounds__(256, (many_waves<T, HDP>())) void k_tree_many(Args 
   typedef Loader<T, HDP, 4> Ld;
   __shared__ __attribute__((aligned(1024))) unsigned char sK0[NS * 32 * RB], sK1[NS * 32 * RB];
   __shared__ __attribute__((aligned(1024))) unsigned char sV0[NS * 32 * RB], sV1[NS * 32 * RB];
-  __shared__ Seg sg;
   __shared__ int sOdd;
-  for_segments<BM, BN>(a.wgs, &sg, [&](const Tile& t, bool whole, int slot) {
+  for_tiles<BM, BN>(a.wgs, [&](const Tile& t, int slot) {
     const int tid = threadIdx.x, lane = tid & 63, wv = uni(tid >> 6), l32 = lane & 31, h = lane >> 5;
     if (tid == 0) sOdd = 0;  // (a barrier of the first block follows)
     Ld ld;
@@ -762,18 +825,16 @@ __global__ __launch_bounds__(256, (many_waves<T, HDP>())) void k_tree_many(Args 
 #pragma unroll
       for (int n = 0; n < NS; ++n) ld.look(b * BN + 32 * n, at[n]);
     };
-    auto issue = [&](LB* kd, LB* vd) {
+    auto issue = [&](const char* src, LB* dst) {
 #pragma unroll
-      for (int n = 0; n < NS; ++n) ld.issue(a.k, kd + n * 32 * RB, at[n], wv);
-#pragma unroll
-      for (int n = 0; n < NS; ++n) ld.issue(a.v, vd + n * 32 * RB, at[n], wv);
+      for (int n = 0; n < NS; ++n) ld.issue(src, dst + n * 32 * RB, at[n], wv);
     };
-    look(t.b0);
-    LB *k0 = (LB*)sK0, *k1 = (LB*)sK1, *v0 = (LB*)sV0, *v1 = (LB*)sV1;
-    issue(k0, v0);
     const int m = t.rt * BM + wv * 32 + l32, mc = m < t.M ? m : t.M - 1, tok = mc / t.group, row = t.row0 + tok;
     u32x4 qf[NQ];
     load_query<T, NQ>(t, mc, qf);
+    look(t.b0);
+    issue(a.k, (LB*)sK0);
+    issue(a.v, (LB*)sV0);
     const int own = t.causal && t.len + tok + 1 < t.kend ? t.len + tok + 1 : t.kend;
     // (of the tile's first row: the waves clean V together)
     const int safe0 = t.causal ? t.len + t.rt * BM / t.group + 1 : t.len;
@@ -785,14 +846,20 @@ __global__ __launch_bounds__(256, (many_waves<T, HDP>())) void k_tree_many(Args 
       for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
     float mx = -INFINITY, l = 0.f;
     look(t.b0 + 1);
-    auto step = [&](const LB* kt, LB* vt, LB* kn, LB* vn, int b) {
+    auto step = [&](auto stage, int b) {
+      // (by name: the compiler lets reads of one stage run beside loads into
+      // the other only where it can tell them apart)
+      constexpr int S = decltype(stage)::value;
+      LB *kt = S ? (LB*)sK1 : (LB*)sK0, *vt = S ? (LB*)sV1 : (LB*)sV0;
+      LB *kn = S ? (LB*)sK0 : (LB*)sK1, *vn = S ? (LB*)sV0 : (LB*)sV1;
       wait_vm<0>();  // this wave's part of the block is here,
       barrier();     // so are the others', and the other block is worked off
-      if (b + 1 < t.b1) issue(kn, vn);
-      look(b + 2);
+      if (b + 1 < t.b1) issue(a.k, kn);
       const int kb = b * BN;
       f32x16 s[NS];
       scores<T, HDP, NS, NQ>(kt, qf, s);
+      // (loads take their turns at issue: these go out beside the products)
+      if (b + 1 < t.b1) issue(a.v, vn);
       if (kb + BN > safe) {
 #pragma unroll
         for (int n = 0; n < NS; ++n) {
@@ -804,6 +871,7 @@ __global__ __launch_bounds__(256, (many_waves<T, HDP>())) void k_tree_many(Args 
       }
       Values<T, HDP, NS, false> vv;
       vv.first(vt);
+      look(b + 2);
       soften<NDT, NS>(s, a.c2, mx, l, o);
       Probs p[NS];
       if constexpr (sizeof(T) == 2) {
@@ -813,8 +881,8 @@ __global__ __launch_bounds__(256, (many_waves<T, HDP>())) void k_tree_many(Args 
       vv.add(s, p, o);
     };
     for (int b = t.b0; b < t.b1; b += 2) {
-      step(k0, v0, k1, v1, b);
-      if (b + 1 < t.b1) step(k1, v1, k0, v0, b + 1);
+      step(std::integral_constant<int, 0>(), b);
+      if (b + 1 < t.b1) step(std::integral_constant<int, 1>(), b + 1);
     }
     l = sum_x32(l);
     if (sOdd)  // (written before the last block's barrier)
@@ -824,7 +892,7 @@ __global__ __launch_bounds__(256, (many_waves<T, HDP>())) void k_tree_many(Args 
     float* po = z.part + (size_t)slot * BM * HDP;
     float* pm = z.part + 2ll * z.wgs * BM * HDP + (size_t)slot * BM * 2;
     const float inv = inverse(l);
-    if (whole) {
+    if (t.whole) {
 #pragma unroll
       for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
@@ -837,65 +905,162 @@ __global__ __launch_bounds__(256, (many_waves<T, HDP>())) void k_tree_many(Args 
       for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
         for (int j4 = 0; j4 < 4; ++j4)
-          *(f32x4*)(po + (size_t)(wv * 32 + l32) * HDP + 32 * dt + 8 * j4 + 4 * h) =
+          // (in lane order: whole lines)
+          *(f32x4*)(po + wv * 32 * HDP + ((dt * 4 + j4) * 64 + lane) * 4) =
               f32x4{o[dt][4 * j4], o[dt][4 * j4 + 1], o[dt][4 * j4 + 2], o[dt][4 * j4 + 3]};
       if (h == 0) pm[2 * (wv * 32 + l32)] = mx, pm[2 * (wv * 32 + l32) + 1] = l;
     }
   });
 }
 
-// Tiles whose keys several workgroups shared out: their partials, in order. A
-// workgroup takes eight rows of one tile, a wave two of them.
+// The join: tiles whose keys several workgroups shared out, from their parts
+// (part 0 in the last slot of its run, the others in the first slots of the
+// runs behind it). How many tiles there are only the descriptors tell, so a
+// fixed number of workgroups (a launch pays for every one) reads them all,
+// lists the work in the LDS and goes through it in turn. With up to four parts
+// each wave does a piece of its own, all parts in flight; with more, the four
+// waves take every fourth part of one piece, four at a time, so that sixteen
+// parts cost one round trip, and their sums meet in the LDS in wave order.
+constexpr int JOIN_MOST = 1024;  // runs
+__device__ __forceinline__ size_t part_slot(int w, int i) { return (size_t)(2ll * (w + i) + (i == 0 ? 1 : 0)); }
+
+// One batch of four parts with maxima m and sums l, values v: into top, den, o.
+template <typename V, int N>
+__device__ __forceinline__ void join_parts(const float (&m)[4], const float (&l)[4], const V (&v)[4][N], float& top,
+                                           float& den, V (&o)[N]) {
+  const float mt = fmaxf(top, fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])));
+  const float back = top == -INFINITY ? 0.f : ex2(top - mt);
+  den *= back;
+#pragma unroll
+  for (int t = 0; t < N; ++t) o[t] *= back;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float f = m[i] == -INFINITY ? 0.f : ex2(m[i] - mt);
+    den = __builtin_fmaf(f, l[i], den);
+#pragma unroll
+    for (int t = 0; t < N; ++t) o[t] += f * v[i][t];
+  }
+  top = mt;
+}
+
+// BM = 32: parts are row-major; a piece is one row, a lane HDP / 64 columns of
+// it. BM = 128: parts lie in the order in which the waves hold them; a piece
+// is 32 columns of 32 rows, a lane four of every eight columns of its row.
 template <typename T, int HDP, int BM>
 __global__ __launch_bounds__(256) void k_tree_join(Args a) {
-  const int w = blockIdx.x;
-  const int4 d = a.desc[w];
-  if (d.x == 0) return;
-  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, hd = a.c.hd;
-  // the entry's rows
-  const int row0 = d.y, head = d.z, rt = d.w;
-  const int e = wave_find(a.r.start, a.r.n_ent, row0);
-  const Entry x = entry_of(a.c, a.r, e < a.r.n_ent ? e : a.r.n_ent - 1);
-  constexpr int C = HDP / 64;
+  constexpr bool MANY = BM == 128;
+  constexpr int C = MANY ? 4 : HDP / 64, N = MANY ? 4 : 1, NDT = HDP / 32;
+  typedef float fc __attribute__((ext_vector_type(C)));
+  __shared__ int sPre[JOIN_MOST + 1];
+  __shared__ int sWave[4];
+  __shared__ fc sO[4][N][64];
+  __shared__ float sT[4][64], sD[4][64];
+  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, l32 = lane & 31, h = lane >> 5, hd = a.c.hd;
+  // pieces of a tile that workgroups take at once: one, or four of few parts
+  auto takes = [&](const int4& d, const int4& e) {
+    if (d.x == 0) return 0;
+    const int rows = e.x - d.w * BM < BM ? e.x - d.w * BM : BM;
+    const int pieces = MANY ? (rows + 31) / 32 * ((hd + 31) / 32) : rows;
+    return d.x <= 4 ? (pieces + 3) / 4 : pieces;
+  };
+  int before = 0;
+  for (int c0 = 0; c0 < a.wgs; c0 += 256) {
+    const int w = c0 + tid;
+    const int cnt = w < a.wgs ? takes(a.desc[2 * w], a.desc[2 * w + 1]) : 0;
+    const int incl = wave_scan(cnt);
+    if (lane == 63) sWave[wv] = incl;
+    __syncthreads();
+    int off = before;
 #pragma unroll
-  for (int rr = 0; rr < 2; ++rr) {
-    const int lm = blockIdx.y * 8 + wv * 2 + rr, mm = rt * BM + lm;
-    if (mm >= x.n * a.group) continue;
-    const float* pm = a.part + 2ll * a.wgs * BM * HDP;
-    auto slot = [&](int i) { return i == 0 ? 2ll * w + 1 : 2ll * (w + i); };
-    float top = -INFINITY;
-    for (int i = lane; i < d.x; i += 64) top = fmaxf(top, pm[(slot(i) * BM + lm) * 2]);
-#pragma unroll
-    for (int s = 1; s < 64; s *= 2) top = fmaxf(top, __shfl_xor(top, s));
-    float den = 0.f, o[C];
-#pragma unroll
-    for (int t = 0; t < C; ++t) o[t] = 0.f;
-    for (int i0 = 0; i0 < d.x; i0 += 64) {
-      float f = 0.f, ld = 0.f;
-      if (i0 + lane < d.x) {
-        const float m = pm[(slot(i0 + lane) * BM + lm) * 2];
-        f = m == -INFINITY ? 0.f : ex2(m - top);
-        ld = f == 0.f ? 0.f : f * pm[(slot(i0 + lane) * BM + lm) * 2 + 1];
-      }
-      const int cnt = d.x - i0 < 64 ? d.x - i0 : 64;
-#pragma unroll 8
-      for (int i = 0; i < cnt; ++i) {
-        const float fi = __shfl(f, i);
-        den += __shfl(ld, i);
-        const float* po = a.part + (slot(i0 + i) * BM + lm) * HDP + lane * C;
-#pragma unroll
-        for (int t = 0; t < C; ++t) o[t] = __builtin_fmaf(fi, po[t], o[t]);
-      }
+    for (int k = 0; k < 4; ++k) off += k < wv ? sWave[k] : 0, before += sWave[k];
+    if (w < a.wgs) sPre[w + 1] = off + incl;
+    __syncthreads();
+  }
+  if (tid == 0) sPre[0] = 0;
+  __syncthreads();
+  const float* pm = a.part + 2ll * a.wgs * BM * HDP;
+  for (int take = blockIdx.x; take < before; take += gridDim.x) {
+    int lo = 0, hi = a.wgs - 1;  // the run whose tile it is of
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) / 2;
+      if (sPre[mid] <= take) lo = mid;
+      else hi = mid - 1;
     }
-    const float inv = den > 0.f || den != den ? 1.f / den : 0.f;
-    const int tk = mm / a.group;
-    T* dst = (T*)a.out + (size_t)(row0 + tk) * (size_t)a.ldo + (size_t)(head * a.group + (mm - tk * a.group)) * hd;
+    const int w = uni(lo);
+    const int4 d = a.desc[2 * w], e = a.desc[2 * w + 1];
+    const int n = d.x, M = e.x, group = e.y, m0 = d.w * BM;
+    const bool own = n <= 4;  // a piece to each wave
+    const int piece = own ? (take - sPre[w]) * 4 + wv : take - sPre[w];
+    const int nd = (hd + 31) / 32, rg = MANY ? piece / nd : 0, dt = MANY ? piece % nd : 0;
+    const int lm = MANY ? rg * 32 + l32 : piece;  // the lane's row of the tile
+    // (rows behind the last have nothing written: theirs is not used)
+    const bool live = MANY ? m0 + rg * 32 < M : m0 + lm < M;
+    const int lr = live ? lm : 0;
+    const float* po = a.part + (MANY ? (live ? rg : 0) * 32 * HDP + (dt * 256 + lane) * 4 : lr * HDP + lane * C);
+    float top = -INFINITY, den = 0.f;
+    fc o[N];
 #pragma unroll
-    for (int t = 0; t < C; ++t)
-      if (lane * C + t < hd) {
-        if constexpr (sizeof(T) == 2) dst[lane * C + t] = (T)bf2(o[t] * inv, 0.f);
-        else dst[lane * C + t] = o[t] * inv;
+    for (int t = 0; t < N; ++t) o[t] = (fc)0.f;
+    const int by = own ? 1 : 4;
+    for (int i0 = own ? 0 : wv; i0 < n; i0 += 16) {
+      float m[4], l[4];
+      fc v[4][N];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const bool in = i0 + by * i < n;
+        const size_t s = part_slot(w, in ? i0 + by * i : i0) * BM;
+        const f32x2 ml = *(const f32x2*)(pm + (s + lr) * 2);
+        m[i] = in ? ml.x : -INFINITY;
+        l[i] = in ? ml.y : 0.f;
+#pragma unroll
+        for (int t = 0; t < N; ++t) {
+          const fc y = *(const fc*)(po + s * HDP + t * 256);
+          v[i][t] = in ? y : (fc)0.f;
+        }
       }
+      join_parts(m, l, v, top, den, o);
+    }
+    auto put = [&](const fc& x, float inv, int col) {
+      const int mm = m0 + lm, tk = mm / group;
+      if (mm >= M || col >= hd) return;
+      T* dst = (T*)a.out + (size_t)(d.y + tk) * (size_t)a.ldo + (size_t)(d.z + mm - tk * group) * hd + col;
+      float r[C];
+#pragma unroll
+      for (int t = 0; t < C; ++t) r[t] = x[t] * inv;
+      if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int t = 0; t < C; ++t) dst[t] = r[t];
+      } else if constexpr (C == 1) {
+        dst[0] = (T)bf2(r[0], 0.f);
+      } else {
+        uint32_t u[C / 2];
+#pragma unroll
+        for (int t = 0; t < C / 2; ++t) u[t] = bf2(r[2 * t], r[2 * t + 1]);
+        __builtin_memcpy(__builtin_assume_aligned(dst, 2 * C), u, 2 * C);
+      }
+    };
+    if (own) {
+      const float inv = inverse(den);
+      if (live) {
+#pragma unroll
+        for (int t = 0; t < N; ++t) put(o[t], inv, MANY ? 32 * dt + 8 * t + 4 * h : lane * C);
+      }
+      continue;
+    }
+#pragma unroll
+    for (int t = 0; t < N; ++t) sO[wv][t][lane] = o[t];
+    sT[wv][lane] = top;
+    sD[wv][lane] = den;
+    __syncthreads();
+    if (live && wv < N) {  // (BM = 128: a wave to the columns 8 wv .. + 7)
+      float m4[4], l4[4], t1 = -INFINITY, d1 = 0.f;
+      fc v4[4][1], o1[1] = {(fc)0.f};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) m4[k] = sT[k][lane], l4[k] = sD[k][lane], v4[k][0] = sO[k][wv][lane];
+      join_parts(m4, l4, v4, t1, d1, o1);
+      put(o1[0], inverse(d1), MANY ? 32 * dt + 8 * wv + 4 * h : lane * C);
+    }
+    __syncthreads();
   }
 }
 
@@ -911,7 +1076,7 @@ int tile_rows(const TreeAttnDesc& d) {
 int tree_wgs(const TreeAttnDesc& d) {
   const int esz = d.c.dtype == DT_BF16 ? 2 : 4;
   const int per = pad_hd(d.c.dtype, d.c.hd) * esz <= 256 ? 2 : 1;
-  return std::max(8, d.cus / 8 * 8) * per;
+  return std::min(std::max(8, d.cus / 8 * 8) * per, JOIN_MOST);
 }
 
 template <typename T, int HDP>
@@ -921,8 +1086,11 @@ hipError_t run(const TreeAttnDesc& d, const Args& a, hipStream_t st) {
   else hipLaunchKernelGGL((k_tree_many<T, HDP>), dim3(a.wgs), dim3(256), 0, st, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if (rows == 32) hipLaunchKernelGGL((k_tree_join<T, HDP, 32>), dim3(a.wgs, 4), dim3(256), 0, st, a);
-  else hipLaunchKernelGGL((k_tree_join<T, HDP, 128>), dim3(a.wgs, 16), dim3(256), 0, st, a);
+  // (at most as many as there can be pieces to take)
+  const long long tiles = ((long long)d.r.n_rows * a.group / rows + d.r.n_ent) * d.c.nkv;
+  const int joins = (int)std::min({(long long)4 * d.cus, 1024ll, tiles * (rows == 32 ? 32 : HDP / 8)});
+  if (rows == 32) hipLaunchKernelGGL((k_tree_join<T, HDP, 32>), dim3(joins), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((k_tree_join<T, HDP, 128>), dim3(joins), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 
@@ -930,7 +1098,7 @@ hipError_t run(const TreeAttnDesc& d, const Args& a, hipStream_t st) {
 
 size_t tree_attn_scratch(const TreeAttnDesc& d) {
   const size_t w = tree_wgs(d), rows = tile_rows(d), hdp = pad_hd(d.c.dtype, d.c.hd);
-  return w * 16 + 2 * w * rows * (hdp + 2) * 4;
+  return w * 32 + 2 * w * rows * (hdp + 2) * 4;
 }
 
 hipError_t launch_tree_attn(const TreeAttnDesc& d, hipStream_t st) {
@@ -952,8 +1120,7 @@ hipError_t launch_tree_attn(const TreeAttnDesc& d, hipStream_t st) {
   a.v = (const char*)d.c.v + layer;
   a.wgs = tree_wgs(d);
   a.desc = (int4*)d.scratch;
-  a.part = (float*)((char*)d.scratch + (size_t)a.wgs * 16);
-  a.min_quota = 1;
+  a.part = (float*)((char*)d.scratch + (size_t)a.wgs * 32);
   const int hdp = pad_hd(d.c.dtype, d.c.hd);
   if (d.c.dtype == DT_BF16)
     return hdp == 64 ? run<uint16_t, 64>(d, a, st) : hdp == 128 ? run<uint16_t, 128>(d, a, st)
