@@ -497,7 +497,9 @@ def make_pages(k, v, table, lens, held, refs, status) -> vla_pages:
     p = vla_pages(VLA_BF16 if kt == "bfloat16" else VLA_F32, layers, nkv, hd, page, n_pages, n_seqs, wide,
                   *(_ptr(t) for t in (k, v, table, lens, held, refs, status)))
     p._src = (k, v, table, lens, held, refs, status)
-    p._dev, p._type = dev, k.dtype
+    # what the calls compare their operands with
+    p._dev, p._index, p._type, p._ints = dev, dev.index, k.dtype, table.dtype
+    p._nkv, p._hd, p._scale = nkv, hd, hd ** -0.5
     return p
 
 
@@ -511,7 +513,7 @@ def make_rows(start, n_rows: int, seqs=None) -> vla_rows:
     if seqs is not None:
         _one_device([("start", dev), ("seqs", _dev(seqs, "seqs", "int32", (n,)))])
     r = vla_rows(int(n_rows), n, _ptr(start), _ptr(seqs))
-    r._src, r._dev = (start, seqs), dev
+    r._src, r._dev, r._n, r._entries = (start, seqs), dev, int(n_rows), n
     return r
 
 
@@ -535,36 +537,58 @@ def make_rope_norm(cos=None, sin=None, q_gain=None, k_gain=None, gain_plus_one: 
     p = vla_rope_norm(_ptr(q_gain), _ptr(k_gain), 1 if gain_plus_one else 0, float(eps), _ptr(cos), _ptr(sin),
                       n_pos, rot)
     p._src, p._dev = (cos, sin, q_gain, k_gain), _one_device(pairs)
+    p._gains = [(what, int(g.shape[0])) for what, g in (("q_gain", q_gain), ("k_gain", k_gain)) if g is not None]
     return p
 
 
+# A decoding step makes a call of these per layer and kernel, so each check is
+# one expression while everything is right; what is wrong is found out after.
+
 def _at(pages, *others) -> None:
-    """The current device holds the cache and the others' tensors."""
+    """The current device holds the cache and the descriptors' tensors."""
     import torch
-    dev = pages._dev
     for x in others:
-        if x is not None and x != dev:
-            raise _einval(f"a tensor is on {x}, the cache on {dev}")
-    if dev.index is not None and torch.cuda.current_device() != dev.index:
-        raise _einval(f"the cache is on {dev}, the current device is {torch.cuda.current_device()}")
+        if x is not None and x != pages._dev:
+            raise _einval(f"a tensor is on {x}, the cache on {pages._dev}")
+    if torch.cuda.current_device() != pages._index:
+        raise _einval(f"the cache is on {pages._dev}, the current device is {torch.cuda.current_device()}")
 
 
-def _heads(x, what: str, pages, rows, heads=None):
-    """[n_rows, heads, head_dim] of the cache's type, heads side by side; its
-    row stride and heads."""
-    if not getattr(x, "is_cuda", False):
-        raise _einval(f"{what} must be a device (cuda) tensor")
-    if x.dtype != pages._type:
-        raise _einval(f"{what} must be {pages._type}, got {x.dtype}")
-    shape, stride = x.shape, x.stride()
-    hd = pages.head_dim
-    if len(shape) != 3 or shape[2] != hd or shape[0] != rows.n_rows or (heads is not None and shape[1] != heads):
-        raise _einval(f"{what} must be [{rows.n_rows}, {'heads' if heads is None else heads}, {hd}], got "
-                      f"{tuple(shape)}")
-    if stride[2] != 1 or (shape[1] > 1 and stride[1] != hd):
+def _heads(x, what: str, pages, n: int, heads=None) -> int:
+    """[n, heads, head_dim] of the cache's type on its device, a row's heads
+    side by side; the row stride."""
+    shape, stride, hd = x.shape, x.stride(), pages._hd
+    if (x.get_device() != pages._index or x.dtype != pages._type or len(shape) != 3 or shape[0] != n
+            or shape[2] != hd or (heads is not None and shape[1] != heads) or stride[2] != 1
+            or (stride[1] != hd and shape[1] > 1)):
+        if not getattr(x, "is_cuda", False):
+            raise _einval(f"{what} must be a device (cuda) tensor")
+        if x.dtype != pages._type:
+            raise _einval(f"{what} must be {pages._type}, got {x.dtype}")
+        if len(shape) != 3 or shape[2] != hd or shape[0] != n or (heads is not None and shape[1] != heads):
+            raise _einval(f"{what} must be [{n}, {'heads' if heads is None else heads}, {hd}], got {tuple(shape)}")
+        if x.get_device() != pages._index:
+            raise _einval(f"{what}: a tensor is on {x.device}, the cache on {pages._dev}")
         raise _einval(f"{what}: a row's heads must be contiguous")
     # (a single row has no stride that counts)
-    return max(stride[0], shape[1] * hd) if shape[0] <= 1 else stride[0]
+    return stride[0] if n > 1 else max(stride[0], shape[1] * hd)
+
+
+def _ints(x, what: str, pages, shape) -> int:
+    """int32 of this shape on the cache's device; its pointer (None: None)."""
+    if x is None:
+        return None
+    if not (hasattr(x, "get_device") and x.get_device() == pages._index and x.dtype == pages._ints
+            and tuple(x.shape) == shape and x.is_contiguous()):
+        dev = _dev(x, what, "int32", shape)
+        raise _einval(f"{what}: a tensor is on {dev}, the cache on {pages._dev}")
+    return x.data_ptr()
+
+
+def _list(x, what: str) -> tuple:
+    if len(getattr(x, "shape", ())) != 1:
+        raise _einval(f"{what} must be [n]")
+    return tuple(x.shape)
 
 
 def vla_pages_init(pages: vla_pages, stream: int = 0) -> None:
@@ -581,19 +605,17 @@ def vla_qk_norm_rope(pages: vla_pages, layer: int, rows: vla_rows, rope: vla_rop
                      stream: int = 0) -> None:
     """q, q_out [n_rows, nq, head_dim], k and v [n_rows, kv_heads, head_dim]
     (rows may be strided: slices of one QKV tensor), pos int32 [n_rows]."""
-    nkv = pages.kv_heads
-    nq = int(q.shape[1]) if len(q.shape) == 3 else -1
-    ldq, ldk, ldv = _heads(q, "q", pages, rows), _heads(k, "k", pages, rows, nkv), _heads(v, "v", pages, rows, nkv)
-    ldo = _heads(q_out, "q_out", pages, rows, nq)
-    cos, _, qg, kg = rope._src
-    for what, g in (("q_gain", qg), ("k_gain", kg)):
-        if g is not None and g.shape[0] != pages.head_dim:
-            raise _einval(f"{what} holds {g.shape[0]} elements, head_dim is {pages.head_dim}")
-    _at(pages, rows._dev, rope._dev, q.device, k.device, v.device, q_out.device,
-        None if pos is None else _dev(pos, "pos", "int32", (rows.n_rows,)))
-    _check(_lib.vla_qk_norm_rope(ctypes.byref(pages), layer, ctypes.byref(rows), ctypes.byref(rope), _ptr(pos), nq,
-                                 q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, q_out.data_ptr(), ldo,
-                                 stream or None))
+    n, nkv = rows._n, pages._nkv
+    ldq = _heads(q, "q", pages, n)
+    nq = q.shape[1]
+    ldk, ldv, ldo = _heads(k, "k", pages, n, nkv), _heads(v, "v", pages, n, nkv), _heads(q_out, "q_out", pages, n, nq)
+    for what, g in rope._gains:
+        if g != pages._hd:
+            raise _einval(f"{what} holds {g} elements, head_dim is {pages._hd}")
+    _at(pages, rows._dev, rope._dev)
+    _check(_lib.vla_qk_norm_rope(ctypes.byref(pages), layer, ctypes.byref(rows), ctypes.byref(rope),
+                                 _ints(pos, "pos", pages, (n,)), nq, q.data_ptr(), ldq, k.data_ptr(), ldk,
+                                 v.data_ptr(), ldv, q_out.data_ptr(), ldo, stream or None))
 
 
 def vla_tree_attention_scratch(pages: vla_pages, rows: vla_rows, nq: int) -> int:
@@ -608,41 +630,44 @@ def vla_tree_attention(pages: vla_pages, layer: int, rows: vla_rows, q, out, scr
     """q and out [n_rows, nq, head_dim] (rows may be strided), scratch uint8
     (vla_tree_attention_scratch), mask int32 [n_rows, words] (the bits of
     uint32) or None; scale None: 1 / sqrt(head_dim)."""
-    nq = int(q.shape[1]) if len(q.shape) == 3 else -1
-    ldq, ldo = _heads(q, "q", pages, rows), _heads(out, "out", pages, rows, nq)
-    words, mdev = 0, None
+    n = rows._n
+    ldq = _heads(q, "q", pages, n)
+    nq = q.shape[1]
+    ldo = _heads(out, "out", pages, n, nq)
+    words, bits = 0, None
     if mask is not None:
-        if len(mask.shape) != 2 or mask.shape[0] != rows.n_rows:
-            raise _einval(f"mask must be [{rows.n_rows}, words], got {tuple(mask.shape)}")
-        mdev, words = _dev(mask, "mask", "int32"), int(mask.shape[1])
-    _at(pages, rows._dev, q.device, out.device, _dev(scratch, "scratch", "uint8"), mdev)
-    _check(_lib.vla_tree_attention(ctypes.byref(pages), layer, ctypes.byref(rows), _ptr(mask), words, nq,
-                                   pages.head_dim ** -0.5 if scale is None else scale, q.data_ptr(), ldq,
-                                   out.data_ptr(), ldo, scratch.data_ptr(), scratch.numel(), stream or None))
+        if len(mask.shape) != 2:
+            raise _einval(f"mask must be [{n}, words], got {tuple(mask.shape)}")
+        words = mask.shape[1]
+        bits = _ints(mask, "mask", pages, (n, words))
+    if _dev(scratch, "scratch", "uint8") != pages._dev:
+        raise _einval(f"scratch: a tensor is on {scratch.device}, the cache on {pages._dev}")
+    _at(pages, rows._dev)
+    _check(_lib.vla_tree_attention(ctypes.byref(pages), layer, ctypes.byref(rows), bits, words, nq,
+                                   pages._scale if scale is None else scale, q.data_ptr(), ldq, out.data_ptr(), ldo,
+                                   scratch.data_ptr(), scratch.numel(), stream or None))
 
 
 def vla_pages_fork(pages: vla_pages, src, dst, made, stream: int = 0) -> None:
     """src, dst, made: int32 [n]."""
-    if len(src.shape) != 1:
-        raise _einval("src must be [n]")
-    _at(pages, _dev(src, "src", "int32"), _dev(dst, "dst", "int32", src.shape), _dev(made, "made", "int32", src.shape))
-    _check(_lib.vla_pages_fork(ctypes.byref(pages), int(src.shape[0]), _ptr(src), _ptr(dst), _ptr(made),
-                               stream or None))
+    n = _list(src, "src")
+    _at(pages)
+    _check(_lib.vla_pages_fork(ctypes.byref(pages), n[0], _ints(src, "src", pages, n), _ints(dst, "dst", pages, n),
+                               _ints(made, "made", pages, n), stream or None))
 
 
 def vla_pages_commit(pages: vla_pages, rows: vla_rows, kept=None, n_kept=None, stream: int = 0) -> None:
     """kept int32 [n_rows], n_kept int32 [n_entries] (None: see vla.h)."""
-    _at(pages, rows._dev, None if kept is None else _dev(kept, "kept", "int32", (rows.n_rows,)),
-        None if n_kept is None else _dev(n_kept, "n_kept", "int32", (rows.n_entries,)))
-    _check(_lib.vla_pages_commit(ctypes.byref(pages), ctypes.byref(rows), _ptr(kept), _ptr(n_kept), stream or None))
+    _at(pages, rows._dev)
+    _check(_lib.vla_pages_commit(ctypes.byref(pages), ctypes.byref(rows), _ints(kept, "kept", pages, (rows._n,)),
+                                 _ints(n_kept, "n_kept", pages, (rows._entries,)), stream or None))
 
 
 def vla_pages_release(pages: vla_pages, seqs, stream: int = 0) -> None:
     """seqs int32 [n]."""
-    if len(seqs.shape) != 1:
-        raise _einval("seqs must be [n]")
-    _at(pages, _dev(seqs, "seqs", "int32"))
-    _check(_lib.vla_pages_release(ctypes.byref(pages), int(seqs.shape[0]), _ptr(seqs), stream or None))
+    n = _list(seqs, "seqs")
+    _at(pages)
+    _check(_lib.vla_pages_release(ctypes.byref(pages), n[0], _ints(seqs, "seqs", pages, n), stream or None))
 
 
 def exported_symbols() -> Iterable[str]:

@@ -154,18 +154,17 @@ hipError_t launch_rope_norm(const RopeNormDesc& d, hipStream_t st) {
 // cache's state alone. One workgroup deals: the work is a scan of refs.
 // ---------------------------------------------------------------------------
 
-constexpr int PT = 1024;  // threads of the dealing workgroup
+// Threads of the dealing workgroup: few for few sequences and a small pool
+// (its barriers are most of the call), many where refs take long to scan.
+constexpr int PT_FEW = 256, PT_MANY = 1024;
+inline bool few_to_deal(const PagedCache& c, int n) { return n <= 16 && c.n_pages <= 4 * 8 * PT_FEW; }
 
 // Exclusive prefix of x over the workgroup, and the total.
+template <int PT>
 __device__ __forceinline__ int block_scan(int x, int* total) {
   __shared__ int sW[PT / 64];
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-  int s = x;
-#pragma unroll
-  for (int m = 1; m < 64; m *= 2) {
-    const int y = __shfl_up(s, m);
-    if (lane >= m) s += y;
-  }
+  const int s = wave_scan(x);
   __syncthreads();  // the last call's sums are read
   if (lane == 63) sW[wv] = s;
   __syncthreads();
@@ -180,21 +179,30 @@ __device__ __forceinline__ int block_scan(int x, int* total) {
   return before + s - x;
 }
 
+// Which of the thread's eight pages of the 8 PT from `base` on are free.
+__device__ __forceinline__ unsigned free_bits(const PagedCache& c, int base) {
+  const int first = base + 8 * threadIdx.x;
+  unsigned bits = 0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int p = first + j < c.n_pages ? first + j : c.n_pages - 1;
+    if (c.refs[p] == 0 && first + j < c.n_pages) bits |= 1u << j;
+  }
+  return bits;
+}
 // The next `want` (<= PT) free pages from page *pos on, ascending, into list;
 // returns how many there are and moves *pos behind the last one taken. Pages
-// that this launch gave out lie before *pos, so refs may be read as it was.
-__device__ int take_free(const PagedCache& c, int* pos, int want, int* list) {
+// that this launch gave out lie before *pos, so refs may be read as it was;
+// bits0 is free_bits(0), which a kernel reads while it has nothing else.
+template <int PT>
+__device__ __forceinline__ int take_free(const PagedCache& c, unsigned bits0, int* pos, int want, int* list) {
   int found = 0, p0 = *pos;
-  for (int base = p0 & ~7; found < want && base < c.n_pages; base += 8 * PT) {
+  for (int base = p0 & ~(8 * PT - 1); found < want && base < c.n_pages; base += 8 * PT) {
     const int first = base + 8 * threadIdx.x;
-    unsigned bits = 0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int p = first + j;
-      if (p >= p0 && p < c.n_pages && c.refs[p] == 0) bits |= 1u << j;
-    }
+    unsigned bits = base == 0 ? bits0 : free_bits(c, base);
+    if (first < p0) bits &= p0 - first < 8 ? ~0u << (p0 - first) : 0u;
     int total;
-    int rank = found + block_scan(__popc(bits), &total);
+    int rank = found + block_scan<PT>(__popc(bits), &total);
     for (; bits && rank < want; bits &= bits - 1, ++rank) list[rank] = first + __ffs(bits) - 1;
     found += total;
   }
@@ -221,9 +229,12 @@ hipError_t launch_pages_init(const PagedCache& c, hipStream_t st) {
 }
 
 // Pages for len + rows slots of every entry, entries in order.
+template <int PT>
 __global__ __launch_bounds__(PT) void k_pages_reserve(PagedCache c, PagedRows r) {
-  __shared__ int sList[PT], sOff[PT], sSeq[PT], sHeld[PT];
+  __shared__ int sList[PT], sOff[PT], sHeld[PT];
+  __shared__ __attribute__((aligned(16))) int sSeq[PT];
   const int tid = threadIdx.x;
+  const unsigned bits0 = free_bits(c, 0);
   int pos = 0;
   for (int base = 0; base < r.n_ent; base += PT) {
     const int e = base + tid;
@@ -244,20 +255,24 @@ __global__ __launch_bounds__(PT) void k_pages_reserve(PagedCache c, PagedRows r)
     sHeld[tid] = held;
     __syncthreads();
     // a sequence that is listed twice: the first entry counts
-    if (need > 0)
-      for (int j = 0; j < tid; ++j)
-        if (sSeq[j] == seq) {
-          need = 0;
-          break;
-        }
+    if (need > 0) {
+      bool again = false;
+#pragma unroll 4
+      for (int j = 0; j < tid; j += 4) {
+        const int4 o = *(const int4*)(sSeq + j);
+        const int q = tid - j;  // entries of these four that come before
+        again = again || o.x == seq || (o.y == seq && q > 1) || (o.z == seq && q > 2) || (o.w == seq && q > 3);
+      }
+      if (again) need = 0;
+    }
     int total;
-    const int off = block_scan(need, &total);
+    const int off = block_scan<PT>(need, &total);
     sOff[tid] = off;
     __syncthreads();
     int given = 0;
     while (given < total) {
       const int want = total - given < PT ? total - given : PT;
-      const int got = take_free(c, &pos, want, sList);
+      const int got = take_free<PT>(c, bits0, &pos, want, sList);
       if (tid < got) {
         // the last entry whose pages start at or before this rank (entries
         // without pages share their offset with the next one)
@@ -288,63 +303,80 @@ __global__ __launch_bounds__(PT) void k_pages_reserve(PagedCache c, PagedRows r)
 
 hipError_t launch_pages_reserve(const PagedCache& c, const PagedRows& r, hipStream_t st) {
   if (r.n_ent <= 0) return hipSuccess;
-  hipLaunchKernelGGL(k_pages_reserve, dim3(1), dim3(PT), 0, st, c, r);
+  if (few_to_deal(c, r.n_ent)) hipLaunchKernelGGL(k_pages_reserve<PT_FEW>, dim3(1), dim3(PT_FEW), 0, st, c, r);
+  else hipLaunchKernelGGL(k_pages_reserve<PT_MANY>, dim3(1), dim3(PT_MANY), 0, st, c, r);
   return hipGetLastError();
 }
 
-// Fork, first half: who holds what. A pair is made when both sequences are
-// in range, the child was empty, no earlier pair of the call has the same
-// child and the parent is no child of the call. Children are claimed by the
-// lowest pair index in lens (0 for an empty sequence; claims are negative).
-constexpr int CLAIM = 1 << 30;
+// Fork, first half: who holds what. A pair may be made when both sequences are
+// in range and the child was empty; it is made when no such pair before it has
+// the same child, no such pair has its parent as child, and there is a page
+// for its last slots. Pairs go by in rounds of PT; what may be made is told by
+// made while there is more than one round.
+template <int PT>
 __global__ __launch_bounds__(PT) void k_pages_fork(PagedCache c, int n, const int32_t* src, const int32_t* dst,
                                                    int32_t* made) {
-  __shared__ int sList[PT], sSrc[PT], sDst[PT], sFull[PT];
+  __shared__ int sList[PT], sSrc[PT], sFull[PT];
+  __shared__ __attribute__((aligned(16))) int sDst[PT];
   const int tid = threadIdx.x;
-  auto len_of = [&](int s) { return __hip_atomic_load(c.lens + s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
-  for (int i = tid; i < n; i += PT) {
-    const int s = src[i], t = dst[i];
-    if (s < 0 || s >= c.n_seqs || t < 0 || t >= c.n_seqs || s == t || c.held[t] != 0) continue;
-    if (len_of(t) <= 0) atomicMin(c.lens + t, i - CLAIM);
-  }
-  __syncthreads();
-  for (int i = tid; i < n; i += PT) {
-    const int s = src[i], t = dst[i];
+  const unsigned bits0 = free_bits(c, 0);
+  auto may = [&](int s, int t) {
     const bool in = s >= 0 && s < c.n_seqs && t >= 0 && t < c.n_seqs && s != t;
-    made[i] = in && len_of(t) == i - CLAIM && len_of(s) >= 0;
+    const int at = in ? t : 0;
+    return in && (c.held[at] | c.lens[at]) == 0;
+  };
+  // what a pair's children are compared with is the state before the call, so
+  // with several rounds all of it is looked at first
+  if (n > PT) {
+    for (int i = tid; i < n; i += PT) made[i] = may(src[i], dst[i]);
+    __syncthreads();
   }
-  __syncthreads();
+  auto child_of = [&](int i) {
+    if (i >= n) return -1;
+    const int t = dst[i];
+    return (n > PT ? made[i] & 1 : may(src[i], t)) ? t : -1;
+  };
   int pos = 0;
   for (int base = 0; base < n; base += PT) {
     const int i = base + tid;
-    int s = -1, t = -1, len = 0, full = 0, need = 0;
-    if (i < n) {
-      s = src[i];
-      t = dst[i];
-      if (made[i]) {
-        int h = c.held[s];
-        h = h < 0 ? 0 : h > c.max_pages ? c.max_pages : h;
-        const int l = len_of(s), cap = h << c.page_lg;
-        len = l < cap ? l : cap;
-        full = len >> c.page_lg;
-        need = (len & (c.page - 1)) != 0;
-      } else {
-        if (t >= 0 && t < c.n_seqs && len_of(t) == i - CLAIM)
-          __hip_atomic_store(c.lens + t, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        s = t = -1;
+    int s = -1, t = child_of(i), len = 0, full = 0, need = 0;
+    if (i < n) s = src[i];
+    bool ok = t >= 0;
+    for (int b = 0; b < n; b += PT) {
+      __syncthreads();
+      sDst[tid] = b == base ? t : child_of(b + tid);
+      __syncthreads();
+      if (ok) {
+        const int cnt = n - b < PT ? n - b : PT;  // (-1 behind the last)
+#pragma unroll 4
+        for (int j = 0; j < cnt; j += 4) {
+          const int4 o = *(const int4*)(sDst + j);
+          const int q = i - b - j;  // pairs of these four that come before
+          ok = ok && o.x != s && o.y != s && o.z != s && o.w != s && !(o.x == t && q > 0) && !(o.y == t && q > 1) &&
+               !(o.z == t && q > 2) && !(o.w == t && q > 3);
+        }
       }
     }
-    int total;
-    const int rank = block_scan(need, &total);
-    const int got = take_free(c, &pos, total, sList);
-    if (need && rank >= got) {  // no page for its last slots: not made
-      __hip_atomic_store(c.lens + t, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      made[i] = 0;
-      flag(c, PG_OUT);
-      s = t = -1;
+    if (ok) {
+      int h = c.held[s];
+      h = h < 0 ? 0 : h > c.max_pages ? c.max_pages : h;
+      const int l = c.lens[s], cap = h << c.page_lg;
+      len = l < 0 ? 0 : l < cap ? l : cap;
+      full = len >> c.page_lg;
+      need = (len & (c.page - 1)) != 0;
     }
-    if (t >= 0) {
-      __hip_atomic_store(c.lens + t, len, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    int total;
+    const int rank = block_scan<PT>(need, &total);
+    const int got = take_free<PT>(c, bits0, &pos, total, sList);
+    if (need && rank >= got) {  // no page for its last slots
+      ok = false;
+      flag(c, PG_OUT);
+    }
+    // (with several rounds, later ones still ask what may have been made: a
+    // second bit tells what was)
+    if (i < n) made[i] = n > PT ? (t >= 0 ? 1 : 0) | (ok ? 2 : 0) : ok;
+    if (ok) {
+      c.lens[t] = len;
       c.held[t] = full + need;
       if (need) {
         const int p = sList[rank];
@@ -352,58 +384,85 @@ __global__ __launch_bounds__(PT) void k_pages_fork(PagedCache c, int n, const in
         c.refs[p] = 1;
       }
     }
+    __syncthreads();
     sSrc[tid] = s;
-    sDst[tid] = t;
+    sDst[tid] = ok ? t : -1;
     sFull[tid] = full;
     __syncthreads();
-    // the full pages are shared, a wave to a pair
-    for (int j = tid >> 6; j < PT && base + j < n; j += PT / 64) {
+    // the full pages are shared, 16 lanes to a pair
+    for (int j = tid >> 4; j < PT && base + j < n; j += PT / 16) {
       if (sDst[j] < 0) continue;
       const int32_t* from = c.table + (size_t)sSrc[j] * c.max_pages;
       int32_t* to = c.table + (size_t)sDst[j] * c.max_pages;
-      for (int k = tid & 63; k < sFull[j]; k += 64) {
-        const int p = from[k];
-        to[k] = p;
-        if ((unsigned)p < (unsigned)c.n_pages) atomicAdd(c.refs + p, 1);
+      for (int k = tid & 15; k < sFull[j]; k += 64) {
+        int p[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) p[u] = from[k + 16 * u < sFull[j] ? k + 16 * u : k];
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (k + 16 * u < sFull[j]) {
+            to[k + 16 * u] = p[u];
+            if ((unsigned)p[u] < (unsigned)c.n_pages) atomicAdd(c.refs + p[u], 1);
+          }
       }
     }
+  }
+  if (n > PT) {
     __syncthreads();
+    for (int i = tid; i < n; i += PT) made[i] = made[i] >> 1;
   }
 }
 
-// Fork, second half: the used slots of the last page, K and V of one layer
-// and KV head to a workgroup.
+// Fork, second half: the used slots of the last page, K and V of FORK_HEADS
+// heads (of all layers) to a workgroup, so that the descriptors' round trips
+// are paid for more bytes.
+constexpr int FORK_HEADS = 4;
 __global__ __launch_bounds__(256) void k_pages_copy(PagedCache c, const int32_t* src, const int32_t* dst,
-                                                    const int32_t* made, int esz) {
-  const int i = blockIdx.x / (c.layers * c.nkv), lh = blockIdx.x % (c.layers * c.nkv);
-  if (!made[i]) return;
-  const int s = src[i], t = dst[i], len = c.lens[t];
-  const int part = len & (c.page - 1), cap = c.held[t] << c.page_lg;
-  if (!part) return;
-  const int ps = page_of(c, s, len, cap), pt = page_of(c, t, len, cap);
-  if (ps < 0 || pt < 0) return;
-  const size_t from = slot_elem(c, lh / c.nkv, ps, lh % c.nkv, 0) * esz;
-  const size_t to = slot_elem(c, lh / c.nkv, pt, lh % c.nkv, 0) * esz;
-  const int chunks = part * c.hd * esz / 16;
-  const uint4 *ka = (const uint4*)((const char*)c.k + from), *va = (const uint4*)((const char*)c.v + from);
-  uint4 *kb = (uint4*)((char*)c.k + to), *vb = (uint4*)((char*)c.v + to);
+                                                    const int32_t* made, int esz, int groups) {
+  const int i = blockIdx.x / groups, g0 = blockIdx.x % groups * FORK_HEADS;
+  const int ok = made[i], s = src[i], t = dst[i];
+  if (!ok) return;
+  const int len = c.lens[t], part = len & (c.page - 1), col = len >> c.page_lg;
+  if (!part || col >= c.max_pages) return;
+  const int ps = c.table[(size_t)s * c.max_pages + col], pt = c.table[(size_t)t * c.max_pages + col];
+  if ((unsigned)ps >= (unsigned)c.n_pages || (unsigned)pt >= (unsigned)c.n_pages) return;
+  const int chunks = part * c.hd * esz / 16, heads = c.layers * c.nkv;
+  size_t from[FORK_HEADS], to[FORK_HEADS];
+#pragma unroll
+  for (int k = 0; k < FORK_HEADS; ++k) {
+    const int g = g0 + k < heads ? g0 + k : heads - 1;
+    from[k] = slot_elem(c, g / c.nkv, ps, g % c.nkv, 0) * esz;
+    to[k] = slot_elem(c, g / c.nkv, pt, g % c.nkv, 0) * esz;
+  }
   for (int j = threadIdx.x; j < chunks; j += 256) {
-    const uint4 a = ka[j], b = va[j];
-    kb[j] = a;
-    vb[j] = b;
+    u32x4 a[FORK_HEADS], b[FORK_HEADS];
+#pragma unroll
+    for (int k = 0; k < FORK_HEADS; ++k) {
+      a[k] = ((const u32x4*)((const char*)c.k + from[k]))[j];
+      b[k] = ((const u32x4*)((const char*)c.v + from[k]))[j];
+    }
+#pragma unroll
+    for (int k = 0; k < FORK_HEADS; ++k) {
+      if (g0 + k < heads) {
+        __builtin_nontemporal_store(a[k], (u32x4*)((char*)c.k + to[k]) + j);
+        __builtin_nontemporal_store(b[k], (u32x4*)((char*)c.v + to[k]) + j);
+      }
+    }
   }
 }
 
 hipError_t launch_pages_fork(const PagedCache& c, int n, const int32_t* src, const int32_t* dst, int32_t* made,
                              hipStream_t st) {
   if (n <= 0) return hipSuccess;
-  const long long wgs = (long long)n * c.layers * c.nkv;
+  const int groups = (c.layers * c.nkv + FORK_HEADS - 1) / FORK_HEADS;
+  const long long wgs = (long long)n * groups;
   if (wgs > 0x7FFFFFFFll) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(k_pages_fork, dim3(1), dim3(PT), 0, st, c, n, src, dst, made);
+  if (few_to_deal(c, n)) hipLaunchKernelGGL(k_pages_fork<PT_FEW>, dim3(1), dim3(PT_FEW), 0, st, c, n, src, dst, made);
+  else hipLaunchKernelGGL(k_pages_fork<PT_MANY>, dim3(1), dim3(PT_MANY), 0, st, c, n, src, dst, made);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(k_pages_copy, dim3((unsigned)wgs), dim3(256), 0, st, c, src, dst, made,
-                     c.dtype == DT_BF16 ? 2 : 4);
+                     c.dtype == DT_BF16 ? 2 : 4, groups);
   return hipGetLastError();
 }
 
@@ -437,80 +496,17 @@ hipError_t launch_pages_release(const PagedCache& c, int n, const int32_t* seqs,
 // Commit: accepted drafts move together
 // ---------------------------------------------------------------------------
 
-// Whether entry x's accepted list holds ascending drafts of it, by a whole
-// workgroup of 256 (or one wave with W = 64).
-template <int W>
-__device__ __forceinline__ bool kept_fine(const int32_t* kept, int n, int a) {
+// Whether an entry's accepted list holds ascending drafts of its n, as far as
+// thread `me` of `all` looks at it.
+__device__ __forceinline__ bool kept_fine(const int32_t* kept, int n, int a, int me, int all) {
   bool ok = true;
-  for (int j = threadIdx.x % W; j < a; j += W) {
-    const int k = kept[j];
-    ok = ok && k >= 0 && k < n && (j == 0 || k > kept[j - 1]);
+  for (int j = me; j < a; j += all) {
+    const int k = kept[j], b = j ? kept[j - 1] : -1;
+    ok = ok && k >= 0 && k < n && k > b;
   }
-  return W == 64 ? __all(ok) : __syncthreads_and(ok);
+  return ok;
 }
-__device__ __forceinline__ int kept_count(const int32_t* n_kept, int e, int n) {
-  return n_kept ? n_kept[e] : n;
-}
-
-// Draft kept[j] moves to the slot of draft j. A thread owns one 16-byte
-// column of one layer's K or V head and takes the drafts in order: a list
-// ascends, so kept[j] >= j and no draft is written over before it is read
-// (groups are read whole before they are written).
-constexpr int KMOVE = 256;  // drafts whose places are worked out at a time
-__global__ __launch_bounds__(256) void k_pages_move(PagedCache c, PagedRows r, const int32_t* kept,
-                                                    const int32_t* n_kept, int cpr, int esz) {
-  __shared__ int sFrom[KMOVE], sTo[KMOVE], sFromAt[KMOVE], sToAt[KMOVE];
-  const int e = blockIdx.x;
-  const Entry x = entry_of(c, r, e);
-  const int a = kept_count(n_kept, e, x.n);
-  if (x.seq < 0 || a <= 0 || a > x.n) return;
-  const int32_t* list = kept + x.row0;
-  if (!kept_fine<256>(list, x.n, a)) return;
-  const int per = 256 / cpr;
-  const int combo = blockIdx.y * per + (int)threadIdx.x / cpr, chunk = (int)threadIdx.x % cpr;
-  const bool live = (int)threadIdx.x < per * cpr && combo < 2 * c.layers * c.nkv;
-  const int kv = combo & 1, lh = combo >> 1;
-  char* base = (char*)(kv ? c.v : c.k) + (size_t)chunk * 16;
-  const size_t lbase = live ? (size_t)(lh / c.nkv) * c.n_pages : 0;
-  const int head = lh % c.nkv;
-  auto at = [&](int page, int slot) {
-    return (uint4*)(base + ((((lbase + page) * c.nkv + head) * c.page + slot) * c.hd) * esz);
-  };
-  for (int j0 = 0; j0 < a; j0 += KMOVE) {
-    const int cnt = a - j0 < KMOVE ? a - j0 : KMOVE;
-    __syncthreads();
-    if ((int)threadIdx.x < cnt) {
-      const int j = j0 + threadIdx.x, from = x.len + list[j], to = x.len + j;
-      const int pf = page_of(c, x.seq, from, x.cap), pt = page_of(c, x.seq, to, x.cap);
-      sFrom[threadIdx.x] = pt < 0 || from == to ? -1 : pf;
-      sTo[threadIdx.x] = pt;
-      sFromAt[threadIdx.x] = from & (c.page - 1);
-      sToAt[threadIdx.x] = to & (c.page - 1);
-    }
-    __syncthreads();
-    if (!live) continue;
-    for (int j = 0; j < cnt; j += 8) {
-      uint4 v[8];
-#pragma unroll
-      for (int u = 0; u < 8; ++u)
-        if (j + u < cnt && sFrom[j + u] >= 0) v[u] = *at(sFrom[j + u], sFromAt[j + u]);
-#pragma unroll
-      for (int u = 0; u < 8; ++u)
-        if (j + u < cnt && sFrom[j + u] >= 0) *at(sTo[j + u], sToAt[j + u]) = v[u];
-    }
-  }
-}
-
-// The new lengths, a wave to an entry.
-__global__ __launch_bounds__(256) void k_pages_grow(PagedCache c, PagedRows r, const int32_t* kept,
-                                                    const int32_t* n_kept) {
-  const int e = blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (e >= r.n_ent) return;
-  const Entry x = entry_of(c, r, e);
-  const int a = kept_count(n_kept, e, x.n);
-  if (x.seq < 0) return;
-  const bool fine = a >= 0 && a <= x.n && (!kept || kept_fine<64>(kept + x.row0, x.n, a));
-  if ((threadIdx.x & 63) != 0) return;
+__device__ __forceinline__ void grow(const PagedCache& c, const Entry& x, int a, bool fine) {
   if (!fine) {
     flag(c, PG_BAD);
     return;
@@ -520,14 +516,93 @@ __global__ __launch_bounds__(256) void k_pages_grow(PagedCache c, PagedRows r, c
   c.lens[x.seq] = fits ? x.len + a : x.cap;
 }
 
+// Draft kept[j] moves to the slot of draft j. A thread owns one 16-byte
+// column of one layer's K or V head and takes the drafts in order: a list
+// ascends, so kept[j] >= j and no draft is written over before it is read
+// (groups are read whole before they are written). With one workgroup to an
+// entry (gridDim.y 1) it sets the new length as well.
+constexpr int KMOVE = 256;  // drafts whose places are worked out at a time
+__global__ __launch_bounds__(1024) void k_pages_move(PagedCache c, PagedRows r, const int32_t* kept,
+                                                     const int32_t* n_kept, int cpr, int esz) {
+  __shared__ int2 sFrom[KMOVE], sTo[KMOVE];  // page, slot in it
+  __shared__ int sCount;
+  const int e = blockIdx.x, tid = threadIdx.x;
+  const Entry x = entry_of(c, r, e);
+  const int a = n_kept[e];
+  if (x.seq < 0) return;
+  const int32_t* list = kept + x.row0;
+  const bool count = a >= 0 && a <= x.n;
+  const bool fine = __syncthreads_and(count && kept_fine(list, x.n, a, tid, blockDim.x));
+  const int per = blockDim.x / cpr, mine = tid / cpr, chunk = tid % cpr, combos = 2 * c.layers * c.nkv;
+  for (int j0 = 0; fine && j0 < a; j0 += KMOVE) {
+    __syncthreads();
+    if (tid < 64) {  // the first wave lists what moves
+      int n = 0;
+      for (int q = 0; q < KMOVE; q += 64) {
+        const int j = j0 + q + tid;
+        const bool in = j < a;
+        const int from = x.len + (in ? list[j] : 0), to = x.len + j;
+        const int pf = in ? page_of(c, x.seq, from, x.cap) : -1, pt = in ? page_of(c, x.seq, to, x.cap) : -1;
+        const bool go = pf >= 0 && pt >= 0 && from != to;
+        const unsigned long long m = __ballot(go);
+        if (go) {
+          const int k = n + __popcll(m & ((1ull << tid) - 1));
+          sFrom[k] = make_int2(pf, from & (c.page - 1));
+          sTo[k] = make_int2(pt, to & (c.page - 1));
+        }
+        n += __popcll(m);
+      }
+      if (tid == 0) sCount = n;
+    }
+    __syncthreads();
+    const int n = sCount;
+    if (n == 0) continue;
+    for (int co = blockIdx.y * per + mine; mine < per && co < combos; co += gridDim.y * per) {
+      const int lh = co >> 1;
+      char* base = (char*)(co & 1 ? c.v : c.k) + (size_t)chunk * 16;
+      auto at = [&](int2 p) { return (u32x4*)(base + slot_elem(c, lh / c.nkv, p.x, lh % c.nkv, p.y) * esz); };
+      for (int j = 0; j < n; j += 8) {
+        u32x4 v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] = *at(sFrom[j + u < n ? j + u : n - 1]);
+        // (all of them read before any is written)
+#pragma unroll
+        for (int u = 0; u < 8; ++u) asm volatile("" : "+v"(v[u]));
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+          if (j + u < n) *at(sTo[j + u]) = v[u];
+      }
+    }
+  }
+  if (gridDim.y == 1 && tid == 0) grow(c, x, a, fine);
+}
+
+// The new lengths, a wave to an entry.
+__global__ __launch_bounds__(256) void k_pages_grow(PagedCache c, PagedRows r, const int32_t* kept,
+                                                    const int32_t* n_kept) {
+  const int e = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (e >= r.n_ent) return;
+  const Entry x = entry_of(c, r, e);
+  const int a = n_kept ? n_kept[e] : x.n;
+  if (x.seq < 0) return;
+  const bool count = a >= 0 && a <= x.n;
+  const bool fine = __all(count && (!kept || kept_fine(kept + x.row0, x.n, a, lane, 64)));
+  if (lane == 0) grow(c, x, a, fine);
+}
+
 hipError_t launch_pages_commit(const PagedCache& c, const PagedRows& r, const int32_t* kept, const int32_t* n_kept,
                                hipStream_t st) {
   if (r.n_ent <= 0) return hipSuccess;
   if (kept) {
-    const int esz = c.dtype == DT_BF16 ? 2 : 4, cpr = c.hd * esz / 16, per = 256 / cpr;
-    const int combos = 2 * c.layers * c.nkv;
-    const int gy = (combos + per - 1) / per;
-    if (gy > 65535) return hipErrorInvalidValue;
+    const int esz = c.dtype == DT_BF16 ? 2 : 4, cpr = c.hd * esz / 16, combos = 2 * c.layers * c.nkv;
+    // Up to two columns to a thread of 1,024: one workgroup moves an entry's
+    // drafts and sets its length. More: workgroups of 256, and a second launch
+    // when all of them have read the old length.
+    if ((long long)combos * cpr <= 2048) {
+      hipLaunchKernelGGL(k_pages_move, dim3(r.n_ent, 1), dim3(1024), 0, st, c, r, kept, n_kept, cpr, esz);
+      return hipGetLastError();
+    }
+    const int per = 256 / cpr, gy = std::min((combos + per - 1) / per, 65535);
     hipLaunchKernelGGL(k_pages_move, dim3(r.n_ent, gy), dim3(256), 0, st, c, r, kept, n_kept, cpr, esz);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;

@@ -10,6 +10,8 @@ namespace vla {
 namespace pg {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 // A lane's chunk: 16 bytes of a row, VEC elements.
 template <typename T>
@@ -50,6 +52,28 @@ __device__ __forceinline__ uint4 pack(const float (&x)[4]) {
   return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
 }
 
+// Inclusive sum over the wave's lanes, by shifts inside rows of 16 lanes and
+// broadcasts of their last ones (no LDS round trips).
+template <int CTRL, int ROWS>
+__device__ __forceinline__ void scan_step(int& v) {
+  v += __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false);
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ void scan_step(long long& v) {
+  const int lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CTRL, ROWS, 0xf, false);
+  const int hi = __builtin_amdgcn_update_dpp(0, (int)(v >> 32), CTRL, ROWS, 0xf, false);
+  v += (long long)(((unsigned long long)(uint32_t)hi << 32) | (uint32_t)lo);
+}
+template <typename I>
+__device__ __forceinline__ I wave_scan(I v) {
+  scan_step<0x111, 0xf>(v);  // row_shr 1, 2, 4, 8
+  scan_step<0x112, 0xf>(v);
+  scan_step<0x114, 0xf>(v);
+  scan_step<0x118, 0xf>(v);
+  scan_step<0x142, 0xa>(v);  // row_bcast 15 to rows 1 and 3
+  scan_step<0x143, 0xc>(v);  // row_bcast 31 to rows 2 and 3
+  return v;
+}
 // The entry whose rows hold row t, by the whole wave: the largest e <= n with
 // start[e] <= t (start[0] is taken to be; n: t lies behind the last entry).
 // 64 entries a step, so 4,096 entries take two round trips. Every index stays

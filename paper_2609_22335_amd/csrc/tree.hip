@@ -20,8 +20,6 @@ namespace {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 // Pointers into the LDS are typed as such: the compiler must not lose sight of
 // their address space.
 #define LDS_AS __attribute__((address_space(3)))
@@ -137,28 +135,6 @@ struct Geo {
   }
 };
 
-// Inclusive sum over the wave's lanes, by shifts inside rows of 16 lanes and
-// broadcasts of their last ones (no LDS round trips).
-template <int CTRL, int ROWS>
-__device__ __forceinline__ void scan_step(int& v) {
-  v += __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false);
-}
-template <int CTRL, int ROWS>
-__device__ __forceinline__ void scan_step(long long& v) {
-  const int lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CTRL, ROWS, 0xf, false);
-  const int hi = __builtin_amdgcn_update_dpp(0, (int)(v >> 32), CTRL, ROWS, 0xf, false);
-  v += (long long)(((unsigned long long)(uint32_t)hi << 32) | (uint32_t)lo);
-}
-template <typename I>
-__device__ __forceinline__ I wave_scan(I v) {
-  scan_step<0x111, 0xf>(v);  // row_shr 1, 2, 4, 8
-  scan_step<0x112, 0xf>(v);
-  scan_step<0x114, 0xf>(v);
-  scan_step<0x118, 0xf>(v);
-  scan_step<0x142, 0xa>(v);  // row_bcast 15 to rows 1 and 3
-  scan_step<0x143, 0xc>(v);  // row_bcast 31 to rows 2 and 3
-  return v;
-}
 __device__ __forceinline__ long long lane_of(long long v, int i) {
   const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)v, i);
   const uint32_t hi = __builtin_amdgcn_readlane((int)(v >> 32), i);

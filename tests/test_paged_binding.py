@@ -33,6 +33,9 @@ class Dev:
     def numel(self):
         return self._n
 
+    def get_device(self):
+        return self.device.index if self.is_cuda else -1
+
     def stride(self):
         return self._s
 
@@ -108,7 +111,7 @@ def test_calls_refuse_wrong_operands():
     refused("16-byte", V.vla_qk_norm_rope, p, 0, r, rope, Dev((7, 4, 64), BF, stride=(260, 64, 1)), k, k, q)
     refused("row stride", V.vla_qk_norm_rope, p, 0, r, rope, Dev((7, 4, 64), BF, stride=(64, 64, 1)), k, k, q)
     refused("q's row stride", V.vla_qk_norm_rope, p, 0, r, rope, Dev((7, 4, 64), BF, stride=(512, 64, 1)), k, k, q)
-    refused("current device", V.vla_qk_norm_rope, cache(**{n: Dev(s, t, dev="cuda:1") for n, s, t in [
+    refused("the current device is 0", V.vla_qk_norm_rope, cache(**{n: Dev(s, t, dev="cuda:1") for n, s, t in [
         ("k", (2, 10, 2, 16, 64), BF), ("v", (2, 10, 2, 16, 64), BF), ("table", (3, 5), I), ("lens", (3,), I),
         ("held", (3,), I), ("refs", (10,), I), ("status", (1,), I)]}),
         0, V.make_rows(Dev((3,), dev="cuda:1"), 7), V.make_rope_norm(),
@@ -116,7 +119,8 @@ def test_calls_refuse_wrong_operands():
     refused("a tensor is on cuda:1", V.vla_qk_norm_rope, p, 0, r, rope, q, k, k, Dev((7, 4, 64), BF, dev="cuda:1"))
 
     scr = Dev((1 << 20,), torch.uint8)
-    refused("mask must be", V.vla_tree_attention, p, 0, r, q, q, scr, mask=Dev((6, 1)))
+    refused("mask must be", V.vla_tree_attention, p, 0, r, q, q, scr, mask=Dev((7,)))
+    refused("mask holds", V.vla_tree_attention, p, 0, r, q, q, scr, mask=Dev((6, 1)))
     refused("mask must be int32", V.vla_tree_attention, p, 0, r, q, q, scr, mask=Dev((7, 1), torch.int64))
     refused("scratch must be uint8", V.vla_tree_attention, p, 0, r, q, q, Dev((9,), F))
     refused("out must be [7, 4, 64]", V.vla_tree_attention, p, 0, r, q, k, scr)
