@@ -13,19 +13,50 @@ using namespace pg;
 // RMSNorm of queries and keys per head, rotation, store
 // ---------------------------------------------------------------------------
 
+// Rows times groups of heads from which on rows count as many: about what the
+// chip holds in waves.
+constexpr long long MANY_WAVES = 16384;
+
 // y = R(pos) (x / sqrt(mean(x^2) + eps) * g) for every query and key head, K
 // and V into the cache. A wave takes one row and 64 / LPH heads of it at a
 // time; a lane holds the two 16-byte chunks that the rotation pairs (elements
 // i and i + rot / 2), so the rotation needs no other lane and the mean of
 // squares one butterfly over the LPH lanes of a head. Squares, mean, angles
 // and rotation are fp32; the result is rounded once.
-template <typename T, int LPH>
+//
+// Bound by memory: every value is read and written once. A wave's loads are out
+// before it looks for the row's sequence (four dependent round trips), and
+// stores pass the L2 by when there are many rows. With many rows a wave takes
+// three groups of heads, so that its look-ups are paid for more bytes; with
+// few, one, so that more waves share the latency.
+template <typename T, int LPH, int U>
 __global__ __launch_bounds__(256) void k_rope_norm(RopeNormDesc d, int parts) {
   constexpr int VEC = El<T>::VEC, HPW = 64 / LPH;
   const int lane = threadIdx.x & 63;
   const long long w = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int row = (int)(w / parts), part = (int)(w % parts);
   if (row >= d.r.n_rows) return;
+  // the lane's two chunks: rotated pairs first, then the rest in neighbours
+  const int half = d.rot / 2, hd = d.c.hd;
+  const int sub = lane % LPH, hs = lane / LPH, np = hd / (2 * VEC), rp = half / VEC;
+  const bool on = sub < np, turn = sub < rp;
+  const int lo = turn ? sub * VEC : 2 * (rp * VEC) + 2 * (sub - rp) * VEC;
+  const int hi = turn ? lo + half : lo + VEC;
+  const int gq = (d.nq + HPW - 1) / HPW, gk = (d.c.nkv + HPW - 1) / HPW;
+  // group g: 0 queries, 1 keys, 2 values; 3 behind the last
+  auto kind_of = [&](int g) { return g < gq ? 0 : g < gq + gk ? 1 : g < gq + 2 * gk ? 2 : 3; };
+  auto head_of = [&](int g, int kind) { return (kind == 0 ? g : kind == 1 ? g - gq : g - gq - gk) * HPW + hs; };
+  u32x4 ua[U], ub[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int g = part + u * parts, kind = kind_of(g), head = head_of(g, kind);
+    const bool live = on && kind < 3 && head < (kind == 0 ? d.nq : d.c.nkv);
+    const T* src = (const T*)(kind == 0 ? d.q : kind == 1 ? d.k : d.v) +
+                   (size_t)row * (size_t)(kind == 0 ? d.ldq : kind == 1 ? d.ldk : d.ldv);
+    src += live ? (size_t)head * hd : 0;
+    ua[u] = *(const u32x4*)(src + (live ? lo : 0));
+    ub[u] = *(const u32x4*)(src + (live ? hi : 0));
+  }
   const int e = wave_find(d.r.start, d.r.n_ent, row);
   if (e >= d.r.n_ent) return;
   const Entry x = entry_of(d.c, d.r, e);
@@ -33,7 +64,6 @@ __global__ __launch_bounds__(256) void k_rope_norm(RopeNormDesc d, int parts) {
   if (x.seq < 0 || i < 0 || i >= x.n) return;
   const int slot = x.len + i;
   const int pos = d.pos ? d.pos[row] : slot;
-  const int half = d.rot / 2;
   if (d.rot && (pos < 0 || pos >= d.n_pos)) {
     if (part == 0 && lane == 0) flag(d.c, PG_BAD);
     return;
@@ -41,12 +71,6 @@ __global__ __launch_bounds__(256) void k_rope_norm(RopeNormDesc d, int parts) {
   const int page = page_of(d.c, x.seq, slot, x.cap);
   if (page < 0 && part == 0 && lane == 0) flag(d.c, PG_OUT);
   const int at = slot & (d.c.page - 1);
-
-  // the lane's two chunks: rotated pairs first, then the rest in neighbours
-  const int sub = lane % LPH, hs = lane / LPH, np = d.c.hd / (2 * VEC), rp = half / VEC;
-  const bool on = sub < np, turn = sub < rp;
-  const int lo = turn ? sub * VEC : 2 * (rp * VEC) + 2 * (sub - rp) * VEC;
-  const int hi = turn ? lo + half : lo + VEC;
   float cs[VEC], sn[VEC];
 #pragma unroll
   for (int j = 0; j < VEC; ++j) cs[j] = 1.f, sn[j] = 0.f;
@@ -59,37 +83,24 @@ __global__ __launch_bounds__(256) void k_rope_norm(RopeNormDesc d, int parts) {
       *(f32x4*)(sn + j) = *(const f32x4*)(ps + j);
     }
   }
-  const int gq = (d.nq + HPW - 1) / HPW, gk = (d.c.nkv + HPW - 1) / HPW;
-  for (int g = part; g < gq + 2 * gk; g += parts) {
-    const int kind = g < gq ? 0 : g < gq + gk ? 1 : 2;
-    const int head = (kind == 0 ? g : kind == 1 ? g - gq : g - gq - gk) * HPW + hs;
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int g = part + u * parts, kind = kind_of(g), head = head_of(g, kind);
+    if (kind == 3) break;
     const bool live = on && head < (kind == 0 ? d.nq : d.c.nkv);
-    const T* src = (const T*)(kind == 0 ? d.q : kind == 1 ? d.k : d.v) +
-                   (size_t)row * (size_t)(kind == 0 ? d.ldq : kind == 1 ? d.ldk : d.ldv) + (size_t)head * d.c.hd;
-    uint4 ua = make_uint4(0, 0, 0, 0), ub = ua;
-    if (live) {
-      ua = *(const uint4*)(src + lo);
-      ub = *(const uint4*)(src + hi);
-    }
-    T* dst;
-    if (kind == 0) {
-      dst = (T*)d.q_out + (size_t)row * (size_t)d.ldo + (size_t)head * d.c.hd;
-    } else {
-      dst = (T*)(kind == 1 ? d.c.k : d.c.v) + (page < 0 ? 0 : slot_elem(d.c, d.layer, page, head, at));
-    }
-    const bool put = live && (kind == 0 || page >= 0);
     if (kind < 2) {
       float a[VEC], b[VEC];
-      unpack(ua, a);
-      unpack(ub, b);
+      unpack(ua[u], a);
+      unpack(ub[u], b);
       const float* gp = kind == 0 ? d.q_gain : d.k_gain;
       if (gp) {
         float ss = 0.f;
 #pragma unroll
         for (int j = 0; j < VEC; ++j) ss = __builtin_fmaf(a[j], a[j], __builtin_fmaf(b[j], b[j], ss));
+        if (!on) ss = 0.f;
 #pragma unroll
         for (int m = 1; m < LPH; m *= 2) ss += __shfl_xor(ss, m);
-        const float inv = 1.f / sqrtf(ss / d.c.hd + d.eps);
+        const float inv = 1.f / sqrtf(ss / hd + d.eps);
         const float one = d.gain_plus_one ? 1.f : 0.f;
         if (on) {
 #pragma unroll
@@ -102,45 +113,47 @@ __global__ __launch_bounds__(256) void k_rope_norm(RopeNormDesc d, int parts) {
       if (turn) {
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
-          const float u = a[j] * cs[j] - b[j] * sn[j];
+          const float t = a[j] * cs[j] - b[j] * sn[j];
           b[j] = b[j] * cs[j] + a[j] * sn[j];
-          a[j] = u;
+          a[j] = t;
         }
       }
-      ua = pack(a);
-      ub = pack(b);
+      ua[u] = pack(a);
+      ub[u] = pack(b);
     }
-    if (put) {
-      *(uint4*)(dst + lo) = ua;
-      *(uint4*)(dst + hi) = ub;
+    if (!live || (kind > 0 && page < 0)) continue;
+    T* dst = kind == 0 ? (T*)d.q_out + (size_t)row * (size_t)d.ldo + (size_t)head * hd
+                       : (T*)(kind == 1 ? d.c.k : d.c.v) + slot_elem(d.c, d.layer, page, head, at);
+    if (U > 1) {
+      __builtin_nontemporal_store(ua[u], (u32x4*)(dst + lo));
+      __builtin_nontemporal_store(ub[u], (u32x4*)(dst + hi));
+    } else {
+      *(u32x4*)(dst + lo) = ua[u];
+      *(u32x4*)(dst + hi) = ub[u];
     }
   }
 }
 
-template <typename T>
-static hipError_t rope_norm_t(const RopeNormDesc& d, hipStream_t st) {
-  const int np = d.c.hd / (2 * El<T>::VEC);
-  const int lph = np <= 2 ? 2 : np <= 4 ? 4 : np <= 8 ? 8 : 16;
-  const int hpw = 64 / lph;
+template <typename T, int LPH>
+static hipError_t rope_norm_l(const RopeNormDesc& d, hipStream_t st) {
+  const int hpw = 64 / LPH;
   const int groups = (d.nq + hpw - 1) / hpw + 2 * ((d.c.nkv + hpw - 1) / hpw);
-  const int parts = groups;
+  const bool many = (long long)d.r.n_rows * groups > MANY_WAVES;
+  const int parts = many ? (groups + 2) / 3 : groups;
   const long long wgs = ((long long)d.r.n_rows * parts + 3) / 4;
   if (wgs > 0x7FFFFFFFll) return hipErrorInvalidValue;
-  const dim3 grid((unsigned)wgs), block(256);
-  switch (lph) {
-    case 2:
-      hipLaunchKernelGGL((k_rope_norm<T, 2>), grid, block, 0, st, d, parts);
-      break;
-    case 4:
-      hipLaunchKernelGGL((k_rope_norm<T, 4>), grid, block, 0, st, d, parts);
-      break;
-    case 8:
-      hipLaunchKernelGGL((k_rope_norm<T, 8>), grid, block, 0, st, d, parts);
-      break;
-    default:
-      hipLaunchKernelGGL((k_rope_norm<T, 16>), grid, block, 0, st, d, parts);
-  }
+  if (many) hipLaunchKernelGGL((k_rope_norm<T, LPH, 3>), dim3((unsigned)wgs), dim3(256), 0, st, d, parts);
+  else hipLaunchKernelGGL((k_rope_norm<T, LPH, 1>), dim3((unsigned)wgs), dim3(256), 0, st, d, parts);
   return hipGetLastError();
+}
+
+template <typename T>
+static hipError_t rope_norm_t(const RopeNormDesc& d, hipStream_t st) {
+  const int np = d.c.hd / (2 * El<T>::VEC);  // lanes that a head keeps busy
+  return np <= 2   ? rope_norm_l<T, 2>(d, st)
+         : np <= 4 ? rope_norm_l<T, 4>(d, st)
+         : np <= 8 ? rope_norm_l<T, 8>(d, st)
+                   : rope_norm_l<T, 16>(d, st);
 }
 
 hipError_t launch_rope_norm(const RopeNormDesc& d, hipStream_t st) {
@@ -570,7 +583,7 @@ __global__ __launch_bounds__(1024) void k_pages_move(PagedCache c, PagedRows r, 
         for (int u = 0; u < 8; ++u) asm volatile("" : "+v"(v[u]));
 #pragma unroll
         for (int u = 0; u < 8; ++u)
-          if (j + u < n) *at(sTo[j + u]) = v[u];
+          if (j + u < n) __builtin_nontemporal_store(v[u], at(sTo[j + u]));
       }
     }
   }

@@ -31,7 +31,7 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ uint32_t bf2(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{lo, hi}), bf16x2));
 }
-__device__ __forceinline__ void unpack(uint4 u, float (&x)[8]) {
+__device__ __forceinline__ void unpack(u32x4 u, float (&x)[8]) {
   const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -39,17 +39,17 @@ __device__ __forceinline__ void unpack(uint4 u, float (&x)[8]) {
     x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
   }
 }
-__device__ __forceinline__ void unpack(uint4 u, float (&x)[4]) {
+__device__ __forceinline__ void unpack(u32x4 u, float (&x)[4]) {
   x[0] = __uint_as_float(u.x);
   x[1] = __uint_as_float(u.y);
   x[2] = __uint_as_float(u.z);
   x[3] = __uint_as_float(u.w);
 }
-__device__ __forceinline__ uint4 pack(const float (&x)[8]) {
-  return make_uint4(bf2(x[0], x[1]), bf2(x[2], x[3]), bf2(x[4], x[5]), bf2(x[6], x[7]));
+__device__ __forceinline__ u32x4 pack(const float (&x)[8]) {
+  return u32x4{bf2(x[0], x[1]), bf2(x[2], x[3]), bf2(x[4], x[5]), bf2(x[6], x[7])};
 }
-__device__ __forceinline__ uint4 pack(const float (&x)[4]) {
-  return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+__device__ __forceinline__ u32x4 pack(const float (&x)[4]) {
+  return u32x4{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])};
 }
 
 // Inclusive sum over the wave's lanes, by shifts inside rows of 16 lanes and
