@@ -13,9 +13,11 @@ using namespace pg;
 // RMSNorm of queries and keys per head, rotation, store
 // ---------------------------------------------------------------------------
 
-// Rows times groups of heads from which on rows count as many: about what the
-// chip holds in waves.
-constexpr long long MANY_WAVES = 16384;
+// Rows times groups of heads above which a wave takes three groups. 32 query
+// heads and 8 KV heads of 128: 512 rows (3,072 groups) 5.0 us with one and 5.5
+// with three, 1,024 rows 7.7 and 6.4, 8,192 rows 47 and 33; 8 and 1 of 256: 512
+// rows (2,048) 4.1 and 4.8, 1,024 rows 5.4 and 5.2.
+constexpr long long MANY_WAVES = 4096;
 
 // y = R(pos) (x / sqrt(mean(x^2) + eps) * g) for every query and key head, K
 // and V into the cache. A wave takes one row and 64 / LPH heads of it at a
@@ -167,10 +169,12 @@ hipError_t launch_rope_norm(const RopeNormDesc& d, hipStream_t st) {
 // cache's state alone. One workgroup deals: the work is a scan of refs.
 // ---------------------------------------------------------------------------
 
-// Threads of the dealing workgroup: few for few sequences and a small pool
-// (its barriers are most of the call), many where refs take long to scan.
+// Threads of the dealing workgroup: few while one to an entry are enough and
+// the pool is small (barriers are most of the call: release, fork and reserve
+// of 16 pairs 15.8 us with 256 threads and 17.3 with 1,024, of 250 pairs 51.1
+// and 51.8), many where refs take long to scan.
 constexpr int PT_FEW = 256, PT_MANY = 1024;
-inline bool few_to_deal(const PagedCache& c, int n) { return n <= 16 && c.n_pages <= 4 * 8 * PT_FEW; }
+inline bool few_to_deal(const PagedCache& c, int n) { return n <= PT_FEW && c.n_pages <= 4 * 8 * PT_FEW; }
 
 // Exclusive prefix of x over the workgroup, and the total.
 template <int PT>
@@ -608,10 +612,11 @@ hipError_t launch_pages_commit(const PagedCache& c, const PagedRows& r, const in
   if (r.n_ent <= 0) return hipSuccess;
   if (kept) {
     const int esz = c.dtype == DT_BF16 ? 2 : 4, cpr = c.hd * esz / 16, combos = 2 * c.layers * c.nkv;
-    // Up to two columns to a thread of 1,024: one workgroup moves an entry's
+    // About a column to each of 1,024 threads: one workgroup moves an entry's
     // drafts and sets its length. More: workgroups of 256, and a second launch
-    // when all of them have read the old length.
-    if ((long long)combos * cpr <= 2048) {
+    // when all of them have read the old length (eight entries of 512 columns
+    // 4.3 us against 5.6, 1,152 columns 5.5 / 5.7, 2,048 columns 7.1 / 5.7).
+    if ((long long)combos * cpr <= 1280) {
       hipLaunchKernelGGL(k_pages_move, dim3(r.n_ent, 1), dim3(1024), 0, st, c, r, kept, n_kept, cpr, esz);
       return hipGetLastError();
     }

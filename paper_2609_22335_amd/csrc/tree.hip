@@ -122,16 +122,18 @@ struct Geo {
     return (int)floor_sum(rt, group * unit, BM, BM - 1 + group * (len + unit));
   }
   __device__ __forceinline__ int sum() const { return tiles == 0 ? 0 : before(tiles - 1) + units(tiles - 1); }
-  // the tile that holds unit u of the head's
+  // the tile that holds unit u of the head's: units grow by a line, their sum
+  // by a parabola, whose root is close
   __device__ __forceinline__ int find(int u) const {
     if (flat) return u / all();
-    int lo = 0, hi = tiles - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) / 2;
-      if (before(mid) <= u) lo = mid;
-      else hi = mid - 1;
-    }
-    return lo;
+    if (tiles <= 1) return 0;
+    const float first = (float)units(0), grow = (float)(units(tiles - 1) - units(0)) / (float)(tiles - 1);
+    const float h = first - 0.5f * grow;
+    int rt = grow > 0.f ? (int)((sqrtf(h * h + 2.f * grow * (float)u) - h) / grow) : (int)((float)u / first);
+    rt = rt < 0 ? 0 : rt > tiles - 1 ? tiles - 1 : rt;
+    while (rt > 0 && before(rt) > u) --rt;
+    while (rt + 1 < tiles && before(rt + 1) <= u) ++rt;
+    return rt;
   }
 };
 
@@ -231,11 +233,16 @@ __device__ __forceinline__ Tile deal(Run& r, bool first, int w) {
   const long long at = r.u - (base + lane_of(incl, el) - lane_of(units, el));
   g.set(a.group, causal, x, BN * per);
   Tile t{};
-  // (a head's units fit 31 bits; most entries' do as well)
-  t.head = at >> 31 ? (int)(at / persum) : (int)((uint32_t)at / (uint32_t)persum);
+  // (a head's units fit 31 bits; most entries' do as well. Divisions are long,
+  // and a short call waits for each: one head and one tile need none.)
+  t.head = nkv == 1 ? 0 : at >> 31 ? (int)(at / persum) : (int)((uint32_t)at / (uint32_t)persum);
   const int rem = (int)(at - (long long)t.head * persum);
-  t.rt = g.find(rem);
-  const int u0 = rem - g.before(t.rt), nu = g.units(t.rt);
+  int u0 = rem, nu = persum;
+  if (g.tiles > 1) {
+    t.rt = g.find(rem);
+    u0 = rem - g.before(t.rt);
+    nu = g.units(t.rt);
+  }
   const int u1 = (int)(nu - u0 < r.u_end - r.u ? nu : u0 + (r.u_end - r.u));
   t.seq = x.seq;
   t.row0 = x.row0;
@@ -604,14 +611,15 @@ __device__ __forceinline__ void load_query(const Tile& t, int mc, u32x4 (&qf)[NQ
   }
 }
 
-// Four results (d .. d + 3) of row mm of the tile, to the output.
+// Where row mm of the tile goes, and four results of it.
 template <typename T>
-__device__ __forceinline__ void put_out(const Args& a, const Tile& t, int mm, int d, float inv, const float (&v)[4]) {
-  if (mm >= t.M || d >= a.c.hd) return;
+__device__ __forceinline__ T* out_row(const Args& a, const Tile& t, int mm) {
   const int tk = mm / t.group;
-  T* dst = (T*)a.out + (size_t)(t.row0 + tk) * (size_t)a.ldo +
-           (size_t)(t.head * t.group + (mm - tk * t.group)) * a.c.hd + d;
-  if constexpr (sizeof(T) == 2) *(uint2*)dst = make_uint2(bf2(v[0] * inv, v[1] * inv), bf2(v[2] * inv, v[3] * inv));
+  return (T*)a.out + (size_t)(t.row0 + tk) * (size_t)a.ldo + (size_t)(t.head * t.group + (mm - tk * t.group)) * a.c.hd;
+}
+template <typename T>
+__device__ __forceinline__ void put4(T* dst, float inv, const float (&v)[4]) {
+  if constexpr (sizeof(T) == 2) *(u32x2*)dst = u32x2{bf2(v[0] * inv, v[1] * inv), bf2(v[2] * inv, v[3] * inv)};
   else *(f32x4*)dst = f32x4{v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv};
 }
 __device__ __forceinline__ float inverse(float l) { return l > 0.f || l != l ? 1.f / l : 0.f; }
@@ -763,7 +771,7 @@ __global__ __launch_bounds__(256, (many_waves<T, HDP>())) void k_tree_few(Args a
         den = __builtin_fmaf(f, sL[k][lm], den);
       }
       if (t.whole) {
-        put_out<T>(z, t, t.rt * BM + lm, col, inverse(den), v);
+        if (col < z.c.hd) put4<T>(out_row<T>(z, t, t.rt * BM + lm) + col, inverse(den), v);
       } else {
         float* pm = z.part + 2ll * z.wgs * BM * HDP + (size_t)slot * BM * 2;
         *(f32x4*)(z.part + ((size_t)slot * BM + lm) * HDP + col) = f32x4{v[0], v[1], v[2], v[3]};
@@ -773,11 +781,13 @@ __global__ __launch_bounds__(256, (many_waves<T, HDP>())) void k_tree_few(Args a
   });
 }
 
-// Keys of a block of the many-row kernel: two tiles of 32 while two
-// workgroups' rings fit on a CU.
+// Keys of a block of the many-row kernel: two tiles of 32 to a barrier; one
+// where a block's products are long (fp32, wide heads), so that there are
+// more blocks to deal out (trees of 40 rows in fp32: 19.6 us against 23.5; of
+// 47 rows in bf16 at head dim 256: 34.2 against 33.1).
 template <typename T, int HDP>
 constexpr int many_keys() {
-  return HDP * (int)sizeof(T) <= 256 ? 64 : 32;
+  return sizeof(T) == 2 || HDP <= 64 ? 64 : 32;
 }
 
 // Many rows to a sequence: tiles of 128 rows, 32 to a wave, bound by the
@@ -867,15 +877,21 @@ __global__ __launch_bounds__(256, (many_waves<T, HDP>())) void k_tree_many(Args 
     const Args& z = fresh();
     float* po = z.part + (size_t)slot * BM * HDP;
     float* pm = z.part + 2ll * z.wgs * BM * HDP + (size_t)slot * BM * 2;
-    const float inv = inverse(l);
     if (t.whole) {
+      const float inv = inverse(l);
+      T* dst = out_row<T>(z, t, mc) + 4 * h;
+      const int hd = z.c.hd;
+      if (m < t.M) {
 #pragma unroll
-      for (int dt = 0; dt < NDT; ++dt)
+        for (int dt = 0; dt < NDT; ++dt) {
+          if (32 * dt >= hd) break;
 #pragma unroll
-        for (int j4 = 0; j4 < 4; ++j4) {
-          const float v[4] = {o[dt][4 * j4], o[dt][4 * j4 + 1], o[dt][4 * j4 + 2], o[dt][4 * j4 + 3]};
-          put_out<T>(z, t, m, 32 * dt + 8 * j4 + 4 * h, inv, v);
+          for (int j4 = 0; j4 < 4; ++j4) {
+            const float v[4] = {o[dt][4 * j4], o[dt][4 * j4 + 1], o[dt][4 * j4 + 2], o[dt][4 * j4 + 3]};
+            put4<T>(dst + 32 * dt + 8 * j4, inv, v);
+          }
         }
+      }
     } else if (m < t.M) {
 #pragma unroll
       for (int dt = 0; dt < NDT; ++dt)
@@ -1042,11 +1058,16 @@ __global__ __launch_bounds__(256) void k_tree_join(Args a) {
 
 int pad_hd(int dtype, int hd) { return hd <= 64 ? 64 : hd <= 128 ? 128 : 256; }
 
-// Many rows to a sequence (on average more than two tiles of 32): tiles of
-// 128 rows, whose waves share K and V.
+// Many rows to a sequence (on average more than one tile of 128): tiles of 128
+// rows, whose waves share K and V. Below that the two are close, and tiles of
+// 32 keep more of the probabilities: eight caches of 4,000 slots at head dim
+// 128, 8 query heads on one KV head, 64 rows 22.2 us against 20.3, 128 rows 23.7
+// against 23.1, 192 rows 27.6 against 25.4; two of 30,000 slots 26.2 / 30.5,
+// 33.3 / 32.4, 37.4 / 31.7; eight of 2,000 at head dim 256 25.5 / 25.0, 25.7 /
+// 29.0, 29.2 / 26.4; of 1,000 in fp32 21.2 / 23.4, 26.2 / 26.6, 27.2 / 29.4.
 int tile_rows(const TreeAttnDesc& d) {
   const long long rows = (long long)d.r.n_rows * (d.nq / d.c.nkv);
-  return rows > 64ll * d.r.n_ent ? 128 : 32;
+  return rows > 128ll * d.r.n_ent ? 128 : 32;
 }
 // Workgroups, each with a run of blocks: as many as the CUs hold.
 int tree_wgs(const TreeAttnDesc& d) {

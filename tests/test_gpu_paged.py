@@ -13,7 +13,7 @@ of it; fp32 sums of n terms by n 2^-24 of the sum of their magnitudes.
   of its magnitude in the exponent), so a weight by a factor of e^(2 ds); the
   two sums over n keys add (n + 16) 2^-24. Every such error moves the result by
   at most itself times sum p |v| (numerator) and |o| <= sum p |v|
-  (denominator). bf16 with more than 64 rows a sequence (on average) rounds the
+  (denominator). bf16 with more than 128 rows of a KV head to a sequence (on average) rounds the
   probabilities once: 2^-8 in both sums; with fewer they are kept to 2^-16.
   Then one rounding of the output.
 """
@@ -241,7 +241,7 @@ def expect(m, T, layer, order, start, counts, q, bits, scale, mean_rows, see_all
                 for g in range(group):
                     o, mag, ds = U.attention_row(q[a + i, h * group + g], k, v, see, scale)
                     ds *= (hd + 4) * 2.0 ** -24
-                    p = 0.0 if T is T32 else 2.0 ** -8 if mean_rows * group > 64 else 2.0 ** -16
+                    p = 0.0 if T is T32 else 2.0 ** -8 if mean_rows * group > 128 else 2.0 ** -16
                     rel = np.expm1(2 * ds) + (end + 16) * 2.0 ** -24 + p
                     want[a + i, h * group + g] = o
                     tol[a + i, h * group + g] = rel * (mag + np.abs(o)) + HALF[T] * np.abs(o) * (1 + rel) + 1e-38
