@@ -3420,7 +3420,7 @@ static int tree_desc(const vla_pages* p, const vla_rows* rows, int32_t layer, in
     return fail(VLA_EUNSUPPORTED, "more than 2^29 query rows or grouped slots, or 2^31 blocks of scores, to a KV head");
   d->layer = layer;
   d->nq = nq;
-  return device_cus(&d->cus);
+  return VLA_OK;
 }
 
 int vla_tree_attention_scratch(const vla_pages* p, const vla_rows* rows, int32_t nq, int64_t* bytes) {
@@ -3428,6 +3428,7 @@ int vla_tree_attention_scratch(const vla_pages* p, const vla_rows* rows, int32_t
     if (!bytes) return fail(VLA_EINVAL, "bytes is NULL");
     TreeAttnDesc d;
     VLA_TRY(tree_desc(p, rows, 0, nq, &d));
+    VLA_TRY(device_cus(&d.cus));
     *bytes = (int64_t)tree_attn_scratch(d);
     return VLA_OK;
   })
@@ -3444,6 +3445,8 @@ int vla_tree_attention(const vla_pages* p, int32_t layer, const vla_rows* rows, 
     if (d.r.n_rows == 0 || d.r.n_ent == 0) return VLA_OK;  // nothing is read or written
     VLA_TRY(paged_operand(d.c, "q", q, ldq, nq));
     VLA_TRY(paged_operand(d.c, "out", out, ldo, nq));
+    if (out == q) return fail(VLA_EINVAL, "out must not be q");
+    VLA_TRY(device_cus(&d.cus));
     const size_t need = tree_attn_scratch(d);
     if (!scratch || !aligned16(scratch) || scratch_bytes < 0 || (size_t)scratch_bytes < need)
       return fail(VLA_EINVAL, "scratch: needs " + std::to_string(need) + " bytes, 16-byte aligned");

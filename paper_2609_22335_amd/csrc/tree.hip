@@ -160,6 +160,7 @@ struct Tile {
 struct Run {
   long long u, u_end;  // this run's next and last unit
   long long quota;     // units of a run
+  int w;               // this run (behind the last: none)
   int per;             // blocks of a unit
 };
 
@@ -170,10 +171,10 @@ struct Run {
 // workgroups), a unit is as many blocks of one tile as give every workgroup at
 // most one unit: a run that crossed into another tile would start twice for
 // a few blocks each. deal() finds the tile at r.u; with `first` set it works
-// out the run of workgroup w before. Every wave does so for itself; lanes hold
+// out the workgroup's run before. Every wave does so for itself; lanes hold
 // 64 entries at a time.
 template <int BM, int BN>
-__device__ __forceinline__ Tile deal(Run& r, bool first, int w) {
+__device__ __forceinline__ Tile deal(Run& r, bool first) {
   const Args& a = fresh();
   const int lane = threadIdx.x & 63, n_ent = a.r.n_ent, nkv = a.c.nkv;
   const bool causal = a.mask == nullptr;
@@ -184,7 +185,8 @@ __device__ __forceinline__ Tile deal(Run& r, bool first, int w) {
   // One loop over the entries, in passes: 0 counts blocks and tiles, 1 counts
   // units of several blocks, 2 finds the unit. (One copy of the code: what a
   // short call waits for most is instructions.)
-  int pass = first ? 0 : 2, tiles = 0, per = first ? 1 : r.per;
+  int pass = first ? 0 : 2, per = first ? 1 : r.per;
+  long long tiles = 0;
   for (int c0 = 0;;) {
     if (c0 == 0 ? pass == 0 || pass == 2 : true) {
       x = Entry{-1, 0, 0, 0, 0};
@@ -202,12 +204,12 @@ __device__ __forceinline__ Tile deal(Run& r, bool first, int w) {
       continue;
     }
     total += all;
-    if (pass == 0) tiles += __builtin_amdgcn_readlane(wave_scan(g.tiles), 63) * nkv;
+    if (pass == 0) tiles += (long long)__builtin_amdgcn_readlane(wave_scan(g.tiles), 63) * nkv;
     c0 += 64;
     if (c0 < n_ent) continue;
     c0 = 0;
     if (pass == 0 && 2 * tiles <= a.wgs) {
-      per = (int)ceil_div(total, a.wgs - tiles);
+      per = (int)ceil_div(total, a.wgs - (int)tiles);
       pass = 1;
       if (per > 1) {
         total = 0;
@@ -217,7 +219,14 @@ __device__ __forceinline__ Tile deal(Run& r, bool first, int w) {
     }
     r.per = per;
     r.quota = pass == 1 || total <= a.wgs ? 1 : ceil_div(total, a.wgs);
-    r.u = w * r.quota;
+    // Workgroups go round the eight XCDs: each XCD takes an eighth of the runs,
+    // consecutive ones, so that its L2 serves K and V of neighbouring tiles
+    // once (and the join what was written there), and few runs still use every
+    // XCD's share of the memory.
+    const int runs = r.quota == 1 ? (int)total : (int)ceil_div(total, (int)r.quota), share = (runs + 7) >> 3;
+    const int i = (int)(blockIdx.x >> 3);
+    r.w = i < share ? (int)(blockIdx.x & 7) * share + i : a.wgs;
+    r.u = r.w * r.quota;
     r.u_end = r.u + r.quota < total ? r.u + r.quota : total;
     if (r.u >= r.u_end) return Tile{};
     if (n_ent <= 64) break;
@@ -255,7 +264,7 @@ __device__ __forceinline__ Tile deal(Run& r, bool first, int w) {
   const int nb = t.kend > 0 ? (t.kend + BN - 1) / BN : 1;
   t.b1 = u1 * per < nb ? u1 * per : nb;
   t.whole = u0 == 0 && u1 == nu;
-  t.parts = t.whole || u0 > 0 ? 0 : (int)(r.quota == 1 ? r.u + nu - 1 : (r.u + nu - 1) / r.quota) - w + 1;
+  t.parts = t.whole || u0 > 0 ? 0 : (int)(r.quota == 1 ? r.u + nu - 1 : (r.u + nu - 1) / r.quota) - r.w + 1;
   r.u += u1 - u0;
   return t;
 }
@@ -624,33 +633,27 @@ __device__ __forceinline__ void put4(T* dst, float inv, const float (&v)[4]) {
 }
 __device__ __forceinline__ float inverse(float l) { return l > 0.f || l != l ? 1.f / l : 0.f; }
 
-// The run of this workgroup: consecutive runs on one XCD (workgroups go round
-// the eight), so that its L2 serves K and V of neighbouring tiles once, and
-// the joins what was written there.
-__device__ __forceinline__ int run_of(int wgs) { return (int)(blockIdx.x & 7) * (wgs >> 3) + (int)(blockIdx.x >> 3); }
-
 // The workgroup's run of blocks: calls f(tile, slot) for each of its tiles,
 // slot being where a shared tile's part goes; what other workgroups hold of the last one is written down for the
 // join.
 template <int BM, int BN, typename F>
 __device__ __forceinline__ void for_tiles(int wgs, F&& f) {
-  const int w = run_of(wgs);
   Run r;
-  Tile t = deal<BM, BN>(r, true, w);
+  Tile t = deal<BM, BN>(r, true);
   int4 desc = make_int4(0, 0, 0, 0), more = desc;
   while (t.b1 > t.b0) {
     if (t.parts) {
       desc = make_int4(t.parts, t.row0, t.head * t.group, t.rt);
-      more = make_int4(t.M, t.group, 0, 0);
+      more = make_int4(t.M, t.group, r.w, 0);
     }
-    f(t, 2 * w + (t.b0 == 0 ? 1 : 0));
+    f(t, 2 * r.w + (t.b0 == 0 ? 1 : 0));
     if (r.u >= r.u_end) break;
     wait_vm<0>();  // no store of this tile in the next one's counts
     __syncthreads();
-    t = deal<BM, BN>(r, false, w);
+    t = deal<BM, BN>(r, false);
   }
   if (threadIdx.x == 0) {
-    int4* to = fresh().desc + 2 * w;
+    int4* to = fresh().desc + 2 * ((int)(blockIdx.x & 7) * (wgs >> 3) + (int)(blockIdx.x >> 3));  // by XCD
     to[0] = desc;
     to[1] = more;
   }
@@ -971,18 +974,20 @@ __global__ __launch_bounds__(256) void k_tree_join(Args a) {
   if (tid == 0) sPre[0] = 0;
   __syncthreads();
   const float* pm = a.part + 2ll * a.wgs * BM * HDP;
-  for (int take = blockIdx.x; take < before; take += gridDim.x) {
-    int lo = 0, hi = a.wgs - 1;  // the run whose tile it is of
+  // what workgroups of this XCD wrote
+  const int xcd = blockIdx.x & 7, last = sPre[(xcd + 1) * (a.wgs >> 3)];
+  for (int take = sPre[xcd * (a.wgs >> 3)] + (blockIdx.x >> 3); take < last; take += gridDim.x >> 3) {
+    int lo = 0, hi = a.wgs - 1;  // the descriptor of its tile
     while (lo < hi) {
       const int mid = (lo + hi + 1) / 2;
       if (sPre[mid] <= take) lo = mid;
       else hi = mid - 1;
     }
-    const int w = uni(lo);
-    const int4 d = a.desc[2 * w], e = a.desc[2 * w + 1];
-    const int n = d.x, M = e.x, group = e.y, m0 = d.w * BM;
+    const int k = uni(lo);
+    const int4 d = a.desc[2 * k], e = a.desc[2 * k + 1];
+    const int n = d.x, M = e.x, group = e.y, w = e.z, m0 = d.w * BM;
     const bool own = n <= 4;  // a piece to each wave
-    const int piece = own ? (take - sPre[w]) * 4 + wv : take - sPre[w];
+    const int piece = own ? (take - sPre[k]) * 4 + wv : take - sPre[k];
     const int nd = (hd + 31) / 32, rg = MANY ? piece / nd : 0, dt = MANY ? piece % nd : 0;
     const int lm = MANY ? rg * 32 + l32 : piece;  // the lane's row of the tile
     // (rows behind the last have nothing written: theirs is not used)
@@ -1085,7 +1090,7 @@ hipError_t run(const TreeAttnDesc& d, const Args& a, hipStream_t st) {
   if (e != hipSuccess) return e;
   // (at most as many as there can be pieces to take)
   const long long tiles = ((long long)d.r.n_rows * a.group / rows + d.r.n_ent) * d.c.nkv;
-  const int joins = (int)std::min({(long long)4 * d.cus, 1024ll, tiles * (rows == 32 ? 32 : HDP / 8)});
+  const int joins = (int)std::min({(long long)4 * d.cus / 8, 128ll, (tiles * (rows == 32 ? 32 : HDP / 8) + 7) / 8}) * 8;
   if (rows == 32) hipLaunchKernelGGL((k_tree_join<T, HDP, 32>), dim3(joins), dim3(256), 0, st, a);
   else hipLaunchKernelGGL((k_tree_join<T, HDP, 128>), dim3(joins), dim3(256), 0, st, a);
   return hipGetLastError();

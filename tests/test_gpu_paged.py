@@ -219,32 +219,44 @@ def pack(bits):
     return w.astype(np.uint32).view(np.int32)
 
 
-def expect(m, T, layer, order, start, counts, q, bits, scale, mean_rows, see_all=None):
-    """Results and tolerances of every row (rows of nobody: None)."""
-    n_rows, nq, hd = q.shape
-    group = nq // m.dims[2]
+def expect(m, T, layer, order, start, counts, q, bits, scale, mean_rows):
+    """Results and tolerances of every row (rows of nobody: nan), in 64 bits."""
+    nq, hd = q.shape[1:]
+    nkv = m.dims[2]
+    group = nq // nkv
     want, tol = np.full(q.shape, np.nan), np.full(q.shape, np.nan)
     for s, a, c in zip(order, start, counts):
-        if s < 0:
+        if s < 0 or c == 0:
             continue
         L, cap = int(m.lens[s]), int(m.held[s]) * m.page
         end = min(L + c, cap)
-        slots = [m.where(s, i) for i in range(end)]
-        for h in range(m.dims[2]):
-            k = np.array([m.k[layer, p, h, at] for p, at in slots]).reshape(end, hd)
-            v = np.array([m.v[layer, p, h, at] for p, at in slots]).reshape(end, hd)
-            for i in range(c):
-                see = np.zeros(end, bool)
-                see[:min(L, end)] = True
-                j = np.arange(L, end) - L
-                see[L:] = (j <= i) if bits is None else (j < bits.shape[1]) & bits[a + i][np.minimum(j, bits.shape[1] - 1)]
-                for g in range(group):
-                    o, mag, ds = U.attention_row(q[a + i, h * group + g], k, v, see, scale)
-                    ds *= (hd + 4) * 2.0 ** -24
-                    p = 0.0 if T is T32 else 2.0 ** -8 if mean_rows * group > 128 else 2.0 ** -16
-                    rel = np.expm1(2 * ds) + (end + 16) * 2.0 ** -24 + p
-                    want[a + i, h * group + g] = o
-                    tol[a + i, h * group + g] = rel * (mag + np.abs(o)) + HALF[T] * np.abs(o) * (1 + rel) + 1e-38
+        pages, places = m.table[s][np.arange(end) // m.page], np.arange(end) % m.page
+        see = np.zeros((c, end), bool)
+        see[:, :min(L, end)] = True
+        j = np.arange(L, end) - L
+        if bits is None:
+            see[:, L:] = j[None, :] <= np.arange(c)[:, None]
+        else:
+            see[:, L:] = (j < bits.shape[1]) & bits[a:a + c][:, np.minimum(j, bits.shape[1] - 1)]
+        any_seen = see.any(1)[:, None, None]
+        see = see[:, None, :]  # [rows, heads of the group, keys]
+        for h in range(nkv):
+            k, v = m.k[layer, pages, h, places], m.v[layer, pages, h, places]
+            x = q[a:a + c, h * group:(h + 1) * group]
+            # hidden keys' and values' contents do not count
+            shown = see[:, 0].any(0)
+            k, v = np.where(shown[:, None], k, 0), np.where(shown[:, None], v, 0)
+            score = np.where(see, np.matmul(x, k.T) * scale, -np.inf)
+            top = np.where(any_seen, score.max(-1, keepdims=True, initial=-np.inf), 0)
+            p = np.exp(score - top)
+            p /= np.where(any_seen, p.sum(-1, keepdims=True), 1)
+            o, mag = np.matmul(p, v), np.matmul(p, np.abs(v))
+            ds = np.where(see, np.matmul(np.abs(x), np.abs(k).T), 0).max(-1, initial=0)[..., None] * scale
+            ds = ds * (hd + 4) * 2.0 ** -24
+            one = 0.0 if T is T32 else 2.0 ** -8 if mean_rows * group > 128 else 2.0 ** -16
+            rel = np.expm1(2 * ds) + (end + 16) * 2.0 ** -24 + one
+            want[a:a + c, h * group:(h + 1) * group] = o
+            tol[a:a + c, h * group:(h + 1) * group] = rel * (mag + np.abs(o)) + HALF[T] * np.abs(o) * (1 + rel) + 1e-38
     return want, tol
 
 
@@ -387,6 +399,83 @@ def test_long_uneven_sequences_are_shared_out(V):
         want, tol = expect(m, T, 0, list(range(len(lens))), start, rows, q, None, hd ** -0.5, n / len(rows))
         assert np.all(np.abs(vals(outs[0]) - want) <= tol)
         assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+
+
+@pytest.mark.parametrize("T,hd,nq,nkv,lens,rows", [
+    (T16, 64, 28, 4, [500, 3, 70], [1100, 900, 40]),    # seven heads to a KV head: tiles that part tokens
+    (T16, 128, 32, 8, [0, 900], [1100, 60]),
+    (T16, 256, 24, 8, [100, 0], [500, 700]),
+    (T32, 64, 16, 16, [40, 600], [900, 1100]),
+    (T16, 64, 8, 8, [int(x) for x in range(90)], [1 + x % 3 for x in range(90)])])
+def test_more_tiles_than_workgroups(V, T, hd, nq, nkv, lens, rows):
+    """Runs that begin and end inside tiles, causal tiles of growing length."""
+    say(f"attend many tiles {T} hd={hd} nq={nq} nkv={nkv}")
+    rng = np.random.default_rng(nq + hd)
+    m = filled(rng, T, lens, rows, nkv=nkv, page=64, hd=hd)
+    d = Dev(V, m, T)
+    start = np.concatenate([[0], np.cumsum(rows)])
+    n = int(start[-1])
+    q = rounded(rng.standard_normal((n, nq, hd)), T)
+    qd = torch.from_numpy(q).to(T).cuda()
+    r = V.make_rows(i32(start), n)
+    out = torch.full((n, nq, hd), float("nan"), dtype=T, device="cuda")
+    scratch = torch.full((V.vla_tree_attention_scratch(d.p, r, nq),), 255, dtype=torch.uint8, device="cuda")
+    V.vla_tree_attention(d.p, 0, r, qd, out, scratch)
+    torch.cuda.synchronize()
+    want, tol = expect(m, T, 0, list(range(len(lens))), start, rows, q, None, hd ** -0.5, n / len(rows))
+    off = np.abs(vals(out) - want) / tol
+    assert np.all(off <= 1), float(np.nanmax(off))
+
+
+def test_drafts_without_pages_are_not_seen(V):
+    """A pool that ran dry: rows see the slots that have pages; a row that has
+    none is zero."""
+    say("attend without pages")
+    rng = np.random.default_rng(15)
+    for rows in ([20, 3, 40], [300, 5, 200]):
+        m = filled(rng, T16, [30, 0, 10], rows, hd=64)
+        m.held[:] = [2, 0, 2]  # 32 slots, none, 32 slots
+        d = Dev(V, m, T16)
+        start = np.concatenate([[0], np.cumsum(rows)])
+        n = int(start[-1])
+        q = rounded(rng.standard_normal((n, 2, 64)), T16)
+        r = V.make_rows(i32(start), n)
+        out = torch.full((n, 2, 64), float("nan"), dtype=T16, device="cuda")
+        scratch = torch.empty(V.vla_tree_attention_scratch(d.p, r, 2), dtype=torch.uint8, device="cuda")
+        V.vla_tree_attention(d.p, 0, r, torch.from_numpy(q).to(T16).cuda(), out, scratch)
+        torch.cuda.synchronize()
+        want, tol = expect(m, T16, 0, [0, 1, 2], start, rows, q, None, 0.125, n / 3)
+        assert np.all(np.abs(vals(out) - want) <= tol)
+        assert not vals(out)[start[1]:start[2]].any()
+
+
+def test_thousands_of_entries(V):
+    """Two steps of the search for a row's sequence, many chunks of entries."""
+    say("5,000 entries")
+    rng = np.random.default_rng(16)
+    lens, rows = [int(x) for x in rng.integers(0, 20, 5000)], [int(x) for x in rng.integers(0, 3, 5000)]
+    m = filled(rng, T16, lens, rows, hd=32)
+    d = Dev(V, m, T16)
+    start = np.concatenate([[0], np.cumsum(rows)])
+    n = int(start[-1])
+    x = rounded(rng.standard_normal((n, 3, 32)), T16)
+    xd = torch.from_numpy(x).to(T16).cuda()
+    r = V.make_rows(i32(start), n)
+    q, out = torch.empty((n, 1, 32), dtype=T16, device="cuda"), torch.empty((n, 1, 32), dtype=T16, device="cuda")
+    V.vla_qk_norm_rope(d.p, 0, r, V.make_rope_norm(), xd[:, :1], xd[:, 1:2], xd[:, 2:], q)
+    scratch = torch.empty(V.vla_tree_attention_scratch(d.p, r, 1), dtype=torch.uint8, device="cuda")
+    V.vla_tree_attention(d.p, 0, r, q, out, scratch)
+    V.vla_pages_commit(d.p, r)
+    torch.cuda.synchronize()
+    assert np.array_equal(vals(q), x[:, :1])
+    for s in range(5000):
+        for i in range(rows[s]):
+            p, at = m.where(s, lens[s] + i)
+            m.k[0, p, :, at], m.v[0, p, :, at] = x[start[s] + i, 1:2], x[start[s] + i, 2:]
+    want, tol = expect(m, T16, 0, list(range(5000)), start, rows, x[:, :1], None, 32 ** -0.5, n / 5000)
+    assert np.all(np.abs(vals(out) - want) <= tol)
+    m.lens += np.array(rows, np.int32)
+    d.same()
 
 
 def test_many_entries(V):

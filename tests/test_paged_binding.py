@@ -124,6 +124,9 @@ def test_calls_refuse_wrong_operands():
     refused("mask must be int32", V.vla_tree_attention, p, 0, r, q, q, scr, mask=Dev((7, 1), torch.int64))
     refused("scratch must be uint8", V.vla_tree_attention, p, 0, r, q, q, Dev((9,), F))
     refused("out must be [7, 4, 64]", V.vla_tree_attention, p, 0, r, q, k, scr)
+    refused("out must not be q", V.vla_tree_attention, p, 0, r, q, q, scr)
+    refused("scale", V.vla_tree_attention, p, 0, r, q, Dev((7, 4, 64), BF, ptr=0x20000), scr, scale=0.0)
+    refused("scale", V.vla_tree_attention, p, 0, r, q, Dev((7, 4, 64), BF, ptr=0x20000), scr, scale=float("inf"))
     refused("src must be", V.vla_pages_fork, p, Dev((2, 2)), Dev((4,)), Dev((4,)))
     refused("dst must have shape", V.vla_pages_fork, p, Dev((2,)), Dev((3,)), Dev((2,)))
     refused("made holds", V.vla_pages_fork, p, Dev((2,)), Dev((2,)), Dev((1,)))
