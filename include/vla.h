@@ -591,6 +591,15 @@ int vla_pages_commit(const vla_pages* c, const vla_rows* r, const int32_t* kept,
  * pages that no other sequence holds are free again. */
 int vla_pages_release(const vla_pages* c, int32_t n, const int32_t* seqs, void* stream);
 
+/* Store a context's prefix (every LM layer's K after RoPE and V, as
+ * vla_vlm_prefill wrote them) as new rows of sequence seq: row i to slot
+ * lens[seq] + i, for which the sequence holds pages (vla_pages_reserve;
+ * without: VLA_PAGES_OUT). vla_pages_commit then keeps them like any step's
+ * rows, and the LM can answer from there. pages' dtype, layers, kv_heads and
+ * head_dim are the model's. *rows (host, may be NULL) receives the number of
+ * rows. Asynchronous; ordered after the prefill by the caller. */
+int vla_ctx_to_pages(vla_model* m, const vla_ctx* c, const vla_pages* pages, int32_t seq, int32_t* rows, void* stream);
+
 /* Message for the last non-zero status on this thread ("" if none). */
 const char* vla_last_error(void);
 

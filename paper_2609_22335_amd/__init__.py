@@ -154,6 +154,7 @@ def _load():
         "vla_pages_fork": [P, I32, P, P, P, P],
         "vla_pages_commit": [P, P, P, P, P],
         "vla_pages_release": [P, I32, P, P],
+        "vla_ctx_to_pages": [P, P, P, I32, ctypes.POINTER(I32), P],
         "vla_kernel_timer": [P, ctypes.c_char_p],
         "vla_kernel_timer_read": [P, ctypes.POINTER(D), ctypes.POINTER(I64)],
     }
@@ -670,6 +671,14 @@ def vla_pages_release(pages: vla_pages, seqs, stream: int = 0) -> None:
     _check(_lib.vla_pages_release(ctypes.byref(pages), n[0], _ints(seqs, "seqs", pages, n), stream or None))
 
 
+def vla_ctx_to_pages(model: int, ctx: int, pages: vla_pages, seq: int, stream: int = 0) -> int:
+    """Returns the number of rows stored (the prefix)."""
+    n = ctypes.c_int32()
+    _at(pages)
+    _check(_lib.vla_ctx_to_pages(model, ctx, ctypes.byref(pages), int(seq), ctypes.byref(n), stream or None))
+    return n.value
+
+
 def exported_symbols() -> Iterable[str]:
     """Names of the C entry points this binding wraps."""
     return ["vla_preset", "vla_validate", "vla_model_config", "vla_create", "vla_destroy", "vla_ctx_create",
@@ -677,6 +686,6 @@ def exported_symbols() -> Iterable[str]:
             "vla_param_count", "vla_param_info", "vla_export_param", "vla_ctx_export_kv", "vla_ctx_export_cross", "vla_ctx_export_cog", "vla_wavelog_enable", "vla_wavelog_read",
             "vla_debug_gemm", "vla_debug_gemm_epi", "vla_debug_gemm_fold", "vla_debug_gemm_ln", "vla_gemm_noalloc", "vla_debug_attention", "vla_debug_attention_cache", "vla_debug_norm", "vla_debug_generate",
             "vla_debug_gemm_plan", "vla_pages_init", "vla_pages_reserve", "vla_qk_norm_rope", "vla_tree_attention",
-            "vla_tree_attention_scratch", "vla_pages_fork", "vla_pages_commit", "vla_pages_release",
+            "vla_tree_attention_scratch", "vla_pages_fork", "vla_pages_commit", "vla_pages_release", "vla_ctx_to_pages",
             "vla_kernel_timer",
             "vla_kernel_timer_read", "vla_last_error"]

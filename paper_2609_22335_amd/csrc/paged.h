@@ -69,4 +69,10 @@ hipError_t launch_pages_commit(const PagedCache& c, const PagedRows& r, const in
                                hipStream_t st);
 hipError_t launch_pages_release(const PagedCache& c, int n, const int32_t* seqs, hipStream_t st);
 
+// The prefix rows 0 .. rows - 1 of a context (K and V in the KV-cache layout,
+// nb 32-key blocks per KV head, layers lk / lv elements apart) to the slots
+// behind sequence seq's committed ones, in every layer.
+hipError_t launch_ctx_to_pages(const PagedCache& c, const void* k, const void* v, size_t lk, size_t lv, int nb,
+                               int rows, int seq, hipStream_t st);
+
 }  // namespace vla

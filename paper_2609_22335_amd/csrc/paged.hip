@@ -629,4 +629,61 @@ hipError_t launch_pages_commit(const PagedCache& c, const PagedRows& r, const in
   return hipGetLastError();
 }
 
+// ---------------------------------------------------------------------------
+// A context's prefix into a sequence
+// ---------------------------------------------------------------------------
+
+// A thread takes VEC keys by VEC head-dim elements: K's 16-byte runs lie along
+// the head dim as the pages' do, V's along the keys, so V is turned in
+// registers. 256 threads cover the elements of VEC keys first, so that rows are
+// written in one piece.
+template <typename T>
+__global__ __launch_bounds__(256) void k_ctx_to_pages(PagedCache c, const T* k, const T* v, size_t lk, size_t lv, int nb,
+                                                      int rows, int seq) {
+  constexpr int VEC = El<T>::VEC, DT = sizeof(T) == 2 ? DT_BF16 : DT_F32;
+  const int layer = blockIdx.y / c.nkv, j = blockIdx.y % c.nkv, chunks = c.hd / VEC;
+  const int i = blockIdx.x * 256 + threadIdx.x, key0 = i / chunks * VEC, d0 = i % chunks * VEC;
+  if (key0 >= rows) return;
+  int h = c.held[seq], l = c.lens[seq];
+  h = h < 0 ? 0 : h > c.max_pages ? c.max_pages : h;
+  const int cap = h << c.page_lg;
+  l = l < 0 ? 0 : l > cap ? cap : l;
+  T a[VEC][VEC];
+#pragma unroll
+  for (int e = 0; e < VEC; ++e)
+    *(u32x4*)a[e] = *(const u32x4*)(v + layer * lv + kv_vidx(DT, nb, c.hd, j, key0, d0 + e));
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) {
+    const int key = key0 + e;
+    if (key >= rows) break;
+    const int slot = l + key, page = page_of(c, seq, slot, cap);
+    if (page < 0) {
+      if (d0 == 0 && j == 0 && layer == 0) flag(c, PG_OUT);
+      continue;
+    }
+    const size_t to = slot_elem(c, layer, page, j, slot & (c.page - 1)) + d0;
+    T b[VEC];
+#pragma unroll
+    for (int t = 0; t < VEC; ++t) b[t] = a[t][e];
+    *(u32x4*)((T*)c.v + to) = *(const u32x4*)b;
+    *(u32x4*)((T*)c.k + to) = *(const u32x4*)(k + layer * lk + kv_kidx(DT, nb, c.hd, j, key, d0));
+  }
+}
+
+hipError_t launch_ctx_to_pages(const PagedCache& c, const void* k, const void* v, size_t lk, size_t lv, int nb,
+                               int rows, int seq, hipStream_t st) {
+  if (rows <= 0) return hipSuccess;
+  const int vec = c.dtype == DT_BF16 ? 8 : 4;
+  const long long items = (long long)((rows + vec - 1) / vec) * (c.hd / vec);
+  const dim3 grid((unsigned)((items + 255) / 256), (unsigned)(c.layers * c.nkv));
+  if (grid.y > 65535) return hipErrorInvalidValue;
+  if (c.dtype == DT_BF16)
+    hipLaunchKernelGGL(k_ctx_to_pages<uint16_t>, grid, dim3(256), 0, st, c, (const uint16_t*)k, (const uint16_t*)v, lk,
+                       lv, nb, rows, seq);
+  else
+    hipLaunchKernelGGL(k_ctx_to_pages<float>, grid, dim3(256), 0, st, c, (const float*)k, (const float*)v, lk, lv, nb,
+                       rows, seq);
+  return hipGetLastError();
+}
+
 }  // namespace vla

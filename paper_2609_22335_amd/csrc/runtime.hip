@@ -3497,4 +3497,20 @@ int vla_pages_release(const vla_pages* p, int32_t n, const int32_t* seqs, void* 
   })
 }
 
+int vla_ctx_to_pages(vla_model* m, const vla_ctx* ctx, const vla_pages* p, int32_t seq, int32_t* rows, void* stream) {
+  ABI_GUARD({
+    if (!m || !ctx) return fail(VLA_EINVAL, "NULL argument");
+    if (ctx->m != m) return fail(VLA_ESTATE, "context belongs to another model");
+    PagedCache c;
+    VLA_TRY(paged_cache(p, &c));
+    if (c.dtype != m->dt || c.layers != m->c.lm_layers || c.nkv != m->c.lm_kv_heads || c.hd != m->c.head_dim)
+      return fail(VLA_EINVAL, "pages: dtype, layers, kv_heads and head_dim must be the model's");
+    if (seq < 0 || seq >= c.n_seqs) return fail(VLA_EINVAL, "seq outside the cache");
+    if (rows) *rows = m->d.prefix;
+    return paged_launch("ctx to pages", launch_ctx_to_pages(c, ctx->K, ctx->V, ctx_layer_k(m), ctx_layer_v(m),
+                                                            m->d.prefix_pad / 32, m->d.prefix, seq,
+                                                            (hipStream_t)stream));
+  })
+}
+
 }  // extern "C"

@@ -882,3 +882,53 @@ def test_two_caches_on_two_streams(V):
     for a, b in zip(alone, got):
         for x, y in zip(a, b):
             assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("cfg", ["micro-f32", "micro-bf16", "tiny", "micro_dit"])
+def test_a_prefill_goes_on_in_pages(V, cfg):
+    """A frame's prefix moves from its context into a sequence's pages (bit for
+    bit what vla_ctx_export_kv gives, in every layer), behind slots that are
+    there, and a new token attends to it."""
+    import gpu_util as g
+    import synth
+    say(f"context to pages {cfg}")
+    c = {"micro-f32": synth.micro(0), "micro-bf16": synth.micro(1), "tiny": synth.TINY,
+         "micro_dit": synth.micro_dit(1)}[cfg]
+    T = T16 if c["dtype"] == V.VLA_BF16 else T32
+    P, nkv, hd, L = synth.derived(c)["prefix"], c["lm_kv_heads"], c["head_dim"], c["lm_layers"]
+    rng = np.random.default_rng(1)
+    m = filled(rng, T, [5, 18], [P + 1, P + 1], layers=L, nkv=nkv, page=16, hd=hd)
+    d = Dev(V, m, T)
+    with g.model(c) as model, g.context(model) as ctx:
+        f = g.DevFrame(synth.make_frame(c, 0, 0))
+        V.vla_vlm_prefill(model, f.c, ctx)
+        for s in (1, 0):
+            assert V.vla_ctx_to_pages(model, ctx, d.p, s) == P
+        torch.cuda.synchronize()
+        kv = [V.vla_ctx_export_kv(model, ctx, l, P * nkv * hd) for l in range(L)]
+        for s in (0, 1):
+            for i in range(P):
+                p, at = m.where(s, int(m.lens[s]) + i)
+                for l in range(L):
+                    m.k[l, p, :, at] = kv[l][0].reshape(P, nkv, hd)[i]
+                    m.v[l, p, :, at] = kv[l][1].reshape(P, nkv, hd)[i]
+        d.same()
+        for what, bad in (("layers", L + 1), ("kv_heads", nkv + 1), ("head_dim", hd + 32), ("dtype", 1 - c["dtype"])):
+            p = V.make_pages(d.k, d.v, d.table, d.lens, d.held, d.refs, d.status)
+            setattr(p, what, bad)
+            with pytest.raises(V.VlaError) as e:
+                V.vla_ctx_to_pages(model, ctx, p, 0)
+            assert e.value.code == -1
+        with pytest.raises(V.VlaError):
+            V.vla_ctx_to_pages(model, ctx, d.p, 2)
+    V.vla_pages_commit(d.p, V.make_rows(i32([0, P, 2 * P]), 2 * P))
+    m.commit([(0, P), (1, P)], [P, P])
+    nq = c["lm_heads"]
+    q = rounded(rng.standard_normal((2, nq, hd)), T)
+    r = V.make_rows(i32([0, 1, 2]), 2)
+    out = torch.empty((2, nq, hd), dtype=T, device="cuda")
+    scratch = torch.empty(V.vla_tree_attention_scratch(d.p, r, nq), dtype=torch.uint8, device="cuda")
+    V.vla_tree_attention(d.p, L - 1, r, torch.from_numpy(q).to(T).cuda(), out, scratch)
+    d.same()
+    want, tol = expect(m, T, L - 1, [0, 1], [0, 1, 2], [1, 1], q, None, hd ** -0.5, 1)
+    assert np.all(np.abs(vals(out) - want) <= tol)

@@ -166,6 +166,7 @@ def test_null_arguments_are_errors():
     assert lib.vla_pages_fork(p, 2, None, None, None, None) == -1
     assert lib.vla_pages_fork(p, -1, None, None, None, None) == -1
     assert lib.vla_pages_release(p, 1, None, None) == -1
+    assert lib.vla_ctx_to_pages(None, None, p, 0, None, None) == -1
     bad = V.make_rows(Dev((3,)), -1)
     assert lib.vla_pages_reserve(p, C.byref(bad), None) == -1
     # nothing to do reads nothing
