@@ -573,16 +573,19 @@ int vla_tree_attention_scratch(const vla_pages* c, const vla_rows* r, int32_t nq
 
 /* Branch: sequence dst[i] becomes a copy of src[i] (committed slots only).
  * Full pages are shared, the used slots of the last page are copied in every
- * layer to a page of the child's own. A pair is made (made[i] = 1) when dst[i]
- * holds no page, is not dst of an earlier pair and src[i] is not dst of any
- * pair; otherwise, or when no page is free (VLA_PAGES_OUT), made[i] = 0 and
- * dst[i] stays empty or as it was. src, dst and made: int32 [n]. */
+ * layer to a page of the child's own. A pair is fit when both are sequences of
+ * the cache and differ, and dst[i] holds no page and no slot. A fit pair is
+ * made (made[i] = 1) when dst[i] is not that of an earlier fit pair and src[i]
+ * is not dst of any fit pair; otherwise, or when no page is free
+ * (VLA_PAGES_OUT), made[i] = 0 and dst[i] stays as it was. src, dst and made:
+ * int32 [n], made an array of its own. */
 int vla_pages_fork(const vla_pages* c, int32_t n, const int32_t* src, const int32_t* dst, int32_t* made, void* stream);
 
 /* Keep the accepted drafts of every entry: draft kept[start[e] + j] moves to
  * slot lens + j in every layer, for j < n_kept[e], and lens grows by
- * n_kept[e]. A list ascends. kept NULL: the first n_kept[e] drafts (nothing
- * moves); n_kept NULL: all rows (kept must then be NULL). An entry whose list
+ * n_kept[e]. A list ascends. kept (int32 [n_rows]) NULL: the first n_kept[e]
+ * drafts (nothing moves); n_kept (int32 [n_entries]) NULL: all rows (kept must
+ * then be NULL). An entry whose list
  * does not ascend within its drafts keeps none (VLA_PAGES_BAD). Pages stay
  * with the sequence for its next drafts. */
 int vla_pages_commit(const vla_pages* c, const vla_rows* r, const int32_t* kept, const int32_t* n_kept, void* stream);

@@ -26,6 +26,9 @@ struct PagedRows {
   const int32_t* seqs = nullptr;   // [n_ent] or null
 };
 
+// A grid holds fewer than 2^32 threads in each direction.
+inline bool launchable(long long wgs, int threads) { return wgs * threads < (1ll << 32); }
+
 // status bits
 enum { PG_OUT = 1, PG_BAD = 2 };
 

@@ -174,6 +174,18 @@ def test_null_arguments_are_errors():
     assert lib.vla_pages_release(p, 0, None, None) == 0
 
 
+def test_grids_of_2_to_32_threads_are_refused():
+    lib, p, x = V._lib, C.byref(cache()), C.c_void_p(0x10000)
+    n = 1 << 24
+    r = V.make_rows(Dev((n + 1,)), 1 << 28)
+    assert lib.vla_pages_release(p, n, x, None) == -4
+    assert lib.vla_pages_fork(p, n, x, x, x, None) == -4
+    assert lib.vla_pages_commit(p, C.byref(r), x, x, None) == -4
+    rope = V.make_rope_norm()
+    assert lib.vla_qk_norm_rope(p, 0, C.byref(r), C.byref(rope), None, 4, x, 256, x, 128, x, 128, x, 256, None) == -4
+    assert "grid" in V.vla_last_error()
+
+
 @pytest.mark.parametrize("struct", ["vla_pages", "vla_rows", "vla_rope_norm"])
 def test_structs_match_header(struct):
     src = re.sub(r"/\*.*?\*/", "", open(os.path.join(ROOT, "include", "vla.h")).read(), flags=re.S)
