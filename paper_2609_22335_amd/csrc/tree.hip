@@ -42,6 +42,13 @@ __device__ __forceinline__ void barrier() {
   asm volatile("" ::: "memory");
 }
 
+// All waves meet; what this one has in flight stays there.
+__device__ __forceinline__ void meet() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
 struct Args {
   PagedCache c;
   PagedRows r;
@@ -270,12 +277,23 @@ __device__ __forceinline__ Tile deal(Run& r, bool first) {
 }
 __device__ __forceinline__ int uni(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
-// 16-byte chunk c of row r of a tile sits at position c ^ swz(r). Eight rows
-// read at one chunk (K fragments) start in eight different 16-byte columns of
-// a 128-byte line, four rows read at two chunks (V, transposed) in four
-// different pairs; only the low three bits of c change, so that the rest of a
-// fragment's address is an immediate.
-__device__ __forceinline__ constexpr int swz(int r) { return ((r & 3) << 1) | ((r >> 2) & 1); }
+// 16-byte chunk c of row r (of RB bytes) of a tile sits at position
+// c ^ swz(r). The LDS serves 256 bytes a cycle when they lie in different
+// 16-byte columns of a 256-byte line: 16 rows read at one chunk (K fragments)
+// do, and so do four rows read at four chunks (V, transposed). 128 bf16 a row:
+// K 245 and V 147 bytes a cycle, against 128 and 118 where only the low three
+// bits of c changed.
+template <int RB>
+__device__ __forceinline__ constexpr int swz(int r) {
+  return RB == 128 ? (((r >> 1) & 1) << 2) | ((r >> 2) & 3) : ((r & 3) << 2) | ((r >> 2) & 3);
+}
+// Byte b of a row whose first byte's column is x (a lane's constant): the part
+// that the swizzle reaches, and the rest, an immediate.
+template <int RB>
+__device__ __forceinline__ int turned(int x, int b) {
+  constexpr int IN = RB < 256 ? RB - 1 : 255;
+  return (x ^ (b & IN)) + (b & ~IN);
+}
 
 __device__ __forceinline__ f32x16 mma(u32x4 a, u32x4 b, f32x16 c, uint16_t) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0,
@@ -325,7 +343,7 @@ struct Loader {
     const Args& a = fresh();
     const int lane = threadIdx.x & 63;
     lrow = lane / CPR;
-    lchunk = (lane % CPR) ^ swz(lrow);
+    lchunk = (lane % CPR) ^ swz<RB>(lrow);
     hb = a.c.hd * (int)sizeof(T);
     pbytes = (uint32_t)(a.c.page * hb);
     table = (const __attribute__((address_space(4))) int32_t*)(a.c.table + (size_t)t.seq * a.c.max_pages);
@@ -333,12 +351,26 @@ struct Loader {
   }
   __device__ __forceinline__ Place place(int s0) const {
     const int left = kend - s0;
-    const int id = left > 0 ? table[s0 >> page_lg] : -1;
-    const bool ok = (unsigned)id < (unsigned)n_pages;
+    const int id = table[(left > 0 ? s0 : 0) >> page_lg];  // (one load, no branch)
+    const bool ok = left > 0 && (unsigned)id < (unsigned)n_pages;
     const int at = s0 & (page - 1), room = page - at;
     const unsigned long long off =
         (unsigned long long)(uint32_t)((ok ? id : 0) * nkv + head) * pbytes + (uint32_t)(at * hb);
     return Place{(uint32_t)off, (uint32_t)(off >> 32), ok ? (uint32_t)((left < room ? left : room) * hb) : 0u};
+  }
+  // The same by lanes, for the halves of 32 blocks of 32 slots from block j
+  // on: lane i's page, and from it its place (nothing from block j1 on).
+  __device__ __forceinline__ int page_id(int j, int j1) const {
+    const int lane = threadIdx.x & 63, s0 = 32 * j + 16 * lane;
+    return table[s0 < kend && s0 < 32 * j1 ? s0 >> page_lg : 0];
+  }
+  __device__ __forceinline__ void spread(int j, int j1, int id, uint32_t& lo, uint32_t& hi, uint32_t& bytes) const {
+    const int lane = threadIdx.x & 63, s0 = 32 * j + 16 * lane, left = kend - s0;
+    const bool ok = left > 0 && s0 < 32 * j1 && (unsigned)id < (unsigned)n_pages;
+    const int at = s0 & (page - 1), room = page - at;
+    const unsigned long long off =
+        (unsigned long long)(uint32_t)((ok ? id : 0) * nkv + head) * pbytes + (uint32_t)(at * hb);
+    lo = (uint32_t)off, hi = (uint32_t)(off >> 32), bytes = ok ? (uint32_t)((left < room ? left : room) * hb) : 0u;
   }
   // the places of slots kb and kb + 16 (which may lie in different pages)
   __device__ __forceinline__ void look(int kb, Place (&p)[2]) const {
@@ -358,7 +390,7 @@ struct Loader {
         if (PER < PARTS && hh * PER + i != part) continue;
         const int in = PER >= PARTS ? i + part : i;  // the load's place in its half
         const int r0 = in * RPI, idx = hh * PER + in;
-        const int ch = lchunk ^ swz(r0);
+        const int ch = lchunk ^ swz<RB>(r0);
         uint32_t off = (uint32_t)((r0 + lrow) * hb + ch * 16);
         if (HDP * (int)sizeof(T) != hb && ch * 16 >= hb) off = OOB;
         __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (LDS_AS void*)(dst + idx * 1024), 16, off, 0, 0, 0);
@@ -396,12 +428,12 @@ __device__ __forceinline__ void scores(const LB* kt, const u32x4 (&qf)[NQ], f32x
   constexpr int RB = HDP * (int)sizeof(T), SETS = NS * NQ / 4;
   const int l32 = threadIdx.x & 31, h = (threadIdx.x >> 5) & 1;
   const LB* base = kt + l32 * RB;
-  const int x = (h ^ swz(l32)) * 16;
+  const int x = (h ^ swz<RB>(l32)) * 16;
   u32x4 kf[2][4];
   auto read = [&](int set) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      kf[set & 1][i] = *(const LDS_AS u32x4*)(base + (x ^ (i * 32)) + (set % (NQ / 4)) * 128 +
+      kf[set & 1][i] = *(const LDS_AS u32x4*)(base + turned<RB>(x, (set % (NQ / 4) * 4 + i) * 32) +
                                              set / (NQ / 4) * 32 * RB);
   };
 #pragma unroll
@@ -419,13 +451,13 @@ __device__ __forceinline__ void scores(const LB* kt, const u32x4 (&qf)[NQ], f32x
   }
 }
 
-// Probabilities as operands of the second product: in bf16 rounded once, or
-// (TWO) as the sum of two bf16 values, where the matrix cores wait for memory
-// anyway.
+// Probabilities as operands of the second product, in bf16 as the sum of two
+// bf16 values: with few rows the matrix cores wait for memory anyway. (With
+// many they are rounded once: an error of at most 2^-8 of each, as much as the
+// result's own rounding may make.)
 struct Probs {
   u32x4 hi[2], lo[2];
 };
-template <bool TWO>
 __device__ __forceinline__ void round_probs(const f32x16& s, Probs& p) {
 #pragma unroll
   for (int kk = 0; kk < 2; ++kk) {
@@ -434,17 +466,17 @@ __device__ __forceinline__ void round_probs(const f32x16& s, Probs& p) {
     for (int i = 0; i < 4; ++i) {
       const float p0 = s[8 * kk + 2 * i], p1 = s[8 * kk + 2 * i + 1];
       hw[i] = bf2(p0, p1);
-      if (TWO) lw[i] = bf2(p0 - __uint_as_float(hw[i] << 16), p1 - __uint_as_float(hw[i] & 0xFFFF0000u));
+      lw[i] = bf2(p0 - __uint_as_float(hw[i] << 16), p1 - __uint_as_float(hw[i] & 0xFFFF0000u));
     }
     p.hi[kk] = u32x4{hw[0], hw[1], hw[2], hw[3]};
-    if (TWO) p.lo[kk] = u32x4{lw[0], lw[1], lw[2], lw[3]};
+    p.lo[kk] = u32x4{lw[0], lw[1], lw[2], lw[3]};
   }
 }
 
 // O^T += V^T P^T over NS x 32 keys. The first set of V's fragments (16 keys,
 // every column) is read by first(), before the softmax; each further set
 // before the products of the one ahead of it.
-template <typename T, int HDP, int NS, bool TWO>
+template <typename T, int HDP, int NS>
 struct Values {
   static constexpr int RB = HDP * (int)sizeof(T), NDT = HDP / 32;
   u32x4 vf[2][sizeof(T) == 2 ? NDT : 1];
@@ -458,7 +490,7 @@ struct Values {
 #pragma unroll
       for (int dt = 0; dt < NDT; ++dt) {
         auto tr = [&](int k0) {
-          const LB* q = base + (x ^ ((dt & 1) * 64)) + (dt >> 1) * 128 + k0 * RB;
+          const LB* q = base + turned<RB>(x ^ (swz<RB>(k0) * 16), dt * 64) + k0 * RB;
           return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)q));
         };
         const u32x2 u0 = tr(16 * set), u1 = tr(16 * set + 8);
@@ -470,7 +502,7 @@ struct Values {
     const int lane = threadIdx.x & 63, h = lane >> 5, il = lane & 15;
     if constexpr (sizeof(T) == 2) {
       base = vt + (4 * h + (il >> 2)) * RB + 8 * (il & 1);
-      x = ((2 * ((lane >> 4) & 1) + ((il & 3) >> 1)) ^ swz(4 * h + (il >> 2))) * 16;
+      x = ((2 * ((lane >> 4) & 1) + ((il & 3) >> 1)) ^ swz<RB>(4 * h + (il >> 2))) * 16;
     } else {
       base = vt;
       x = 0;
@@ -485,10 +517,8 @@ struct Values {
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int dt = 0; dt < NDT; ++dt) o[dt] = mma(vf[set & 1][dt], p[set >> 1].hi[set & 1], o[dt], T());
-        if (TWO) {
 #pragma unroll
-          for (int dt = 0; dt < NDT; ++dt) o[dt] = mma(vf[set & 1][dt], p[set >> 1].lo[set & 1], o[dt], T());
-        }
+        for (int dt = 0; dt < NDT; ++dt) o[dt] = mma(vf[set & 1][dt], p[set >> 1].lo[set & 1], o[dt], T());
       }
     } else {
       const int lane = threadIdx.x & 63, l32 = lane & 31, h = lane >> 5;
@@ -500,7 +530,7 @@ struct Values {
 #pragma unroll
           for (int dt = 0; dt < NDT; ++dt) {
             const int d = 32 * dt + l32;
-            const float v = *(const LDS_AS float*)(base + (32 * n + key) * RB + (((d / 4) ^ swz(key)) * 16) + (d % 4) * 4);
+            const float v = *(const LDS_AS float*)(base + (32 * n + key) * RB + (((d / 4) ^ swz<RB>(key)) * 16) + (d % 4) * 4);
             o[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[n][j], o[dt], 0, 0, 0);
           }
         }
@@ -719,14 +749,14 @@ __global__ __launch_bounds__(256, (many_waves<T, HDP>())) void k_tree_few(Args a
       if (masked) hide(s[0], seen_bits(t, kb, own, row));
       soften<NDT, 1>(s, a.c2, mx, l, o);
       Probs p[1];
-      if constexpr (sizeof(T) == 2) round_probs<true>(s[0], p[0]);
+      if constexpr (sizeof(T) == 2) round_probs(s[0], p[0]);
       if (more) wait_vm<Ld::NI>();  // V is here, the next K may be on its way
       else wait_vm<0>();
       if (masked) {
         odd |= clean_values<T, HDP, 1>(vl, 0);
         wait_lds();
       }
-      Values<T, HDP, 1, true> vv;
+      Values<T, HDP, 1> vv;
       vv.first(vl);
       vv.add(s, p, o);
       wait_lds();
@@ -784,21 +814,262 @@ __global__ __launch_bounds__(256, (many_waves<T, HDP>())) void k_tree_few(Args a
   });
 }
 
-// Keys of a block of the many-row kernel: two tiles of 32 to a barrier; one
-// where a block's products are long (fp32, wide heads), so that there are
-// more blocks to deal out (trees of 40 rows in fp32: 19.6 us against 23.5; of
-// 47 rows in bf16 at head dim 256: 34.2 against 33.1).
+// What the many-row kernels do with the rows of a wave: row m's sums o over l,
+// to out or, where a tile is shared, to the part `slot`.
 template <typename T, int HDP>
-constexpr int many_keys() {
-  return sizeof(T) == 2 || HDP <= 64 ? 64 : 32;
+__device__ __forceinline__ void finish(const Tile& t, int slot, int wv, int m, float mx, float l,
+                                       const f32x16 (&o)[HDP / 32]) {
+  constexpr int BM = 128, NDT = HDP / 32;
+  const Args& z = fresh();
+  const int lane = threadIdx.x & 63, l32 = lane & 31, h = lane >> 5, hd = z.c.hd;
+  if (m >= t.M) return;
+  if (t.whole) {
+    const float inv = inverse(l);
+    T* dst = out_row<T>(z, t, m) + 4 * h;
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt) {
+      if (32 * dt >= hd) break;
+#pragma unroll
+      for (int j4 = 0; j4 < 4; ++j4) {
+        const float v[4] = {o[dt][4 * j4], o[dt][4 * j4 + 1], o[dt][4 * j4 + 2], o[dt][4 * j4 + 3]};
+        put4<T>(dst + 32 * dt + 8 * j4, inv, v);
+      }
+    }
+    return;
+  }
+  float* po = z.part + ((size_t)slot * BM + wv * 32) * HDP;
+  float* pm = z.part + 2ll * z.wgs * BM * HDP + ((size_t)slot * BM + wv * 32) * 2;
+#pragma unroll
+  for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+    for (int j4 = 0; j4 < 4; ++j4)
+      // (in lane order: whole lines)
+      *(f32x4*)(po + ((dt * 4 + j4) * 64 + lane) * 4) =
+          f32x4{o[dt][4 * j4], o[dt][4 * j4 + 1], o[dt][4 * j4 + 2], o[dt][4 * j4 + 3]};
+  if (h == 0) pm[2 * l32] = mx, pm[2 * l32 + 1] = l;
 }
 
-// Many rows to a sequence: tiles of 128 rows, 32 to a wave, bound by the
-// matrix cores. The four waves share a ring of two blocks in the LDS, the
-// next one on its way while one is worked on: one barrier to a block.
-template <typename T, int HDP>
-__global__ __launch_bounds__(256, (many_waves<T, HDP>())) void k_tree_many(Args a) {
-  constexpr int BM = 128, BN = many_keys<T, HDP>(), NS = BN / 32;
+// Many rows to a sequence in bf16: tiles of 128 rows, 32 to a wave, bound by
+// the matrix cores (and, over seconds, by the power that they may draw: the
+// same call on zeros takes four fifths of the time). A wave keeps its matrix
+// core and its vector unit busy side by side: the products K Q^T of the next
+// 32 keys are issued between the exponentials of these, and V^T P^T between
+// the last of those and the next maxima. Fragments are read four products
+// ahead, also across the barrier in the middle of a step, and loads are out
+// two steps ahead. Against one block after another, scores, softmax, products
+// (both with two workgroups on a CU): chunks of 2,000 rows behind 4,000 slots,
+// 32 heads on 8, 277 us against 293 at head dim 64 and 387 against 390 (0.85
+// PFLOP/s, two sequences) at 128; 8 on 1 at head dim 256, one workgroup on a
+// CU, 381 against 435.
+template <int HDP>
+__global__ __launch_bounds__(256, (many_waves<uint16_t, HDP>())) void k_tree_many(Args a) {
+  typedef uint16_t T;
+  constexpr int BM = 128, BN = 32, RB = HDP * 2, NQ = RB / 32, NDT = HDP / 32;
+  typedef Loader<T, HDP, 4> Ld;
+  constexpr int LW = Ld::NI / 2;  // loads of a stage by a wave
+  // With two waves to a SIMD the new maxima are looked at beside products that
+  // are out; a wave on its own is faster with that between its steps (head dim
+  // 256, as above: 375 us against 420; head dim 64, two waves: 285 and 276).
+  constexpr bool PAIR = many_waves<T, HDP>() == 2;
+  constexpr int UP = PAIR ? 2 : 0;
+  // A stage of the ring holds V of a block and K of the next one. (By name: the
+  // compiler lets reads of one stage run beside loads into another only where
+  // it can tell them apart.)
+  __shared__ __attribute__((aligned(1024))) unsigned char s0[64 * RB], s1[64 * RB], s2[64 * RB], s3[64 * RB];
+  __shared__ int sOdd;
+  for_tiles<BM, BN>(a.wgs, [&](const Tile& t, int slot) {
+    const int tid = threadIdx.x, lane = tid & 63, wv = uni(tid >> 6), l32 = lane & 31, h = lane >> 5, il = lane & 15;
+    if (tid == 0) sOdd = 0;  // (barriers follow)
+    Ld ld;
+    ld.set(t);
+    auto stage = [&](int i) -> LB* {
+      const int S = i & 3;
+      return S == 0 ? (LB*)s0 : S == 1 ? (LB*)s1 : S == 2 ? (LB*)s2 : (LB*)s3;
+    };
+    // Where 32 blocks lie: lane i holds the place of half i. (A scalar look-up a
+    // step would make every read of the LDS behind it wait.)
+    uint32_t lo = 0, hi = 0, bytes = 0;
+    int id = ld.page_id(t.b0, t.b1);
+    auto window = [&](int j) {  // of blocks j .. j + 31, and the next one's pages on their way
+      ld.spread(j, t.b1, id, lo, hi, bytes);
+      id = ld.page_id(j + 32, t.b1);
+    };
+    Place pk[2] = {}, pv[2];  // K of block j, V of j - 1
+    auto look = [&](int j) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int at = 2 * ((j - t.b0) & 31) + e;
+        pv[e] = pk[e];
+        pk[e] = Place{(uint32_t)__builtin_amdgcn_readlane((int)lo, at), (uint32_t)__builtin_amdgcn_readlane((int)hi, at),
+                      (uint32_t)__builtin_amdgcn_readlane((int)bytes, at)};
+      }
+    };
+    auto issue = [&](LB* st) {
+      ld.issue(a.k, st, pk, wv);
+      ld.issue(a.v, st + 32 * RB, pv, wv);
+    };
+    const int m = t.rt * BM + wv * 32 + l32, mc = m < t.M ? m : t.M - 1, tok = mc / t.group, row = t.row0 + tok;
+    u32x4 qf[NQ];
+    load_query<T, NQ>(t, mc, qf);
+    window(t.b0);
+    look(t.b0);
+    ld.issue(a.k, (LB*)s0, pk, wv);
+    look(t.b0 + 1);
+    issue((LB*)s1);
+    look(t.b0 + 2);
+    issue((LB*)s2);
+    look(t.b0 + 3);
+    issue((LB*)s3);
+    const int own = t.causal && t.len + tok + 1 < t.kend ? t.len + tok + 1 : t.kend;
+    // (of the tile's first row: the waves clean V together)
+    const int safe0 = t.causal ? t.len + t.rt * BM / t.group + 1 : t.len;
+    const int safe = safe0 < t.kend ? safe0 : t.kend;
+    const f32x16 zero = {0.f};
+    f32x16 o[NDT], s[2];  // scores of two blocks, in turn
+#pragma unroll
+    for (int i = 0; i < NDT; ++i) o[i] = zero;
+    float mx = -INFINITY, l = 0.f, ref = 0.f, bm = 0.f;
+    // fragments: K's of 16 of the head dim and 32 keys; V's, transposed, of 16
+    // keys and 32 of the head dim
+    u32x4 kf[4], vf[2][NDT], p[2];
+    const int kx = (h ^ swz<RB>(l32)) * 16, kr = l32 * RB;
+    const int vr = (4 * h + (il >> 2)) * RB + 8 * (il & 1);
+    const int vx = ((2 * ((lane >> 4) & 1) + ((il & 3) >> 1)) ^ swz<RB>(4 * h + (il >> 2))) * 16;
+    auto read_k = [&](const LB* st, int i) { kf[i & 3] = *(const LDS_AS u32x4*)(st + kr + turned<RB>(kx, i * 32)); };
+    auto read_v = [&](const LB* st, int kk, int dt) {
+      auto tr = [&](int k0) {
+        const LB* q = st + 32 * RB + vr + turned<RB>(vx ^ (swz<RB>(k0) * 16), dt * 64) + k0 * RB;
+        return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)q));
+      };
+      const u32x2 u0 = tr(16 * kk), u1 = tr(16 * kk + 8);
+      vf[kk][dt] = u32x4{u0.x, u0.y, u1.x, u1.y};
+    };
+    auto fence = [&] { __builtin_amdgcn_sched_barrier(0); };
+    auto cover = [&](int b, f32x16& x) {  // scores of block b that their rows do not see
+      hide(x, seen_bits(t, b * BN, own, row));
+      bm = x[0];
+#pragma unroll
+      for (int j = 1; j < 16; ++j) bm = fmaxf(bm, x[j]);
+    };
+    // (as soften())
+    auto raise = [&] {
+      bm = max_x32(bm) * a.c2;
+      if (__any(bm > mx + 8.f)) {
+        const float mn = fmaxf(mx, bm);
+        const float f = mn == -INFINITY ? 1.f : ex2(mx - mn);
+        mx = mn;
+        l *= f;
+#pragma unroll
+        for (int i = 0; i < NDT; ++i)
+#pragma unroll
+          for (int j = 0; j < 16; ++j) o[i][j] *= f;
+      }
+      ref = mx == -INFINITY ? 0.f : mx;
+    };
+    // probabilities j0 .. j1 - 1 of the lane's 16, rounded once for the products
+    auto soft = [&](f32x16& cur, int j0, int j1) {
+#pragma unroll
+      for (int j = j0; j < j1; ++j) {
+        cur[j] = ex2(__builtin_fmaf(cur[j], a.c2, -ref));
+        l += cur[j];
+        if (j & 1) p[j >> 3][(j >> 1) & 3] = bf2(cur[j - 1], cur[j]);
+        asm volatile("" : "+v"(l));  // (here, not behind the step's branches)
+      }
+    };
+    // Step b, P = (b - b0) % 4: scores of block b + 1 (behind the last block,
+    // of zeros), probabilities and products of block b.
+    auto step = [&](auto phase, int b) {
+      constexpr int P = decltype(phase)::value, JQ = 12;
+      const LB *st = stage(P + 1), *sn = stage(P + 2);
+      f32x16 &cur = s[P & 1], &nxt = s[(P + 1) & 1];
+      if ((b + 1) * BN > safe) {
+        if (clean_values<T, HDP, 4>((LB*)st + 32 * RB, wv)) sOdd = 1;
+        wait_lds();
+        barrier();
+      }
+#pragma unroll
+      for (int i = 0; i < NQ; ++i) {
+        if (i == UP && PAIR) raise();
+        nxt = mma(kf[i & 3], qf[i], i ? nxt : zero, T());
+        if (i + 4 < NQ) read_k(st, i + 4);
+        else
+#pragma unroll
+          for (int dt = NDT * (i - NQ + 4) / 4; dt < NDT * (i - NQ + 5) / 4; ++dt) read_v(st, 0, dt);
+        if (i == 2) look(b + 4);
+        if (i >= UP) soft(cur, (i - UP) * JQ / (NQ - UP), (i + 1 - UP) * JQ / (NQ - UP));
+        fence();
+      }
+      wait_vm<LW>();  // stage b + 1 is here, b + 2 may be on its way,
+      meet();         // and stage b - 1 is worked off
+#pragma unroll
+      for (int dt = 0; dt < NDT; ++dt) {
+        o[dt] = mma(vf[0][dt], p[0], o[dt], T());
+        read_v(st, 1, dt);
+        soft(cur, JQ + dt * (16 - JQ) / NDT, JQ + (dt + 1) * (16 - JQ) / NDT);
+        if (dt == 0) ld.issue(a.k, stage(P), pk, wv);
+        if (dt == 1) ld.issue(a.v, stage(P) + 32 * RB, pv, wv);
+        fence();
+      }
+#pragma unroll
+      for (int dt = 0; dt < NDT; ++dt) {
+        o[dt] = mma(vf[1][dt], p[1], o[dt], T());
+#pragma unroll
+        for (int i = 4 * dt / NDT; i < 4 * (dt + 1) / NDT; ++i) read_k(sn, i);
+#pragma unroll
+        for (int j = 16 * dt / NDT; j < 16 * (dt + 1) / NDT; ++j) bm = j ? fmaxf(bm, nxt[j]) : nxt[0];
+        asm volatile("" : "+v"(bm));
+        fence();
+      }
+      if ((b + 2) * BN > safe) cover(b + 1, nxt);
+      if (!PAIR && b + 1 < t.b1) raise();
+    };
+    // the first block's scores
+    wait_vm<2 * LW>();
+    barrier();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) read_k((LB*)s0, i);
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) {
+      s[0] = mma(kf[i & 3], qf[i], i ? s[0] : zero, T());
+      if (i + 4 < NQ) read_k((LB*)s0, i + 4);
+      fence();
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) read_k((LB*)s1, i);
+    bm = s[0][0];
+#pragma unroll
+    for (int j = 1; j < 16; ++j) bm = fmaxf(bm, s[0][j]);
+    if ((t.b0 + 1) * BN > safe) cover(t.b0, s[0]);
+    if (!PAIR) raise();
+    for (int b = t.b0;; b += 4) {
+      if (((b - t.b0) & 31) == 28) window(b + 4);
+      step(std::integral_constant<int, 0>(), b);
+      if (b + 1 >= t.b1) break;
+      step(std::integral_constant<int, 1>(), b + 1);
+      if (b + 2 >= t.b1) break;
+      step(std::integral_constant<int, 2>(), b + 2);
+      if (b + 3 >= t.b1) break;
+      step(std::integral_constant<int, 3>(), b + 3);
+      if (b + 4 >= t.b1) break;
+    }
+    wait_vm<0>();  // (loads of blocks behind the last, which bring zeros)
+    l = sum_x32(l);
+    if (sOdd)  // (written before the last step's barrier)
+      for (int b = t.b0; b < t.b1; ++b)
+        if ((b + 1) * BN > safe) add_odd_values<T, HDP>(t, b * BN, seen_bits(t, b * BN, own, row), o);
+    finish<T, HDP>(t, slot, wv, m, mx, l, o);
+  });
+}
+
+// Many rows to a sequence in fp32: tiles of 128 rows, 32 to a wave, bound by
+// the matrix cores. The four waves share a ring of two blocks in the LDS, the
+// next one on its way while one is worked on: one barrier to a block. A block
+// is two tiles of 32 keys, at head dim 128 one, so that there are more blocks
+// to deal out (trees of 40 rows 19.6 us against 23.5).
+template <int HDP>
+__global__ __launch_bounds__(256, (many_waves<float, HDP>())) void k_tree_many32(Args a) {
+  typedef float T;
+  constexpr int BM = 128, BN = HDP <= 64 ? 64 : 32, NS = BN / 32;
   constexpr int RB = HDP * (int)sizeof(T), NQ = RB / 32, NDT = HDP / 32;
   typedef Loader<T, HDP, 4> Ld;
   __shared__ __attribute__((aligned(1024))) unsigned char sK0[NS * 32 * RB], sK1[NS * 32 * RB];
@@ -858,16 +1129,11 @@ __global__ __launch_bounds__(256, (many_waves<T, HDP>())) void k_tree_many(Args 
         wait_lds();
         barrier();
       }
-      Values<T, HDP, NS, false> vv;
+      Values<T, HDP, NS> vv;
       vv.first(vt);
       look(b + 2);
       soften<NDT, NS>(s, a.c2, mx, l, o);
-      Probs p[NS];
-      if constexpr (sizeof(T) == 2) {
-#pragma unroll
-        for (int n = 0; n < NS; ++n) round_probs<false>(s[n], p[n]);
-      }
-      vv.add(s, p, o);
+      vv.add(s, {}, o);
     };
     for (int b = t.b0; b < t.b1; b += 2) {
       step(std::integral_constant<int, 0>(), b);
@@ -877,34 +1143,7 @@ __global__ __launch_bounds__(256, (many_waves<T, HDP>())) void k_tree_many(Args 
     if (sOdd)  // (written before the last block's barrier)
       for (int kb = t.b0 * BN; kb < t.b1 * BN; kb += 32)
         if (kb + 32 > safe) add_odd_values<T, HDP>(t, kb, seen_bits(t, kb, own, row), o);
-    const Args& z = fresh();
-    float* po = z.part + (size_t)slot * BM * HDP;
-    float* pm = z.part + 2ll * z.wgs * BM * HDP + (size_t)slot * BM * 2;
-    if (t.whole) {
-      const float inv = inverse(l);
-      T* dst = out_row<T>(z, t, mc) + 4 * h;
-      const int hd = z.c.hd;
-      if (m < t.M) {
-#pragma unroll
-        for (int dt = 0; dt < NDT; ++dt) {
-          if (32 * dt >= hd) break;
-#pragma unroll
-          for (int j4 = 0; j4 < 4; ++j4) {
-            const float v[4] = {o[dt][4 * j4], o[dt][4 * j4 + 1], o[dt][4 * j4 + 2], o[dt][4 * j4 + 3]};
-            put4<T>(dst + 32 * dt + 8 * j4, inv, v);
-          }
-        }
-      }
-    } else if (m < t.M) {
-#pragma unroll
-      for (int dt = 0; dt < NDT; ++dt)
-#pragma unroll
-        for (int j4 = 0; j4 < 4; ++j4)
-          // (in lane order: whole lines)
-          *(f32x4*)(po + wv * 32 * HDP + ((dt * 4 + j4) * 64 + lane) * 4) =
-              f32x4{o[dt][4 * j4], o[dt][4 * j4 + 1], o[dt][4 * j4 + 2], o[dt][4 * j4 + 3]};
-      if (h == 0) pm[2 * (wv * 32 + l32)] = mx, pm[2 * (wv * 32 + l32) + 1] = l;
-    }
+    finish<T, HDP>(t, slot, wv, m, mx, l, o);
   });
 }
 
@@ -1085,7 +1324,8 @@ template <typename T, int HDP>
 hipError_t run(const TreeAttnDesc& d, const Args& a, hipStream_t st) {
   const int rows = tile_rows(d);
   if (rows == 32) hipLaunchKernelGGL((k_tree_few<T, HDP>), dim3(a.wgs), dim3(256), 0, st, a);
-  else hipLaunchKernelGGL((k_tree_many<T, HDP>), dim3(a.wgs), dim3(256), 0, st, a);
+  else if constexpr (sizeof(T) == 2) hipLaunchKernelGGL(k_tree_many<HDP>, dim3(a.wgs), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL(k_tree_many32<HDP>, dim3(a.wgs), dim3(256), 0, st, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   // (at most as many as there can be pieces to take)
