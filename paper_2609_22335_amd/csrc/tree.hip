@@ -217,6 +217,13 @@ __device__ __forceinline__ Tile deal(Run& r, bool first) {
     c0 = 0;
     if (pass == 0 && 2 * tiles <= a.wgs) {
       per = (int)ceil_div(total, a.wgs - (int)tiles);
+      // A part of b blocks of the tile's B costs b steps here and the join B / b
+      // parts, so b stays at a multiple of sqrt(B) or above. One sequence, 8
+      // heads on 1 of 128, with that and without: a token behind 60,000 slots
+      // 24.9 us and 44.8; trees of 24 behind 8,000 28.8 us and 73.8, behind
+      // 60,000 50.5 us and 78.1.
+      const int least = (int)ceilf(sqrtf((float)total / (float)(tiles > 0 ? tiles : 1)) * (BM == 32 ? 0.25f : 0.5f));
+      per = per > least ? per : least;
       pass = 1;
       if (per > 1) {
         total = 0;
