@@ -222,8 +222,9 @@ __device__ __forceinline__ Tile deal(Run& r, bool first) {
       // heads on 1 of 128, with that and without: a token behind 60,000 slots
       // 24.9 us and 44.8; trees of 24 behind 8,000 28.8 us and 73.8, behind
       // 60,000 50.5 us and 78.1.
-      const int least = (int)ceilf(sqrtf((float)total / (float)(tiles > 0 ? tiles : 1)) * (BM == 32 ? 0.25f : 0.5f));
-      per = per > least ? per : least;
+      constexpr float C = BM == 32 ? 16.f : 4.f;
+      if ((float)per * (float)per * (C * (float)tiles) < (float)total)
+        per = (int)ceilf(__builtin_amdgcn_sqrtf((float)total / (C * (float)tiles)));
       pass = 1;
       if (per > 1) {
         total = 0;
@@ -286,19 +287,21 @@ __device__ __forceinline__ int uni(int x) { return __builtin_amdgcn_readfirstlan
 
 // 16-byte chunk c of row r (of RB bytes) of a tile sits at position
 // c ^ swz(r). The LDS serves 256 bytes a cycle when they lie in different
-// 16-byte columns of a 256-byte line: 16 rows read at one chunk (K fragments)
-// do, and so do four rows read at four chunks (V, transposed). 128 bf16 a row:
-// K 245 and V 147 bytes a cycle, against 128 and 118 where only the low three
-// bits of c changed.
-template <int RB>
+// 16-byte columns of a 256-byte line: with the swizzle over 16 columns 16 rows
+// read at one chunk (K fragments) do, and so do four rows read at four chunks
+// (V, transposed). 128 bf16 a row: K 245 and V 147 bytes a cycle, against 128
+// and 118 over 8 columns. Those take fewer addresses (the rest of a fragment's
+// is an immediate) and do where the LDS is not what a wave waits for.
+template <int RB, int COLS>
 __device__ __forceinline__ constexpr int swz(int r) {
-  return RB == 128 ? (((r >> 1) & 1) << 2) | ((r >> 2) & 3) : ((r & 3) << 2) | ((r >> 2) & 3);
+  return COLS == 8 ? ((r & 3) << 1) | ((r >> 2) & 1)
+         : RB == 128 ? (((r >> 1) & 1) << 2) | ((r >> 2) & 3) : ((r & 3) << 2) | ((r >> 2) & 3);
 }
 // Byte b of a row whose first byte's column is x (a lane's constant): the part
 // that the swizzle reaches, and the rest, an immediate.
-template <int RB>
+template <int RB, int COLS>
 __device__ __forceinline__ int turned(int x, int b) {
-  constexpr int IN = RB < 256 ? RB - 1 : 255;
+  constexpr int IN = (RB < 16 * COLS ? RB : 16 * COLS) - 1;
   return (x ^ (b & IN)) + (b & ~IN);
 }
 
@@ -338,7 +341,7 @@ struct Place {
 // A buffer resource spans what is left of one page of one head: slots behind
 // the last key and chunks behind the head dim lie out of its range and become
 // zeros.
-template <typename T, int HDP, int PARTS>
+template <typename T, int HDP, int PARTS, int COLS>
 struct Loader {
   static constexpr int RB = HDP * (int)sizeof(T), CPR = RB / 16, RPI = 1024 / RB, NI = 32 / RPI;
   int lrow, lchunk, hb;  // the lane's row and chunk of a load; bytes of a row in memory
@@ -350,7 +353,7 @@ struct Loader {
     const Args& a = fresh();
     const int lane = threadIdx.x & 63;
     lrow = lane / CPR;
-    lchunk = (lane % CPR) ^ swz<RB>(lrow);
+    lchunk = (lane % CPR) ^ swz<RB, COLS>(lrow);
     hb = a.c.hd * (int)sizeof(T);
     pbytes = (uint32_t)(a.c.page * hb);
     table = (const __attribute__((address_space(4))) int32_t*)(a.c.table + (size_t)t.seq * a.c.max_pages);
@@ -358,8 +361,8 @@ struct Loader {
   }
   __device__ __forceinline__ Place place(int s0) const {
     const int left = kend - s0;
-    const int id = table[(left > 0 ? s0 : 0) >> page_lg];  // (one load, no branch)
-    const bool ok = left > 0 && (unsigned)id < (unsigned)n_pages;
+    const int id = left > 0 ? table[s0 >> page_lg] : -1;
+    const bool ok = (unsigned)id < (unsigned)n_pages;
     const int at = s0 & (page - 1), room = page - at;
     const unsigned long long off =
         (unsigned long long)(uint32_t)((ok ? id : 0) * nkv + head) * pbytes + (uint32_t)(at * hb);
@@ -397,7 +400,7 @@ struct Loader {
         if (PER < PARTS && hh * PER + i != part) continue;
         const int in = PER >= PARTS ? i + part : i;  // the load's place in its half
         const int r0 = in * RPI, idx = hh * PER + in;
-        const int ch = lchunk ^ swz<RB>(r0);
+        const int ch = lchunk ^ swz<RB, COLS>(r0);
         uint32_t off = (uint32_t)((r0 + lrow) * hb + ch * 16);
         if (HDP * (int)sizeof(T) != hb && ch * 16 >= hb) off = OOB;
         __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (LDS_AS void*)(dst + idx * 1024), 16, off, 0, 0, 0);
@@ -435,12 +438,12 @@ __device__ __forceinline__ void scores(const LB* kt, const u32x4 (&qf)[NQ], f32x
   constexpr int RB = HDP * (int)sizeof(T), SETS = NS * NQ / 4;
   const int l32 = threadIdx.x & 31, h = (threadIdx.x >> 5) & 1;
   const LB* base = kt + l32 * RB;
-  const int x = (h ^ swz<RB>(l32)) * 16;
+  const int x = (h ^ swz<RB, 8>(l32)) * 16;
   u32x4 kf[2][4];
   auto read = [&](int set) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      kf[set & 1][i] = *(const LDS_AS u32x4*)(base + turned<RB>(x, (set % (NQ / 4) * 4 + i) * 32) +
+      kf[set & 1][i] = *(const LDS_AS u32x4*)(base + turned<RB, 8>(x, (set % (NQ / 4) * 4 + i) * 32) +
                                              set / (NQ / 4) * 32 * RB);
   };
 #pragma unroll
@@ -497,7 +500,7 @@ struct Values {
 #pragma unroll
       for (int dt = 0; dt < NDT; ++dt) {
         auto tr = [&](int k0) {
-          const LB* q = base + turned<RB>(x ^ (swz<RB>(k0) * 16), dt * 64) + k0 * RB;
+          const LB* q = base + turned<RB, 8>(x ^ (swz<RB, 8>(k0) * 16), dt * 64) + k0 * RB;
           return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)q));
         };
         const u32x2 u0 = tr(16 * set), u1 = tr(16 * set + 8);
@@ -509,7 +512,7 @@ struct Values {
     const int lane = threadIdx.x & 63, h = lane >> 5, il = lane & 15;
     if constexpr (sizeof(T) == 2) {
       base = vt + (4 * h + (il >> 2)) * RB + 8 * (il & 1);
-      x = ((2 * ((lane >> 4) & 1) + ((il & 3) >> 1)) ^ swz<RB>(4 * h + (il >> 2))) * 16;
+      x = ((2 * ((lane >> 4) & 1) + ((il & 3) >> 1)) ^ swz<RB, 8>(4 * h + (il >> 2))) * 16;
     } else {
       base = vt;
       x = 0;
@@ -537,7 +540,7 @@ struct Values {
 #pragma unroll
           for (int dt = 0; dt < NDT; ++dt) {
             const int d = 32 * dt + l32;
-            const float v = *(const LDS_AS float*)(base + (32 * n + key) * RB + (((d / 4) ^ swz<RB>(key)) * 16) + (d % 4) * 4);
+            const float v = *(const LDS_AS float*)(base + (32 * n + key) * RB + (((d / 4) ^ swz<RB, 8>(key)) * 16) + (d % 4) * 4);
             o[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[n][j], o[dt], 0, 0, 0);
           }
         }
@@ -711,7 +714,7 @@ template <typename T, int HDP>
 __global__ __launch_bounds__(256, (many_waves<T, HDP>())) void k_tree_few(Args a) {
   constexpr int BM = 32, BN = 128;
   constexpr int RB = HDP * (int)sizeof(T), NQ = RB / 32, NDT = HDP / 32;
-  typedef Loader<T, HDP, 1> Ld;
+  typedef Loader<T, HDP, 1, 8> Ld;
   static_assert(2 * Ld::NI < 60, "loads in flight");
   __shared__ __attribute__((aligned(1024))) unsigned char sK[4][32 * RB];
   __shared__ __attribute__((aligned(1024))) unsigned char sV[4][32 * RB];
@@ -872,7 +875,7 @@ template <int HDP>
 __global__ __launch_bounds__(256, (many_waves<uint16_t, HDP>())) void k_tree_many(Args a) {
   typedef uint16_t T;
   constexpr int BM = 128, BN = 32, RB = HDP * 2, NQ = RB / 32, NDT = HDP / 32;
-  typedef Loader<T, HDP, 4> Ld;
+  typedef Loader<T, HDP, 4, 16> Ld;
   constexpr int LW = Ld::NI / 2;  // loads of a stage by a wave
   // With two waves to a SIMD the new maxima are looked at beside products that
   // are out; a wave on its own is faster with that between its steps (head dim
@@ -939,13 +942,13 @@ __global__ __launch_bounds__(256, (many_waves<uint16_t, HDP>())) void k_tree_man
     // fragments: K's of 16 of the head dim and 32 keys; V's, transposed, of 16
     // keys and 32 of the head dim
     u32x4 kf[4], vf[2][NDT], p[2];
-    const int kx = (h ^ swz<RB>(l32)) * 16, kr = l32 * RB;
+    const int kx = (h ^ swz<RB, 16>(l32)) * 16, kr = l32 * RB;
     const int vr = (4 * h + (il >> 2)) * RB + 8 * (il & 1);
-    const int vx = ((2 * ((lane >> 4) & 1) + ((il & 3) >> 1)) ^ swz<RB>(4 * h + (il >> 2))) * 16;
-    auto read_k = [&](const LB* st, int i) { kf[i & 3] = *(const LDS_AS u32x4*)(st + kr + turned<RB>(kx, i * 32)); };
+    const int vx = ((2 * ((lane >> 4) & 1) + ((il & 3) >> 1)) ^ swz<RB, 16>(4 * h + (il >> 2))) * 16;
+    auto read_k = [&](const LB* st, int i) { kf[i & 3] = *(const LDS_AS u32x4*)(st + kr + turned<RB, 16>(kx, i * 32)); };
     auto read_v = [&](const LB* st, int kk, int dt) {
       auto tr = [&](int k0) {
-        const LB* q = st + 32 * RB + vr + turned<RB>(vx ^ (swz<RB>(k0) * 16), dt * 64) + k0 * RB;
+        const LB* q = st + 32 * RB + vr + turned<RB, 16>(vx ^ (swz<RB, 16>(k0) * 16), dt * 64) + k0 * RB;
         return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)q));
       };
       const u32x2 u0 = tr(16 * kk), u1 = tr(16 * kk + 8);
@@ -1078,7 +1081,7 @@ __global__ __launch_bounds__(256, (many_waves<float, HDP>())) void k_tree_many32
   typedef float T;
   constexpr int BM = 128, BN = HDP <= 64 ? 64 : 32, NS = BN / 32;
   constexpr int RB = HDP * (int)sizeof(T), NQ = RB / 32, NDT = HDP / 32;
-  typedef Loader<T, HDP, 4> Ld;
+  typedef Loader<T, HDP, 4, 8> Ld;
   __shared__ __attribute__((aligned(1024))) unsigned char sK0[NS * 32 * RB], sK1[NS * 32 * RB];
   __shared__ __attribute__((aligned(1024))) unsigned char sV0[NS * 32 * RB], sV1[NS * 32 * RB];
   __shared__ int sOdd;
