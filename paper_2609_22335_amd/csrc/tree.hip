@@ -1312,16 +1312,18 @@ __global__ __launch_bounds__(256) void k_tree_join(Args a) {
 
 int pad_hd(int dtype, int hd) { return hd <= 64 ? 64 : hd <= 128 ? 128 : 256; }
 
-// Many rows to a sequence (on average more than one tile of 128): tiles of 128
-// rows, whose waves share K and V. Below that the two are close, and tiles of
-// 32 keep more of the probabilities: eight caches of 4,000 slots at head dim
-// 128, 8 query heads on one KV head, 64 rows 22.2 us against 20.3, 128 rows 23.7
-// against 23.1, 192 rows 27.6 against 25.4; two of 30,000 slots 26.2 / 30.5,
-// 33.3 / 32.4, 37.4 / 31.7; eight of 2,000 at head dim 256 25.5 / 25.0, 25.7 /
-// 29.0, 29.2 / 26.4; of 1,000 in fp32 21.2 / 23.4, 26.2 / 26.6, 27.2 / 29.4.
+// Many rows to a sequence (on average more than 128, in fp32 more than 256):
+// tiles of 128 rows, whose waves share K and V. Below that the two are close,
+// and tiles of 32 keep more of the probabilities. Trees over 8 query heads on
+// one KV head, 64, 128, 192 and 256 rows in tiles of 32 / 128: eight caches of
+// 4,000 slots at head dim 128 18.4 / 19.5, 22.1 / 21.1, 25.6 / 24.2 and 27.6 /
+// 25.9 us; two of 30,000 25.9 / 29.9, 32.2 / 31.2, 39.0 / 33.7 and 41.0 / 33.9;
+// eight of 2,000 at head dim 256 23.3 / 19.9, 24.7 / 23.2, 27.7 / 25.5 and
+// 28.8 / 27.3. In fp32, eight of 1,000, 192, 256 and 320 rows: 25.5 / 27.4,
+// 31.8 / 30.4, 37.1 / 34.0; four of 4,000 35.6 / 42.1, 39.2 / 42.7, 44.0 / 50.5.
 int tile_rows(const TreeAttnDesc& d) {
   const long long rows = (long long)d.r.n_rows * (d.nq / d.c.nkv);
-  return rows > 128ll * d.r.n_ent ? 128 : 32;
+  return rows > (d.c.dtype == DT_BF16 ? 128ll : 256ll) * d.r.n_ent ? 128 : 32;
 }
 // Workgroups, each with a run of blocks: as many as the CUs hold.
 int tree_wgs(const TreeAttnDesc& d) {

@@ -281,6 +281,11 @@ ATTEND = [
     (T32, 96, 6, 2, 16, "random", [30, 0, 50], [61, 17, 3]),
     (T32, 32, 2, 1, 16, None, [60], [100]),
     (T32, 128, 8, 1, 64, None, [5, 200], [64, 1]),
+    (T32, 64, 8, 1, 16, "tree", [70, 0], [50, 41]),
+    (T32, 96, 6, 1, 16, "random", [33], [61]),
+    (T32, 128, 8, 1, 32, "tree", [77, 300], [45, 40]),
+    (T16, 128, 8, 1, 16, "tree", [700, 0], [50, 40]),
+    (T16, 64, 8, 1, 16, "random", [1100], [60]),
 ]
 
 
@@ -324,7 +329,7 @@ def test_tree_attention(V, T, hd, nq, nkv, page, kind, lens, rows):
     d.same()
 
 
-@pytest.mark.parametrize("T,rows,nq", [(T16, 20, 4), (T16, 90, 4), (T32, 20, 2)])
+@pytest.mark.parametrize("T,rows,nq", [(T16, 20, 4), (T16, 90, 4), (T32, 20, 2), (T32, 90, 4)])
 def test_masked_drafts_may_hold_anything(V, T, rows, nq):
     """NaN and infinities in K and V of drafts show in the rows that see them
     and in no other, and a row of large scores stays finite."""
@@ -421,6 +426,29 @@ def test_more_tiles_than_workgroups(V, T, hd, nq, nkv, lens, rows):
     out = torch.full((n, nq, hd), float("nan"), dtype=T, device="cuda")
     scratch = torch.full((V.vla_tree_attention_scratch(d.p, r, nq),), 255, dtype=torch.uint8, device="cuda")
     V.vla_tree_attention(d.p, 0, r, qd, out, scratch)
+    torch.cuda.synchronize()
+    want, tol = expect(m, T, 0, list(range(len(lens))), start, rows, q, None, hd ** -0.5, n / len(rows))
+    off = np.abs(vals(out) - want) / tol
+    assert np.all(off <= 1), float(np.nanmax(off))
+
+
+@pytest.mark.parametrize("T,hd,nq,nkv,page,lens,rows", [
+    (T16, 64, 32, 8, 16, [3001, 2040, 1500, 2999], [300, 299, 31, 257]),
+    (T16, 128, 32, 8, 256, [2500, 3100], [300, 260]),
+    (T16, 256, 16, 8, 32, [1025, 2400], [400, 333])])
+def test_long_runs(V, T, hd, nq, nkv, page, lens, rows):
+    """Runs of more blocks of keys than a wave looks up at once."""
+    say(f"attend long runs {T} hd={hd} page={page}")
+    rng = np.random.default_rng(hd + page)
+    m = filled(rng, T, lens, rows, nkv=nkv, page=page, hd=hd)
+    d = Dev(V, m, T)
+    start = np.concatenate([[0], np.cumsum(rows)])
+    n = int(start[-1])
+    q = rounded(rng.standard_normal((n, nq, hd)), T)
+    r = V.make_rows(i32(start), n)
+    out = torch.full((n, nq, hd), float("nan"), dtype=T, device="cuda")
+    scratch = torch.full((V.vla_tree_attention_scratch(d.p, r, nq),), 255, dtype=torch.uint8, device="cuda")
+    V.vla_tree_attention(d.p, 0, r, torch.from_numpy(q).to(T).cuda(), out, scratch)
     torch.cuda.synchronize()
     want, tol = expect(m, T, 0, list(range(len(lens))), start, rows, q, None, hd ** -0.5, n / len(rows))
     off = np.abs(vals(out) - want) / tol
