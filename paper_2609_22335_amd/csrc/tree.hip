@@ -180,7 +180,7 @@ struct Run {
 // a few blocks each. deal() finds the tile at r.u; with `first` set it works
 // out the workgroup's run before. Every wave does so for itself; lanes hold
 // 64 entries at a time.
-template <int BM, int BN>
+template <int BM, int BN, int LONG>
 __device__ __forceinline__ Tile deal(Run& r, bool first) {
   const Args& a = fresh();
   const int lane = threadIdx.x & 63, n_ent = a.r.n_ent, nkv = a.c.nkv;
@@ -216,7 +216,11 @@ __device__ __forceinline__ Tile deal(Run& r, bool first) {
     if (c0 < n_ent) continue;
     c0 = 0;
     if (pass == 0 && 2 * tiles <= a.wgs) {
-      per = (int)ceil_div(total, a.wgs - (int)tiles);
+      // (LONG times that where two workgroups of a CU share its matrix cores and
+      // twice the parts are no gain: two sequences of 2,000 slots, trees of 60,
+      // 32 heads on 8 of 128, 23.8 us and 27.0; eight of 4,000, trees of 40, 8
+      // on 1, 27.0 and 28.9, of 64 23.0 and 22.6)
+      per = (int)ceil_div(total, a.wgs - (int)tiles) * LONG;
       // A part of b blocks of the tile's B costs b steps here and the join B / b
       // parts, so b stays at a multiple of sqrt(B) or above. One sequence, 8
       // heads on 1 of 128, with that and without: a token behind 60,000 slots
@@ -676,10 +680,10 @@ __device__ __forceinline__ float inverse(float l) { return l > 0.f || l != l ? 1
 // The workgroup's run of blocks: calls f(tile, slot) for each of its tiles,
 // slot being where a shared tile's part goes; what other workgroups hold of the last one is written down for the
 // join.
-template <int BM, int BN, typename F>
+template <int BM, int BN, int LONG = 1, typename F>
 __device__ __forceinline__ void for_tiles(int wgs, F&& f) {
   Run r;
-  Tile t = deal<BM, BN>(r, true);
+  Tile t = deal<BM, BN, LONG>(r, true);
   int4 desc = make_int4(0, 0, 0, 0), more = desc;
   while (t.b1 > t.b0) {
     if (t.parts) {
@@ -690,7 +694,7 @@ __device__ __forceinline__ void for_tiles(int wgs, F&& f) {
     if (r.u >= r.u_end) break;
     wait_vm<0>();  // no store of this tile in the next one's counts
     __syncthreads();
-    t = deal<BM, BN>(r, false);
+    t = deal<BM, BN, LONG>(r, false);
   }
   if (threadIdx.x == 0) {
     int4* to = fresh().desc + 2 * ((int)(blockIdx.x & 7) * (wgs >> 3) + (int)(blockIdx.x >> 3));  // by XCD
@@ -887,7 +891,7 @@ __global__ __launch_bounds__(256, (many_waves<uint16_t, HDP>())) void k_tree_man
   // it can tell them apart.)
   __shared__ __attribute__((aligned(1024))) unsigned char s0[64 * RB], s1[64 * RB], s2[64 * RB], s3[64 * RB];
   __shared__ int sOdd;
-  for_tiles<BM, BN>(a.wgs, [&](const Tile& t, int slot) {
+  for_tiles<BM, BN, many_waves<T, HDP>()>(a.wgs, [&](const Tile& t, int slot) {
     const int tid = threadIdx.x, lane = tid & 63, wv = uni(tid >> 6), l32 = lane & 31, h = lane >> 5, il = lane & 15;
     if (tid == 0) sOdd = 0;  // (barriers follow)
     Ld ld;
@@ -1313,14 +1317,16 @@ __global__ __launch_bounds__(256) void k_tree_join(Args a) {
 int pad_hd(int dtype, int hd) { return hd <= 64 ? 64 : hd <= 128 ? 128 : 256; }
 
 // Many rows to a sequence (on average more than 128, in fp32 more than 256):
-// tiles of 128 rows, whose waves share K and V. Below that the two are close,
-// and tiles of 32 keep more of the probabilities. Trees over 8 query heads on
-// one KV head, 64, 128, 192 and 256 rows in tiles of 32 / 128: eight caches of
-// 4,000 slots at head dim 128 18.4 / 19.5, 22.1 / 21.1, 25.6 / 24.2 and 27.6 /
-// 25.9 us; two of 30,000 25.9 / 29.9, 32.2 / 31.2, 39.0 / 33.7 and 41.0 / 33.9;
-// eight of 2,000 at head dim 256 23.3 / 19.9, 24.7 / 23.2, 27.7 / 25.5 and
-// 28.8 / 27.3. In fp32, eight of 1,000, 192, 256 and 320 rows: 25.5 / 27.4,
-// 31.8 / 30.4, 37.1 / 34.0; four of 4,000 35.6 / 42.1, 39.2 / 42.7, 44.0 / 50.5.
+// tiles of 128 rows, whose waves share K and V. Below that the two are close
+// (at head dim 256 64 rows 23.3 us in tiles of 32, 19.9 in tiles of 128; at 64
+// 14.1 and 17.7), and tiles of 32 keep more of the probabilities. Trees over 8
+// query heads on one KV head, 160, 192 and 256 rows in tiles of 32 / 128: eight
+// caches of 4,000 slots at head dim 128 23.1 / 21.2, 25.6 / 21.8 and 27.6 /
+// 22.9 us, at 64 17.6 / 19.4, 19.5 / 19.7 and 20.9 / 20.3; two of 30,000 at 128
+// 37.5 / 33.9, 39.0 / 33.6 and 41.0 / 33.7; eight of 2,000 at 256 25.7 / 25.4,
+// 27.7 / 25.7 and 28.8 / 27.4. In fp32, eight of 1,000 at 128, 192, 256 and 320
+// rows: 25.5 / 27.4, 31.8 / 30.4, 37.1 / 34.0; four of 4,000 35.6 / 42.1,
+// 39.2 / 42.7, 44.0 / 50.5.
 int tile_rows(const TreeAttnDesc& d) {
   const long long rows = (long long)d.r.n_rows * (d.nq / d.c.nkv);
   return rows > (d.c.dtype == DT_BF16 ? 128ll : 256ll) * d.r.n_ent ? 128 : 32;
