@@ -1316,10 +1316,10 @@ __global__ __launch_bounds__(256) void k_tree_join(Args a) {
 
 int pad_hd(int dtype, int hd) { return hd <= 64 ? 64 : hd <= 128 ? 128 : 256; }
 
-// Many rows to a sequence (on average more than 128, in fp32 more than 256):
-// tiles of 128 rows, whose waves share K and V. Below that the two are close
-// (at head dim 256 64 rows 23.3 us in tiles of 32, 19.9 in tiles of 128; at 64
-// 14.1 and 17.7), and tiles of 32 keep more of the probabilities. Trees over 8
+// Many rows to a sequence (on average more than 128, at head dims up to 64 more
+// than 192, in fp32 more than 256): tiles of 128 rows, whose waves share K and
+// V. Below that the two are close (at head dim 256 64 rows 23.3 us in tiles of
+// 32, 19.9 in tiles of 128), and tiles of 32 keep more of the probabilities. Trees over 8
 // query heads on one KV head, 160, 192 and 256 rows in tiles of 32 / 128: eight
 // caches of 4,000 slots at head dim 128 23.1 / 21.2, 25.6 / 21.8 and 27.6 /
 // 22.9 us, at 64 17.6 / 19.4, 19.5 / 19.7 and 20.9 / 20.3; two of 30,000 at 128
@@ -1329,7 +1329,8 @@ int pad_hd(int dtype, int hd) { return hd <= 64 ? 64 : hd <= 128 ? 128 : 256; }
 // 39.2 / 42.7, 44.0 / 50.5.
 int tile_rows(const TreeAttnDesc& d) {
   const long long rows = (long long)d.r.n_rows * (d.nq / d.c.nkv);
-  return rows > (d.c.dtype == DT_BF16 ? 128ll : 256ll) * d.r.n_ent ? 128 : 32;
+  const long long many = d.c.dtype == DT_F32 ? 256 : d.c.hd <= 64 ? 192 : 128;
+  return rows > many * d.r.n_ent ? 128 : 32;
 }
 // Workgroups, each with a run of blocks: as many as the CUs hold.
 int tree_wgs(const TreeAttnDesc& d) {
