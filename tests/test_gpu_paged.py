@@ -13,8 +13,9 @@ of it; fp32 sums of n terms by n 2^-24 of the sum of their magnitudes.
   of its magnitude in the exponent), so a weight by a factor of e^(2 ds); the
   two sums over n keys add (n + 16) 2^-24. Every such error moves the result by
   at most itself times sum p |v| (numerator) and |o| <= sum p |v|
-  (denominator). bf16 with more than 128 rows of a KV head to a sequence (on average) rounds the
-  probabilities once: 2^-8 in both sums; with fewer they are kept to 2^-16.
+  (denominator). bf16 with more than 128 rows of a KV head to a sequence (on
+  average; head dims up to 64: 192) rounds the probabilities once: 2^-8 in both
+  sums; with fewer they are kept to 2^-16.
   Then one rounding of the output.
 """
 import numpy as np
@@ -253,7 +254,7 @@ def expect(m, T, layer, order, start, counts, q, bits, scale, mean_rows):
             o, mag = np.matmul(p, v), np.matmul(p, np.abs(v))
             ds = np.where(see, np.matmul(np.abs(x), np.abs(k).T), 0).max(-1, initial=0)[..., None] * scale
             ds = ds * (hd + 4) * 2.0 ** -24
-            one = 0.0 if T is T32 else 2.0 ** -8 if mean_rows * group > 128 else 2.0 ** -16
+            one = 0.0 if T is T32 else 2.0 ** -8 if mean_rows * group > (128 if hd > 64 else 192) else 2.0 ** -16
             rel = np.expm1(2 * ds) + (end + 16) * 2.0 ** -24 + one
             want[a:a + c, h * group:(h + 1) * group] = o
             tol[a:a + c, h * group:(h + 1) * group] = rel * (mag + np.abs(o)) + HALF[T] * np.abs(o) * (1 + rel) + 1e-38
@@ -453,6 +454,63 @@ def test_long_runs(V, T, hd, nq, nkv, page, lens, rows):
     want, tol = expect(m, T, 0, list(range(len(lens))), start, rows, q, None, hd ** -0.5, n / len(rows))
     off = np.abs(vals(out) - want) / tol
     assert np.all(off <= 1), float(np.nanmax(off))
+
+
+@pytest.mark.parametrize("T,rows,nq", [(T16, 3, 4), (T16, 70, 4), (T32, 5, 2), (T32, 80, 4)])
+def test_odd_queries_stay_alone(V, T, rows, nq):
+    """A query that holds NaN or infinities spoils its own row and head only."""
+    say(f"attend with odd queries {T} rows={rows}")
+    rng = np.random.default_rng(rows + 7)
+    hd = 128
+    m = filled(rng, T, [300], [rows], hd=hd, page=32)
+    d = Dev(V, m, T)
+    q = rounded(rng.standard_normal((rows, nq, hd)), T)
+    odd = q.copy()
+    odd[1, 0, 5], odd[2, 1, 9], odd[rows - 1, nq - 1, 0] = np.nan, np.inf, -np.inf
+    r = V.make_rows(i32([0, rows]), rows)
+    out = torch.empty((rows, nq, hd), dtype=T, device="cuda")
+    scratch = torch.empty(V.vla_tree_attention_scratch(d.p, r, nq), dtype=torch.uint8, device="cuda")
+    V.vla_tree_attention(d.p, 0, r, torch.from_numpy(odd).to(T).cuda(), out, scratch)
+    torch.cuda.synchronize()
+    got = vals(out)
+    want, tol = expect(m, T, 0, [0], [0], [rows], q, None, hd ** -0.5, rows)
+    spoilt = ~np.isfinite(odd).all(-1)
+    assert spoilt.sum() == 3 and np.all(np.isnan(got[1, 0]))
+    assert np.all(np.abs(got - want)[~spoilt] <= tol[~spoilt])
+
+
+@pytest.mark.parametrize("T,hd,nq", [(T16, 64, 2), (T16, 128, 24), (T32, 96, 2)])
+def test_rows_outside_the_entries(V, T, hd, nq):
+    """Rows in front of the first entry and behind the last are left alone, and
+    an entry that passes the buffers ends with them."""
+    say(f"rows outside the entries {T} hd={hd}")
+    rng = np.random.default_rng(hd)
+    page, n_rows = 16, 40
+    m = filled(rng, T, [21, 40, 3], [14, 20, 90], hd=hd, page=page)
+    m.k[:], m.v[:] = rounded(m.k, T), rounded(m.v, T)
+    d = Dev(V, m, T)
+    x = rounded(rng.standard_normal((n_rows, nq + 2, hd)), T)
+    qkv = torch.from_numpy(x).to(T).cuda()
+    # entry 0: rows 4 .. 17, entry 1: none, entry 2 (n_rows behind its start 30): rows 30 .. 39
+    for start, live in (([4, 18, 18, 18], {0: (4, 18)}), ([30, 30, 30, 120], {2: (30, 40)}),
+                        ([5, 12, 31, 36], {0: (5, 12), 1: (12, 31), 2: (31, 36)})):
+        r = V.make_rows(i32(start), n_rows)
+        out = torch.full((n_rows, nq, hd), 7.0, dtype=T, device="cuda")
+        scratch = torch.empty(V.vla_tree_attention_scratch(d.p, r, nq), dtype=torch.uint8, device="cuda")
+        V.vla_qk_norm_rope(d.p, 0, r, V.make_rope_norm(), qkv[:, :nq], qkv[:, nq:nq + 1], qkv[:, nq + 1:],
+                           qkv[:, :nq])
+        V.vla_tree_attention(d.p, 0, r, qkv[:, :nq], out, scratch)
+        want = np.full((n_rows, nq, hd), 7.0)
+        tol = np.zeros_like(want)
+        for s, (a, b) in live.items():
+            for t in range(a, b):
+                p, at = m.where(s, int(m.lens[s]) + t - a)
+                m.k[0, p, :, at], m.v[0, p, :, at] = x[t, nq:nq + 1], x[t, nq + 1:]
+        for s, (a, b) in live.items():
+            w, e = expect(m, T, 0, [s], [a], [b - a], x[:, :nq], None, hd ** -0.5, n_rows / 3)
+            want[a:b], tol[a:b] = w[a:b], e[a:b]
+        d.same()
+        assert np.all(np.abs(vals(out) - want) <= tol), start
 
 
 def test_drafts_without_pages_are_not_seen(V):
