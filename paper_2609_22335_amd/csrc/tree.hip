@@ -565,16 +565,21 @@ __device__ __forceinline__ uint32_t odd_bits(uint32_t w, float) {
 }
 template <typename T, int HDP, int PARTS>
 __device__ __forceinline__ bool clean_values(LB* vt, int part) {
-  constexpr int NI = HDP * (int)sizeof(T) * 32 / 1024;
+  constexpr int NI = HDP * (int)sizeof(T) * 32 / 1024, U = NI / PARTS < 4 ? NI / PARTS : 4;
+  LDS_AS u32x4* at = (LDS_AS u32x4*)(vt + part * 1024 + (threadIdx.x & 63) * 16);
   bool odd = false;
 #pragma unroll 1
-  for (int i = part; i < NI; i += PARTS) {
-    LDS_AS u32x4* at = (LDS_AS u32x4*)(vt + i * 1024 + (threadIdx.x & 63) * 16);
-    u32x4 c = *at;
-    const u32x4 b = {odd_bits(c.x, T()), odd_bits(c.y, T()), odd_bits(c.z, T()), odd_bits(c.w, T())};
-    if (b.x | b.y | b.z | b.w) {
-      *at = c & ~b;
-      odd = true;
+  for (int i = 0; i < NI / PARTS; i += U) {
+    u32x4 c[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) c[u] = at[(i + u) * PARTS * 64];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const u32x4 b = {odd_bits(c[u].x, T()), odd_bits(c[u].y, T()), odd_bits(c[u].z, T()), odd_bits(c[u].w, T())};
+      if (b.x | b.y | b.z | b.w) {
+        at[(i + u) * PARTS * 64] = c[u] & ~b;
+        odd = true;
+      }
     }
   }
   return __any(odd);
@@ -722,7 +727,8 @@ __global__ __launch_bounds__(256, (many_waves<T, HDP>())) void k_tree_few(Args a
   static_assert(2 * Ld::NI < 60, "loads in flight");
   __shared__ __attribute__((aligned(1024))) unsigned char sK[4][32 * RB];
   __shared__ __attribute__((aligned(1024))) unsigned char sV[4][32 * RB];
-  __shared__ float sM[4][32], sL[4][32];
+  __shared__ float sM[4][32], sL[4][32], sF[4][32];
+  __shared__ long long sAt[32];
   for_tiles<BM, BN>(a.wgs, [&](const Tile& t, int slot) {
     const int tid = threadIdx.x, lane = tid & 63, wv = uni(tid >> 6), l32 = lane & 31, h = lane >> 5;
     Ld ld;
@@ -750,7 +756,8 @@ __global__ __launch_bounds__(256, (many_waves<T, HDP>())) void k_tree_few(Args a
     wait_vm<0>();  // (the first block waits for the query as well)
     for (int b = t.b0; b < t.b1; ++b) {
       const int kb = b * BN + wv * 32;
-      const bool more = b + 1 < t.b1;
+      const bool more = b + 1 < t.b1, masked = kb + 32 > safe;
+      const uint32_t see = masked ? seen_bits(t, kb, own, row) : 0u;
       if (b > t.b0) wait_vm<Ld::NI>();  // K is here, V may be on its way
       f32x16 s[1];
       scores<T, HDP, 1, NQ>(kl, qf, s);
@@ -759,8 +766,7 @@ __global__ __launch_bounds__(256, (many_waves<T, HDP>())) void k_tree_few(Args a
         ld.look(kb + BN, at);
         ld.issue(a.k, kl, at, 0);
       }
-      const bool masked = kb + 32 > safe;
-      if (masked) hide(s[0], seen_bits(t, kb, own, row));
+      if (masked) hide(s[0], see);
       soften<NDT, 1>(s, a.c2, mx, l, o);
       Probs p[1];
       if constexpr (sizeof(T) == 2) round_probs(s[0], p[0]);
@@ -783,12 +789,13 @@ __global__ __launch_bounds__(256, (many_waves<T, HDP>())) void k_tree_few(Args a
         if (kb + 32 > safe) add_odd_values<T, HDP>(t, kb, seen_bits(t, kb, own, row), o);
       }
     // the four waves' results: each puts its own into the LDS (columns of the
-    // first half where K was, the others where V was), then 256 threads add
-    // four columns of a row each
-    constexpr int HC = HDP / 2;
+    // first half where K was, the others where V was), two waves work out what
+    // each counts for, then 256 threads add four columns of a row each, four
+    // rows' reads out at once
+    constexpr int HC = HDP / 2, CG = HDP / 4;
     const int rows = t.M - t.rt * BM < 32 ? t.M - t.rt * BM : 32;
-    barrier();  // (every wave is done with K and V)
     if (h == 0) sM[wv][l32] = mx, sL[wv][l32] = l;
+    barrier();  // (every wave is done with K and V)
     if (l32 < rows) {
 #pragma unroll
       for (int dt = 0; dt < NDT; ++dt) {
@@ -801,28 +808,54 @@ __global__ __launch_bounds__(256, (many_waves<T, HDP>())) void k_tree_few(Args a
         }
       }
     }
-    barrier();
     const Args& z = fresh();
-#pragma unroll 1
-    for (int i = tid; i < rows * (HDP / 4); i += 256) {
-      const int lm = i / (HDP / 4), col = i % (HDP / 4) * 4, c4 = col % HC / 4;
-      const LDS_AS float* so = col < HC ? (const LDS_AS float*)sK : (const LDS_AS float*)sV;
-      const float top = fmaxf(fmaxf(sM[0][lm], sM[1][lm]), fmaxf(sM[2][lm], sM[3][lm]));
-      float v[4] = {0.f, 0.f, 0.f, 0.f}, den = 0.f;
+    float* pm = z.part + 2ll * z.wgs * BM * HDP + (size_t)slot * BM * 2;
+    if (tid < 128) {
+      const int k = tid >> 5, r = tid & 31;
+      const float top = fmaxf(fmaxf(sM[0][r], sM[1][r]), fmaxf(sM[2][r], sM[3][r]));
+      float den = 0.f, mine = 0.f;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const float f = sM[k][lm] == -INFINITY ? 0.f : ex2(sM[k][lm] - top);
-        const f32x4 y = *(const LDS_AS f32x4*)(so + ((k * 32 + lm) * HC) + ((c4 ^ (lm & 7)) * 4));
-#pragma unroll
-        for (int u = 0; u < 4; ++u) v[u] = __builtin_fmaf(f, y[u], v[u]);
-        den = __builtin_fmaf(f, sL[k][lm], den);
+      for (int i = 0; i < 4; ++i) {
+        const float f = sM[i][r] == -INFINITY ? 0.f : ex2(sM[i][r] - top);
+        den = __builtin_fmaf(f, sL[i][r], den);
+        mine = i == k ? f : mine;
       }
-      if (t.whole) {
-        if (col < z.c.hd) put4<T>(out_row<T>(z, t, t.rt * BM + lm) + col, inverse(den), v);
-      } else {
-        float* pm = z.part + 2ll * z.wgs * BM * HDP + (size_t)slot * BM * 2;
-        *(f32x4*)(z.part + ((size_t)slot * BM + lm) * HDP + col) = f32x4{v[0], v[1], v[2], v[3]};
-        if (col == 0) pm[2 * lm] = top, pm[2 * lm + 1] = den;
+      sF[k][r] = t.whole ? mine * inverse(den) : mine;
+      if (k == 0) {
+        if (t.whole) {
+          const int mm = t.rt * BM + r, tk = mm / t.group;
+          sAt[r] = (long long)(t.row0 + tk) * z.ldo + (long long)(t.head * t.group + (mm - tk * t.group)) * z.c.hd;
+        } else if (r < rows) {
+          pm[2 * r] = top, pm[2 * r + 1] = den;
+        }
+      }
+    }
+    barrier();
+    const int total = rows * CG;
+#pragma unroll 1
+    for (int i0 = tid; i0 < total; i0 += 1024) {
+      f32x4 y[4][4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int i = i0 + 256 * u < total ? i0 + 256 * u : i0, lm = i / CG, c4 = i % CG;
+        const LDS_AS float* so = c4 < CG / 2 ? (const LDS_AS float*)sK : (const LDS_AS float*)sV;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          y[u][k] = *(const LDS_AS f32x4*)(so + ((k * 32 + lm) * HC) + (((c4 % (CG / 2)) ^ (lm & 7)) * 4));
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int i = i0 + 256 * u, lm = i / CG, col = i % CG * 4;
+        if (i >= total) break;
+        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v += sF[k][lm] * y[u][k];
+        if (t.whole) {
+          const float w[4] = {v.x, v.y, v.z, v.w};
+          if (col < z.c.hd) put4<T>((T*)z.out + sAt[lm] + col, 1.f, w);
+        } else {
+          *(f32x4*)(z.part + ((size_t)slot * BM + lm) * HDP + col) = v;
+        }
       }
     }
   });
@@ -959,8 +992,8 @@ __global__ __launch_bounds__(256, (many_waves<uint16_t, HDP>())) void k_tree_man
       vf[kk][dt] = u32x4{u0.x, u0.y, u1.x, u1.y};
     };
     auto fence = [&] { __builtin_amdgcn_sched_barrier(0); };
-    auto cover = [&](int b, f32x16& x) {  // scores of block b that their rows do not see
-      hide(x, seen_bits(t, b * BN, own, row));
+    auto cover = [&](f32x16& x, uint32_t see) {  // scores that their rows do not see
+      hide(x, see);
       bm = x[0];
 #pragma unroll
       for (int j = 1; j < 16; ++j) bm = fmaxf(bm, x[j]);
@@ -996,6 +1029,8 @@ __global__ __launch_bounds__(256, (many_waves<uint16_t, HDP>())) void k_tree_man
       constexpr int P = decltype(phase)::value, JQ = 12;
       const LB *st = stage(P + 1), *sn = stage(P + 2);
       f32x16 &cur = s[P & 1], &nxt = s[(P + 1) & 1];
+      const bool hidden = (b + 2) * BN > safe;
+      const uint32_t see = hidden ? seen_bits(t, (b + 1) * BN, own, row) : 0u;  // (its loads are out early)
       if ((b + 1) * BN > safe) {
         if (clean_values<T, HDP, 4>((LB*)st + 32 * RB, wv)) sOdd = 1;
         wait_lds();
@@ -1034,7 +1069,7 @@ __global__ __launch_bounds__(256, (many_waves<uint16_t, HDP>())) void k_tree_man
         asm volatile("" : "+v"(bm));
         fence();
       }
-      if ((b + 2) * BN > safe) cover(b + 1, nxt);
+      if (hidden) cover(nxt, see);
       if (!PAIR && b + 1 < t.b1) raise();
     };
     // the first block's scores
@@ -1053,7 +1088,7 @@ __global__ __launch_bounds__(256, (many_waves<uint16_t, HDP>())) void k_tree_man
     bm = s[0][0];
 #pragma unroll
     for (int j = 1; j < 16; ++j) bm = fmaxf(bm, s[0][j]);
-    if ((t.b0 + 1) * BN > safe) cover(t.b0, s[0]);
+    if ((t.b0 + 1) * BN > safe) cover(s[0], seen_bits(t, t.b0 * BN, own, row));
     if (!PAIR) raise();
     for (int b = t.b0;; b += 4) {
       if (((b - t.b0) & 31) == 28) window(b + 4);
