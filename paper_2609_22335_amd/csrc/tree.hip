@@ -161,6 +161,7 @@ struct Tile {
   int seq, row0, len, head, rt;
   int b0, b1;         // blocks of the tile to work on
   int M, group, kend;
+  int n, cap;         // (of its entry)
   int parts;          // with the first of several parts: how many, else 0
   bool whole, causal;
 };
@@ -170,6 +171,32 @@ struct Run {
   int w;               // this run (behind the last: none)
   int per;             // blocks of a unit
 };
+
+// The run's part of tile rt, from unit u0 of its nu on.
+template <int BM, int BN>
+__device__ __forceinline__ Tile cut(Run& r, const Geo<BM>& g, const Entry& x, int head, int rt, int u0, int nu,
+                                    bool causal) {
+  const int u1 = (int)(nu - u0 < r.u_end - r.u ? nu : u0 + (r.u_end - r.u));
+  Tile t{};
+  t.head = head;
+  t.rt = rt;
+  t.seq = x.seq;
+  t.row0 = x.row0;
+  t.n = x.n;
+  t.cap = x.cap;
+  t.len = x.len;
+  t.M = g.M;
+  t.group = g.group;
+  t.causal = causal;
+  t.kend = g.tile_end(rt);
+  t.b0 = u0 * r.per;
+  const int nb = t.kend > 0 ? (t.kend + BN - 1) / BN : 1;
+  t.b1 = u1 * r.per < nb ? u1 * r.per : nb;
+  t.whole = u0 == 0 && u1 == nu;
+  t.parts = t.whole || u0 > 0 ? 0 : (int)(r.quota == 1 ? r.u + nu - 1 : (r.u + nu - 1) / r.quota) - r.w + 1;
+  r.u += u1 - u0;
+  return t;
+}
 
 // All entries' units stand in a row and are dealt out in equal runs, so that
 // uneven sequences load the chip evenly. A unit is a block of keys of a tile,
@@ -260,32 +287,29 @@ __device__ __forceinline__ Tile deal(Run& r, bool first) {
   persum = __builtin_amdgcn_readlane(persum, el);
   const long long at = r.u - (base + lane_of(incl, el) - lane_of(units, el));
   g.set(a.group, causal, x, BN * per);
-  Tile t{};
   // (a head's units fit 31 bits; most entries' do as well. Divisions are long,
   // and a short call waits for each: one head and one tile need none.)
-  t.head = nkv == 1 ? 0 : at >> 31 ? (int)(at / persum) : (int)((uint32_t)at / (uint32_t)persum);
-  const int rem = (int)(at - (long long)t.head * persum);
-  int u0 = rem, nu = persum;
+  const int head = nkv == 1 ? 0 : at >> 31 ? (int)(at / persum) : (int)((uint32_t)at / (uint32_t)persum);
+  const int rem = (int)(at - (long long)head * persum);
+  int rt = 0, u0 = rem, nu = persum;
   if (g.tiles > 1) {
-    t.rt = g.find(rem);
-    u0 = rem - g.before(t.rt);
-    nu = g.units(t.rt);
+    rt = g.find(rem);
+    u0 = rem - g.before(rt);
+    nu = g.units(rt);
   }
-  const int u1 = (int)(nu - u0 < r.u_end - r.u ? nu : u0 + (r.u_end - r.u));
-  t.seq = x.seq;
-  t.row0 = x.row0;
-  t.len = x.len;
-  t.M = g.M;
-  t.group = g.group;
-  t.causal = causal;
-  t.kend = g.tile_end(t.rt);
-  t.b0 = u0 * per;
-  const int nb = t.kend > 0 ? (t.kend + BN - 1) / BN : 1;
-  t.b1 = u1 * per < nb ? u1 * per : nb;
-  t.whole = u0 == 0 && u1 == nu;
-  t.parts = t.whole || u0 > 0 ? 0 : (int)(r.quota == 1 ? r.u + nu - 1 : (r.u + nu - 1) / r.quota) - r.w + 1;
-  r.u += u1 - u0;
-  return t;
+  return cut<BM, BN>(r, g, x, head, rt, u0, nu, causal);
+}
+// The tile behind t in the run, which holds it from its first unit on: the
+// next of its head, or of the next head, or what deal() finds.
+template <int BM, int BN, int LONG>
+__device__ __forceinline__ Tile next(Run& r, const Tile& t) {
+  const Entry x = {t.seq, t.row0, t.n, t.len, t.cap};
+  Geo<BM> g;
+  g.set(t.group, t.causal, x, BN * r.per);
+  const bool same = t.rt + 1 < g.tiles;
+  const int head = same ? t.head : t.head + 1, rt = same ? t.rt + 1 : 0;
+  if (head >= fresh().c.nkv) return deal<BM, BN, LONG>(r, false);
+  return cut<BM, BN>(r, g, x, head, rt, 0, g.units(rt), t.causal);
 }
 __device__ __forceinline__ int uni(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
@@ -699,7 +723,7 @@ __device__ __forceinline__ void for_tiles(int wgs, F&& f) {
     if (r.u >= r.u_end) break;
     wait_vm<0>();  // no store of this tile in the next one's counts
     __syncthreads();
-    t = deal<BM, BN, LONG>(r, false);
+    t = next<BM, BN, LONG>(r, t);
   }
   if (threadIdx.x == 0) {
     int4* to = fresh().desc + 2 * ((int)(blockIdx.x & 7) * (wgs >> 3) + (int)(blockIdx.x >> 3));  // by XCD
