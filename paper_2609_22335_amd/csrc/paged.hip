@@ -30,7 +30,8 @@ constexpr long long MANY_WAVES = 4096;
 // before it looks for the row's sequence (four dependent round trips), and
 // stores pass the L2 by when there are many rows. With many rows a wave takes
 // three groups of heads, so that its look-ups are paid for more bytes; with
-// few, one, so that more waves share the latency.
+// few, one, so that more waves share the latency. 16,000 rows of 48 heads of 128
+// (394 MB): 72 us, 5.4 TB/s.
 template <typename T, int LPH, int U>
 __global__ __launch_bounds__(256) void k_rope_norm(RopeNormDesc d, int parts) {
   constexpr int VEC = El<T>::VEC, HPW = 64 / LPH;
@@ -432,7 +433,8 @@ __global__ __launch_bounds__(PT) void k_pages_fork(PagedCache c, int n, const in
 
 // Fork, second half: the used slots of the last page, K and V of FORK_HEADS
 // heads (of all layers) to a workgroup, so that the descriptors' round trips
-// are paid for more bytes.
+// are paid for more bytes. Bound by memory: 64 children, 306 MB in 54 us, 5.6
+// TB/s (72 us with stores through the L2).
 constexpr int FORK_HEADS = 4;
 __global__ __launch_bounds__(256) void k_pages_copy(PagedCache c, const int32_t* src, const int32_t* dst,
                                                     const int32_t* made, int esz, int groups) {
@@ -538,7 +540,8 @@ __device__ __forceinline__ void grow(const PagedCache& c, const Entry& x, int a,
 // column of one layer's K or V head and takes the drafts in order: a list
 // ascends, so kept[j] >= j and no draft is written over before it is read
 // (groups are read whole before they are written). With one workgroup to an
-// entry (gridDim.y 1) it sets the new length as well.
+// entry (gridDim.y 1) it sets the new length as well. Bound by memory: 64
+// entries' drafts, 89 MB in 19 us; few by seven dependent round trips, 7 us.
 constexpr int KMOVE = 256;  // drafts whose places are worked out at a time
 __global__ __launch_bounds__(1024) void k_pages_move(PagedCache c, PagedRows r, const int32_t* kept,
                                                      const int32_t* n_kept, int cpr, int esz) {
@@ -639,7 +642,8 @@ hipError_t launch_pages_commit(const PagedCache& c, const PagedRows& r, const in
 // A thread takes VEC keys by VEC head-dim elements: K's 16-byte runs lie along
 // the head dim as the pages' do, V's along the keys, so V is turned in
 // registers. 256 threads cover the elements of VEC keys first, so that rows are
-// written in one piece.
+// written in one piece. 305 rows of 256 in 18 layers, 11.2 MB: 7 us, the
+// latency of its look-ups; once a frame.
 template <typename T>
 __global__ __launch_bounds__(256) void k_ctx_to_pages(PagedCache c, const T* k, const T* v, size_t lk, size_t lv, int nb,
                                                       int rows, int seq) {
