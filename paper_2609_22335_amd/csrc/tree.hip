@@ -243,11 +243,14 @@ __device__ __forceinline__ Tile deal(Run& r, bool first) {
     if (c0 < n_ent) continue;
     c0 = 0;
     if (pass == 0 && 2 * tiles <= a.wgs) {
-      // (LONG times that where two workgroups of a CU share its matrix cores and
-      // twice the parts are no gain: two sequences of 2,000 slots, trees of 60,
-      // 32 heads on 8 of 128, 23.8 us and 27.0; eight of 4,000, trees of 40, 8
-      // on 1, 27.0 and 28.9, of 64 23.0 and 22.6)
-      per = (int)ceil_div(total, a.wgs - (int)tiles) * LONG;
+      per = (int)ceil_div(total, a.wgs - (int)tiles);
+      // LONG times that where two workgroups of a CU share its matrix cores and
+      // an average tile still makes four parts: two sequences of 2,000 slots,
+      // trees of 60, 32 heads on 8 of 128, 23.8 us and 27.0; eight of 4,000,
+      // trees of 40, 8 on 1, 27.0 and 28.9, of 64 23.0 and 22.6. With fewer parts
+      // whole CUs would wait: ten uneven sequences of 500 to 8,000, 32 on 8 of
+      // 128, 126 us so and 81.
+      if (LONG > 1 && (float)per * (float)(4 * LONG) * (float)tiles <= (float)total) per *= LONG;
       // A part of b blocks of the tile's B costs b steps here and the join B / b
       // parts, so b stays at a multiple of sqrt(B) or above. One sequence, 8
       // heads on 1 of 128, with that and without: a token behind 60,000 slots
@@ -1380,15 +1383,15 @@ int pad_hd(int dtype, int hd) { return hd <= 64 ? 64 : hd <= 128 ? 128 : 256; }
 
 // Many rows to a sequence (on average more than 128, at head dims up to 64 more
 // than 192, in fp32 more than 256): tiles of 128 rows, whose waves share K and
-// V. Below that the two are close (at head dim 256 64 rows 23.3 us in tiles of
-// 32, 19.9 in tiles of 128), and tiles of 32 keep more of the probabilities. Trees over 8
-// query heads on one KV head, 160, 192 and 256 rows in tiles of 32 / 128: eight
-// caches of 4,000 slots at head dim 128 23.1 / 21.2, 25.6 / 21.8 and 27.6 /
-// 22.9 us, at 64 17.6 / 19.4, 19.5 / 19.7 and 20.9 / 20.3; two of 30,000 at 128
-// 37.5 / 33.9, 39.0 / 33.6 and 41.0 / 33.7; eight of 2,000 at 256 25.7 / 25.4,
-// 27.7 / 25.7 and 28.8 / 27.4. In fp32, eight of 1,000 at 128, 192, 256 and 320
-// rows: 25.5 / 27.4, 31.8 / 30.4, 37.1 / 34.0; four of 4,000 35.6 / 42.1,
-// 39.2 / 42.7, 44.0 / 50.5.
+// V. Below that the two are close (at head dim 256 64 rows 22.3 us in tiles of
+// 32, 19.8 in tiles of 128), and tiles of 32 keep more of the probabilities.
+// Trees over 8 query heads on one KV head, 160, 192 and 256 rows in tiles of
+// 32 / 128: eight caches of 4,000 slots at head dim 128 22.8 / 21.3, 25.5 / 21.7
+// and 27.7 / 23.0 us, at 64 18.1 / 19.8, 20.0 / 19.9 and 21.5 / 20.3; two of
+// 30,000 at 128 36.7 / 34.1, 38.5 / 33.8 and 41.6 / 34.1; eight of 2,000 at 256
+// 25.1 / 25.0, 27.0 / 25.3 and 28.3 / 27.6. In fp32, eight of 1,000 at 128, 192,
+// 256 and 320 rows: 24.8 / 27.3, 30.6 / 29.8, 36.9 / 34.0; four of 4,000 34.9 /
+// 42.1, 39.3 / 43.0, 44.6 / 50.3.
 int tile_rows(const TreeAttnDesc& d) {
   const long long rows = (long long)d.r.n_rows * (d.nq / d.c.nkv);
   const long long many = d.c.dtype == DT_F32 ? 256 : d.c.hd <= 64 ? 192 : 128;
