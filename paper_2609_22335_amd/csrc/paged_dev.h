@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "deal.h"
 #include "kernels.h"
 #include "paged.h"
 
@@ -92,13 +93,6 @@ __device__ __forceinline__ int wave_find(const int32_t* start, int n, int t) {
   return lo + __popcll(__ballot(lane < len && start[lo + (lane < len ? lane + 1 : len)] <= t));
 }
 
-// What an entry of a batch is: its sequence (-1: none), first row, rows,
-// committed slots and the slots that its pages hold. Rows and slots are
-// clamped so that whatever the arrays hold, rows lie in [0, n_rows) and slots
-// in the table.
-struct Entry {
-  int seq, row0, n, len, cap;
-};
 __device__ __forceinline__ Entry entry_of(const PagedCache& c, const PagedRows& r, int e) {
   // (every load is issued at once: an entry without a sequence reads the first)
   const int q = r.seqs ? r.seqs[e] : e;

@@ -74,245 +74,56 @@ __device__ __forceinline__ const Args& fresh() {
   return *(const Args*)p;
 }
 
-// sum over i < n of floor((a i + b) / m), by Euclid's steps
-__device__ __forceinline__ uint32_t floor_sum(uint32_t n, uint32_t m, uint32_t a, uint32_t b) {
-  uint32_t sum = 0;
-  while (n > 0) {
-    if (a >= m) {
-      sum += (uint32_t)((unsigned long long)(n - 1) * n / 2) * (a / m);
-      a %= m;
-    }
-    if (b >= m) {
-      sum += n * (b / m);
-      b %= m;
-    }
-    const uint32_t y = a * n + b;
-    if (y < m) break;
-    n = y / m;
-    b = y % m;
-    const uint32_t t = m;
-    m = a;
-    a = t;
-  }
-  return sum;
-}
-
-// The tiles of an entry and one KV head: BM rows by units of `unit` keys. A
-// causal tile ends with its last row's own slot, so tile rt has
-// ceil((len + 1 + floor((BM (rt + 1) - 1) / group)) / unit) units, which is
-// floor((BM rt + BM - 1 + group (len + unit)) / (group unit)).
-template <int BM>
-struct Geo {
-  int tiles, M, group, len, end, unit;
-  bool flat;  // every tile reads all keys
-  __device__ __forceinline__ void set(int group_, bool causal, const Entry& x, int unit_) {
-    group = group_;
-    unit = unit_;
-    M = x.n * group;
-    tiles = (M + BM - 1) / BM;
-    len = x.len;
-    const long long e = (long long)x.len + x.n;
-    end = e < x.cap ? (int)e : x.cap;
-    flat = !causal || e > x.cap;  // (drafts without pages: no row sees them)
-  }
-  // (a tile without keys has one unit, which writes its zeros)
-  __device__ __forceinline__ int all() const { return end > 0 ? (end + unit - 1) / unit : 1; }
-  __device__ __forceinline__ int tile_end(int rt) const {
-    if (flat) return end;
-    const int last = (rt + 1) * BM < M ? (rt + 1) * BM - 1 : M - 1;
-    return len + last / group + 1;
-  }
-  __device__ __forceinline__ int units(int rt) const { return flat ? all() : (tile_end(rt) + unit - 1) / unit; }
-  // units of the tiles before rt (rt < tiles)
-  __device__ __forceinline__ int before(int rt) const {
-    if (flat) return rt * all();
-    return (int)floor_sum(rt, group * unit, BM, BM - 1 + group * (len + unit));
-  }
-  __device__ __forceinline__ int sum() const { return tiles == 0 ? 0 : before(tiles - 1) + units(tiles - 1); }
-  // the tile that holds unit u of the head's: units grow by a line, their sum
-  // by a parabola, whose root is close
-  __device__ __forceinline__ int find(int u) const {
-    if (flat) return u / all();
-    if (tiles <= 1) return 0;
-    const float first = (float)units(0), grow = (float)(units(tiles - 1) - units(0)) / (float)(tiles - 1);
-    const float h = first - 0.5f * grow;
-    int rt = grow > 0.f ? (int)((sqrtf(h * h + 2.f * grow * (float)u) - h) / grow) : (int)((float)u / first);
-    rt = rt < 0 ? 0 : rt > tiles - 1 ? tiles - 1 : rt;
-    while (rt > 0 && before(rt) > u) --rt;
-    while (rt + 1 < tiles && before(rt + 1) <= u) ++rt;
-    return rt;
-  }
-};
-
 __device__ __forceinline__ long long lane_of(long long v, int i) {
   const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)v, i);
   const uint32_t hi = __builtin_amdgcn_readlane((int)(v >> 32), i);
   return (long long)(((unsigned long long)hi << 32) | lo);
 }
 
-// (64-bit divisions are long: most counts are short)
-__device__ __forceinline__ long long ceil_div(long long a, int b) {
-  return a >> 31 ? (a + b - 1) / b : (long long)(((uint32_t)a + (uint32_t)b - 1) / (uint32_t)b);
-}
-
-// What a wave knows of its workgroup's run and of the tile it works on: the
-// same in every lane.
-struct Tile {
-  int seq, row0, len, head, rt;
-  int b0, b1;         // blocks of the tile to work on
-  int M, group, kend;
-  int n, cap;         // (of its entry)
-  int parts;          // with the first of several parts: how many, else 0
-  bool whole, causal;
-};
-struct Run {
-  long long u, u_end;  // this run's next and last unit
-  long long quota;     // units of a run
-  int w;               // this run (behind the last: none)
-  int per;             // blocks of a unit
-};
-
-// The run's part of tile rt, from unit u0 of its nu on.
-template <int BM, int BN>
-__device__ __forceinline__ Tile cut(Run& r, const Geo<BM>& g, const Entry& x, int head, int rt, int u0, int nu,
-                                    bool causal) {
-  const int u1 = (int)(nu - u0 < r.u_end - r.u ? nu : u0 + (r.u_end - r.u));
-  Tile t{};
-  t.head = head;
-  t.rt = rt;
-  t.seq = x.seq;
-  t.row0 = x.row0;
-  t.n = x.n;
-  t.cap = x.cap;
-  t.len = x.len;
-  t.M = g.M;
-  t.group = g.group;
-  t.causal = causal;
-  t.kend = g.tile_end(rt);
-  t.b0 = u0 * r.per;
-  const int nb = t.kend > 0 ? (t.kend + BN - 1) / BN : 1;
-  t.b1 = u1 * r.per < nb ? u1 * r.per : nb;
-  t.whole = u0 == 0 && u1 == nu;
-  t.parts = t.whole || u0 > 0 ? 0 : (int)(r.quota == 1 ? r.u + nu - 1 : (r.u + nu - 1) / r.quota) - r.w + 1;
-  r.u += u1 - u0;
-  return t;
-}
-
-// All entries' units stand in a row and are dealt out in equal runs, so that
-// uneven sequences load the chip evenly. A unit is a block of keys of a tile,
-// and a run may begin and end inside tiles: at most two of its tiles are
-// shared with other runs. Where there are few tiles (at most half as many as
-// workgroups), a unit is as many blocks of one tile as give every workgroup at
-// most one unit: a run that crossed into another tile would start twice for
-// a few blocks each. deal() finds the tile at r.u; with `first` set it works
-// out the workgroup's run before. Every wave does so for itself; lanes hold
-// 64 entries at a time.
-template <int BM, int BN, int LONG>
-__device__ __forceinline__ Tile deal(Run& r, bool first) {
-  const Args& a = fresh();
-  const int lane = threadIdx.x & 63, n_ent = a.r.n_ent, nkv = a.c.nkv;
-  const bool causal = a.mask == nullptr;
+// A wave's entries for deal(), one a lane.
+template <int BM>
+struct Lanes {
+  const Args& a;
   Entry x;
   Geo<BM> g;
   int persum;
-  long long units, incl, base = 0, total = 0;
-  // One loop over the entries, in passes: 0 counts blocks and tiles, 1 counts
-  // units of several blocks, 2 finds the unit. (One copy of the code: what a
-  // short call waits for most is instructions.)
-  int pass = first ? 0 : 2, per = first ? 1 : r.per;
-  long long tiles = 0;
-  for (int c0 = 0;;) {
-    if (c0 == 0 ? pass == 0 || pass == 2 : true) {
-      x = Entry{-1, 0, 0, 0, 0};
-      if (c0 + lane < n_ent) x = entry_of(a.c, a.r, c0 + lane);
-    }
-    g.set(a.group, causal, x, BN * per);
+  long long all, incl;
+
+  static __device__ __forceinline__ float root(float v) { return __builtin_amdgcn_sqrtf(v); }
+  __device__ __forceinline__ void load(int c0) {
+    const int i = c0 + (int)(threadIdx.x & 63);
+    x = Entry{-1, 0, 0, 0, 0};
+    if (i < a.r.n_ent) x = entry_of(a.c, a.r, i);
+  }
+  __device__ __forceinline__ long long count(bool causal, int unit) {
+    g.set(a.group, causal, x, unit);
     persum = g.sum();
-    units = (long long)persum * nkv;
-    incl = wave_scan(units);
-    const long long all = lane_of(incl, 63);
-    if (pass == 2) {
-      if (r.u < base + all) break;
-      base += all;
-      c0 += 64;
-      continue;
-    }
-    total += all;
-    if (pass == 0) tiles += (long long)__builtin_amdgcn_readlane(wave_scan(g.tiles), 63) * nkv;
-    c0 += 64;
-    if (c0 < n_ent) continue;
-    c0 = 0;
-    if (pass == 0 && 2 * tiles <= a.wgs) {
-      per = (int)ceil_div(total, a.wgs - (int)tiles);
-      // LONG times that where two workgroups of a CU share its matrix cores and
-      // an average tile still makes four parts: two sequences of 2,000 slots,
-      // trees of 60, 32 heads on 8 of 128, 23.8 us and 27.0; eight of 4,000,
-      // trees of 40, 8 on 1, 27.0 and 28.9, of 64 23.0 and 22.6. With fewer parts
-      // whole CUs would wait: ten uneven sequences of 500 to 8,000, 32 on 8 of
-      // 128, 126 us so and 81.
-      if (LONG > 1 && (float)per * (float)(4 * LONG) * (float)tiles <= (float)total) per *= LONG;
-      // A part of b blocks of the tile's B costs b steps here and the join B / b
-      // parts, so b stays at a multiple of sqrt(B) or above. One sequence, 8
-      // heads on 1 of 128, with that and without: a token behind 60,000 slots
-      // 24.9 us and 44.8; trees of 24 behind 8,000 28.8 us and 73.8, behind
-      // 60,000 50.5 us and 78.1.
-      constexpr float C = BM == 32 ? 16.f : 4.f;
-      if ((float)per * (float)per * (C * (float)tiles) < (float)total)
-        per = (int)ceilf(__builtin_amdgcn_sqrtf((float)total / (C * (float)tiles)));
-      pass = 1;
-      if (per > 1) {
-        total = 0;
-        continue;
-      }
-      per = 1;
-    }
-    r.per = per;
-    r.quota = pass == 1 || total <= a.wgs ? 1 : ceil_div(total, a.wgs);
-    // Workgroups go round the eight XCDs: each XCD takes an eighth of the runs,
-    // consecutive ones, so that its L2 serves K and V of neighbouring tiles
-    // once (and the join what was written there), and few runs still use every
-    // XCD's share of the memory.
-    const int runs = r.quota == 1 ? (int)total : (int)ceil_div(total, (int)r.quota), share = (runs + 7) >> 3;
-    const int i = (int)(blockIdx.x >> 3);
-    r.w = i < share ? (int)(blockIdx.x & 7) * share + i : a.wgs;
-    r.u = r.w * r.quota;
-    r.u_end = r.u + r.quota < total ? r.u + r.quota : total;
-    if (r.u >= r.u_end) return Tile{};
-    if (n_ent <= 64) break;
-    pass = 2;
+    all = (long long)persum * a.c.nkv;
+    incl = wave_scan(all);
+    return lane_of(incl, 63);
   }
-  const int el = __ffsll(__ballot(base + incl > r.u)) - 1;
-  x.seq = __builtin_amdgcn_readlane(x.seq, el);
-  x.row0 = __builtin_amdgcn_readlane(x.row0, el);
-  x.n = __builtin_amdgcn_readlane(x.n, el);
-  x.len = __builtin_amdgcn_readlane(x.len, el);
-  x.cap = __builtin_amdgcn_readlane(x.cap, el);
-  persum = __builtin_amdgcn_readlane(persum, el);
-  const long long at = r.u - (base + lane_of(incl, el) - lane_of(units, el));
-  g.set(a.group, causal, x, BN * per);
-  // (a head's units fit 31 bits; most entries' do as well. Divisions are long,
-  // and a short call waits for each: one head and one tile need none.)
-  const int head = nkv == 1 ? 0 : at >> 31 ? (int)(at / persum) : (int)((uint32_t)at / (uint32_t)persum);
-  const int rem = (int)(at - (long long)head * persum);
-  int rt = 0, u0 = rem, nu = persum;
-  if (g.tiles > 1) {
-    rt = g.find(rem);
-    u0 = rem - g.before(rt);
-    nu = g.units(rt);
+  __device__ __forceinline__ long long tiles() { return __builtin_amdgcn_readlane(wave_scan(g.tiles), 63); }
+  __device__ __forceinline__ int at(long long u) { return __ffsll(__ballot(incl > u)) - 1; }
+  __device__ __forceinline__ Entry entry(int l) {
+    return Entry{__builtin_amdgcn_readlane(x.seq, l), __builtin_amdgcn_readlane(x.row0, l),
+                 __builtin_amdgcn_readlane(x.n, l), __builtin_amdgcn_readlane(x.len, l),
+                 __builtin_amdgcn_readlane(x.cap, l)};
   }
-  return cut<BM, BN>(r, g, x, head, rt, u0, nu, causal);
+  __device__ __forceinline__ int units(int l) { return __builtin_amdgcn_readlane(persum, l); }
+  __device__ __forceinline__ long long before(int l) { return lane_of(incl, l) - lane_of(all, l); }
+};
+template <int BM, int BN, int LONG>
+__device__ __forceinline__ Tile dealt(Run& r, bool first) {
+  const Args& a = fresh();
+  Lanes<BM> lanes{a};
+  return deal<BM, BN, LONG>(r, first, Batch{a.r.n_ent, a.c.nkv, a.group, a.wgs, a.mask == nullptr}, (int)blockIdx.x,
+                            lanes);
 }
-// The tile behind t in the run, which holds it from its first unit on: the
-// next of its head, or of the next head, or what deal() finds.
+// The tile behind t in the run.
 template <int BM, int BN, int LONG>
 __device__ __forceinline__ Tile next(Run& r, const Tile& t) {
-  const Entry x = {t.seq, t.row0, t.n, t.len, t.cap};
-  Geo<BM> g;
-  g.set(t.group, t.causal, x, BN * r.per);
-  const bool same = t.rt + 1 < g.tiles;
-  const int head = same ? t.head : t.head + 1, rt = same ? t.rt + 1 : 0;
-  if (head >= fresh().c.nkv) return deal<BM, BN, LONG>(r, false);
-  return cut<BM, BN>(r, g, x, head, rt, 0, g.units(rt), t.causal);
+  Tile n = t;
+  return more<BM, BN>(r, n, fresh().c.nkv) ? n : dealt<BM, BN, LONG>(r, false);
 }
 __device__ __forceinline__ int uni(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
@@ -715,7 +526,7 @@ __device__ __forceinline__ float inverse(float l) { return l > 0.f || l != l ? 1
 template <int BM, int BN, int LONG = 1, typename F>
 __device__ __forceinline__ void for_tiles(int wgs, F&& f) {
   Run r;
-  Tile t = deal<BM, BN, LONG>(r, true);
+  Tile t = dealt<BM, BN, LONG>(r, true);
   int4 desc = make_int4(0, 0, 0, 0), more = desc;
   while (t.b1 > t.b0) {
     if (t.parts) {
