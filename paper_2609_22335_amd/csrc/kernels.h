@@ -8,6 +8,12 @@ namespace vla {
 
 enum Dtype { DT_F32 = 0, DT_BF16 = 1 };
 
+// sched_barrier mask: vector memory operations stay on their side, the rest
+// may cross. It stands between two groups of loads into LDS of which a counted
+// vmcnt waits for the first only: they write different objects through
+// independent addresses, so nothing else keeps the compiler from mixing them.
+constexpr int LDS_ORDER = 0x78F;
+
 // Most frames (robots' action phases) one skinny GEMM, norm or cache
 // attention launch can carry as frame blocks.
 constexpr int MAX_FRAMES = 8;

@@ -188,11 +188,6 @@ __device__ __forceinline__ void bld16_lds(Rsrc r, void* dst, uint32_t off, uint3
 // s_waitcnt operand that waits for every outstanding vector memory load
 // (vmcnt 0; expcnt and lgkmcnt left at their maxima)
 constexpr int VMCNT0 = 0x0F70;
-// sched_barrier mask: vector memory operations stay on their side, the rest
-// may cross. It stands between two groups of loads into LDS of which a counted
-// vmcnt waits for the first only: they write different objects through
-// independent addresses, so nothing else keeps the compiler from mixing them.
-constexpr int LDS_ORDER = 0x78F;
 __device__ __forceinline__ float bld1(Rsrc r, uint32_t off) {
   return __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(r, off, 0, 0));
 }

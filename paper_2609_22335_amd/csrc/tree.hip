@@ -802,8 +802,12 @@ __global__ __launch_bounds__(256, (many_waves<uint16_t, HDP>())) void k_tree_man
     ld.issue(a.k, (LB*)s0, pk, wv);
     look(t.b0 + 1);
     issue((LB*)s1);
+    // (the first wait leaves the loads behind here in flight, the next one the
+    // last stage's)
+    __builtin_amdgcn_sched_barrier(LDS_ORDER);
     look(t.b0 + 2);
     issue((LB*)s2);
+    __builtin_amdgcn_sched_barrier(LDS_ORDER);
     look(t.b0 + 3);
     issue((LB*)s3);
     const int own = t.causal && t.len + tok + 1 < t.kend ? t.len + tok + 1 : t.kend;
