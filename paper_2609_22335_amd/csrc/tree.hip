@@ -216,18 +216,34 @@ struct Loader {
     const int lane = threadIdx.x & 63, s0 = 32 * j + 16 * lane;
     return table[s0 < kend && s0 < 32 * j1 ? s0 >> page_lg : 0];
   }
-  __device__ __forceinline__ void spread(int j, int j1, int id, uint32_t& lo, uint32_t& hi, uint32_t& bytes) const {
+  // (returns whether slots without a page are among them)
+  __device__ __forceinline__ bool spread(int j, int j1, int id, uint32_t& lo, uint32_t& hi, uint32_t& bytes) const {
     const int lane = threadIdx.x & 63, s0 = 32 * j + 16 * lane, left = kend - s0;
-    const bool ok = left > 0 && s0 < 32 * j1 && (unsigned)id < (unsigned)n_pages;
+    const bool in = left > 0 && s0 < 32 * j1, ok = in && (unsigned)id < (unsigned)n_pages;
     const int at = s0 & (page - 1), room = page - at;
     const unsigned long long off =
         (unsigned long long)(uint32_t)((ok ? id : 0) * nkv + head) * pbytes + (uint32_t)(at * hb);
     lo = (uint32_t)off, hi = (uint32_t)(off >> 32), bytes = ok ? (uint32_t)((left < room ? left : room) * hb) : 0u;
+    return __any(in && !ok);
   }
   // the places of slots kb and kb + 16 (which may lie in different pages)
   __device__ __forceinline__ void look(int kb, Place (&p)[2]) const {
     p[0] = place(kb);
     p[1] = place(kb + 16);
+  }
+  // A table may have no page for slots before the last key: nobody sees those.
+  // Whether the slots from kb on have any such, by their places, and a bit for
+  // each slot that has a page.
+  __device__ __forceinline__ bool hole(int kb, const Place (&p)[2]) const {
+    return (kb < kend && p[0].bytes == 0) || (kb + 16 < kend && p[1].bytes == 0);
+  }
+  __device__ __forceinline__ uint32_t paged(const Place (&p)[2]) const {
+    return (p[0].bytes ? 0xFFFFu : 0u) | (p[1].bytes ? 0xFFFF0000u : 0u);
+  }
+  __device__ __forceinline__ uint32_t paged(int kb) const {
+    Place p[2];
+    look(kb, p);
+    return paged(p);
   }
   __device__ __forceinline__ void issue(const char* src, LB* dst, const Place (&p)[2], int part) const {
 #pragma unroll
@@ -595,8 +611,8 @@ __global__ __launch_bounds__(256, (many_waves<T, HDP>())) void k_tree_few(Args a
     wait_vm<0>();  // (the first block waits for the query as well)
     for (int b = t.b0; b < t.b1; ++b) {
       const int kb = b * BN + wv * 32;
-      const bool more = b + 1 < t.b1, masked = kb + 32 > safe;
-      const uint32_t see = masked ? seen_bits(t, kb, own, row) : 0u;
+      const bool more = b + 1 < t.b1, masked = kb + 32 > safe || ld.hole(kb, at);
+      const uint32_t see = masked ? seen_bits(t, kb, own, row) & ld.paged(at) : 0u;
       if (b > t.b0) wait_vm<Ld::NI>();  // K is here, V may be on its way
       f32x16 s[1];
       scores<T, HDP, 1, NQ>(kl, qf, s);
@@ -625,7 +641,8 @@ __global__ __launch_bounds__(256, (many_waves<T, HDP>())) void k_tree_few(Args a
     if (odd)
       for (int b = t.b0; b < t.b1; ++b) {
         const int kb = b * BN + wv * 32;
-        if (kb + 32 > safe) add_odd_values<T, HDP>(t, kb, seen_bits(t, kb, own, row), o);
+        ld.look(kb, at);
+        if (kb + 32 > safe || ld.hole(kb, at)) add_odd_values<T, HDP>(t, kb, seen_bits(t, kb, own, row), o);
       }
     // the four waves' results: each puts its own into the LDS (columns of the
     // first half where K was, the others where V was), two waves work out what
@@ -776,8 +793,9 @@ __global__ __launch_bounds__(256, (many_waves<uint16_t, HDP>())) void k_tree_man
     // step would make every read of the LDS behind it wait.)
     uint32_t lo = 0, hi = 0, bytes = 0;
     int id = ld.page_id(t.b0, t.b1);
+    bool hole = false;          // slots without a page have been met: every block is looked at from then on
     auto window = [&](int j) {  // of blocks j .. j + 31, and the next one's pages on their way
-      ld.spread(j, t.b1, id, lo, hi, bytes);
+      hole |= ld.spread(j, t.b1, id, lo, hi, bytes);
       id = ld.page_id(j + 32, t.b1);
     };
     Place pk[2] = {}, pv[2];  // K of block j, V of j - 1
@@ -835,6 +853,10 @@ __global__ __launch_bounds__(256, (many_waves<uint16_t, HDP>())) void k_tree_man
       vf[kk][dt] = u32x4{u0.x, u0.y, u1.x, u1.y};
     };
     auto fence = [&] { __builtin_amdgcn_sched_barrier(0); };
+    auto seen = [&](int kb) {
+      const uint32_t see = seen_bits(t, kb, own, row);
+      return hole ? see & ld.paged(kb) : see;
+    };
     auto cover = [&](f32x16& x, uint32_t see) {  // scores that their rows do not see
       hide(x, see);
       bm = x[0];
@@ -872,9 +894,9 @@ __global__ __launch_bounds__(256, (many_waves<uint16_t, HDP>())) void k_tree_man
       constexpr int P = decltype(phase)::value, JQ = 12;
       const LB *st = stage(P + 1), *sn = stage(P + 2);
       f32x16 &cur = s[P & 1], &nxt = s[(P + 1) & 1];
-      const bool hidden = (b + 2) * BN > safe;
-      const uint32_t see = hidden ? seen_bits(t, (b + 1) * BN, own, row) : 0u;  // (its loads are out early)
-      if ((b + 1) * BN > safe) {
+      const bool hidden = (b + 2) * BN > safe || hole;
+      const uint32_t see = hidden ? seen((b + 1) * BN) : 0u;  // (its loads are out early)
+      if ((b + 1) * BN > safe || hole) {
         if (clean_values<T, HDP, 4>((LB*)st + 32 * RB, wv)) sOdd = 1;
         wait_lds();
         barrier();
@@ -931,7 +953,7 @@ __global__ __launch_bounds__(256, (many_waves<uint16_t, HDP>())) void k_tree_man
     bm = s[0][0];
 #pragma unroll
     for (int j = 1; j < 16; ++j) bm = fmaxf(bm, s[0][j]);
-    if ((t.b0 + 1) * BN > safe) cover(s[0], seen_bits(t, t.b0 * BN, own, row));
+    if ((t.b0 + 1) * BN > safe || hole) cover(s[0], seen(t.b0 * BN));
     if (!PAIR) raise();
     for (int b = t.b0;; b += 4) {
       if (((b - t.b0) & 31) == 28) window(b + 4);
@@ -948,7 +970,7 @@ __global__ __launch_bounds__(256, (many_waves<uint16_t, HDP>())) void k_tree_man
     l = sum_x32(l);
     if (sOdd)  // (written before the last step's barrier)
       for (int b = t.b0; b < t.b1; ++b)
-        if ((b + 1) * BN > safe) add_odd_values<T, HDP>(t, b * BN, seen_bits(t, b * BN, own, row), o);
+        if ((b + 1) * BN > safe || hole) add_odd_values<T, HDP>(t, b * BN, seen_bits(t, b * BN, own, row), o);
     finish<T, HDP>(t, slot, wv, m, mx, l, o);
   });
 }
@@ -973,9 +995,13 @@ __global__ __launch_bounds__(256, (many_waves<float, HDP>())) void k_tree_many32
     Ld ld;
     ld.set(t);
     Place at[NS][2];
+    bool hole = false;  // (as in k_tree_many)
     auto look = [&](int b) {
 #pragma unroll
-      for (int n = 0; n < NS; ++n) ld.look(b * BN + 32 * n, at[n]);
+      for (int n = 0; n < NS; ++n) {
+        ld.look(b * BN + 32 * n, at[n]);
+        hole |= ld.hole(b * BN + 32 * n, at[n]);
+      }
     };
     auto issue = [&](const char* src, LB* dst) {
 #pragma unroll
@@ -1012,10 +1038,12 @@ __global__ __launch_bounds__(256, (many_waves<float, HDP>())) void k_tree_many32
       scores<T, HDP, NS, NQ>(kt, qf, s);
       // (loads take their turns at issue: these go out beside the products)
       if (b + 1 < t.b1) issue(a.v, vn);
-      if (kb + BN > safe) {
+      if (kb + BN > safe || hole) {
 #pragma unroll
         for (int n = 0; n < NS; ++n) {
-          hide(s[n], seen_bits(t, kb + 32 * n, own, row));
+          uint32_t see = seen_bits(t, kb + 32 * n, own, row);
+          if (hole) see &= ld.paged(kb + 32 * n);
+          hide(s[n], see);
           if (clean_values<T, HDP, 4>(vt + n * 32 * RB, wv)) sOdd = 1;
         }
         wait_lds();
@@ -1034,7 +1062,7 @@ __global__ __launch_bounds__(256, (many_waves<float, HDP>())) void k_tree_many32
     l = sum_x32(l);
     if (sOdd)  // (written before the last block's barrier)
       for (int kb = t.b0 * BN; kb < t.b1 * BN; kb += 32)
-        if (kb + 32 > safe) add_odd_values<T, HDP>(t, kb, seen_bits(t, kb, own, row), o);
+        if (kb + 32 > safe || hole) add_odd_values<T, HDP>(t, kb, seen_bits(t, kb, own, row), o);
     finish<T, HDP>(t, slot, wv, m, mx, l, o);
   });
 }
