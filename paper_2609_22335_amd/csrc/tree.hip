@@ -979,7 +979,9 @@ __global__ __launch_bounds__(256, (many_waves<uint16_t, HDP>())) void k_tree_man
 // the matrix cores. The four waves share a ring of two blocks in the LDS, the
 // next one on its way while one is worked on: one barrier to a block. A block
 // is two tiles of 32 keys, at head dim 128 one, so that there are more blocks
-// to deal out (trees of 40 rows 19.6 us against 23.5).
+// to deal out: eight caches of 1,000 slots, 8 heads on 1, trees of 40 rows 35.0
+// us against 40.6, of 64 39.0 against 41.6; two chunks of 1,000 rows behind
+// 2,000, 32 heads on 8, 750 us against 704.
 template <int HDP>
 __global__ __launch_bounds__(256, (many_waves<float, HDP>())) void k_tree_many32(Args a) {
   typedef float T;
