@@ -26,8 +26,11 @@ struct PagedRows {
   const int32_t* seqs = nullptr;   // [n_ent] or null
 };
 
-// A grid holds fewer than 2^32 threads in each direction.
+// A grid holds fewer than 2^32 threads in each direction. What the launches
+// below return where they would need more: a value that the runtime has no
+// meaning for, so that its own errors stay apart from it.
 inline bool launchable(long long wgs, int threads) { return wgs * threads < (1ll << 32); }
+constexpr hipError_t GRID_FULL = (hipError_t)2000;
 
 // status bits
 enum { PG_OUT = 1, PG_BAD = 2 };

@@ -144,7 +144,7 @@ static hipError_t rope_norm_l(const RopeNormDesc& d, hipStream_t st) {
   const bool many = (long long)d.r.n_rows * groups > MANY_WAVES;
   const int parts = many ? (groups + 2) / 3 : groups;
   const long long wgs = ((long long)d.r.n_rows * parts + 3) / 4;
-  if (!launchable(wgs, 256)) return hipErrorInvalidValue;
+  if (!launchable(wgs, 256)) return GRID_FULL;
   if (many) hipLaunchKernelGGL((k_rope_norm<T, LPH, 3>), dim3((unsigned)wgs), dim3(256), 0, st, d, parts);
   else hipLaunchKernelGGL((k_rope_norm<T, LPH, 1>), dim3((unsigned)wgs), dim3(256), 0, st, d, parts);
   return hipGetLastError();
@@ -241,7 +241,7 @@ __global__ void k_pages_init(PagedCache c) {
 hipError_t launch_pages_init(const PagedCache& c, hipStream_t st) {
   const long long n = std::max({(long long)c.n_seqs * c.max_pages, (long long)c.n_pages, 1ll});
   const long long wgs = (n + 255) / 256;
-  if (!launchable(wgs, 256)) return hipErrorInvalidValue;
+  if (!launchable(wgs, 256)) return GRID_FULL;
   hipLaunchKernelGGL(k_pages_init, dim3((unsigned)wgs), dim3(256), 0, st, c);
   return hipGetLastError();
 }
@@ -475,7 +475,7 @@ hipError_t launch_pages_fork(const PagedCache& c, int n, const int32_t* src, con
   if (n <= 0) return hipSuccess;
   const int groups = (c.layers * c.nkv + FORK_HEADS - 1) / FORK_HEADS;
   const long long wgs = (long long)n * groups;
-  if (!launchable(wgs, 256)) return hipErrorInvalidValue;
+  if (!launchable(wgs, 256)) return GRID_FULL;
   if (few_to_deal(c, n)) hipLaunchKernelGGL(k_pages_fork<PT_FEW>, dim3(1), dim3(PT_FEW), 0, st, c, n, src, dst, made);
   else hipLaunchKernelGGL(k_pages_fork<PT_MANY>, dim3(1), dim3(PT_MANY), 0, st, c, n, src, dst, made);
   hipError_t e = hipGetLastError();
@@ -507,7 +507,7 @@ __global__ __launch_bounds__(256) void k_pages_release(PagedCache c, const int32
 
 hipError_t launch_pages_release(const PagedCache& c, int n, const int32_t* seqs, hipStream_t st) {
   if (n <= 0) return hipSuccess;
-  if (!launchable(n, 256)) return hipErrorInvalidValue;
+  if (!launchable(n, 256)) return GRID_FULL;
   hipLaunchKernelGGL(k_pages_release, dim3(n), dim3(256), 0, st, c, seqs);
   return hipGetLastError();
 }
@@ -621,7 +621,7 @@ hipError_t launch_pages_commit(const PagedCache& c, const PagedRows& r, const in
     // when all of them have read the old length (eight entries of 512 columns
     // 4.3 us against 5.6, 1,152 columns 5.5 / 5.7, 2,048 columns 7.1 / 5.7).
     const bool one = (long long)combos * cpr <= 1280;
-    if (!launchable(r.n_ent, one ? 1024 : 256)) return hipErrorInvalidValue;
+    if (!launchable(r.n_ent, one ? 1024 : 256)) return GRID_FULL;
     if (one) {
       hipLaunchKernelGGL(k_pages_move, dim3(r.n_ent, 1), dim3(1024), 0, st, c, r, kept, n_kept, cpr, esz);
       return hipGetLastError();
@@ -683,7 +683,7 @@ hipError_t launch_ctx_to_pages(const PagedCache& c, const void* k, const void* v
   const int vec = c.dtype == DT_BF16 ? 8 : 4;
   const long long items = (long long)((rows + vec - 1) / vec) * (c.hd / vec);
   const dim3 grid((unsigned)((items + 255) / 256), (unsigned)(c.layers * c.nkv));
-  if (grid.y > 65535) return hipErrorInvalidValue;
+  if (grid.y > 65535) return GRID_FULL;
   if (c.dtype == DT_BF16)
     hipLaunchKernelGGL(k_ctx_to_pages<uint16_t>, grid, dim3(256), 0, st, c, (const uint16_t*)k, (const uint16_t*)v, lk,
                        lv, nb, rows, seq);

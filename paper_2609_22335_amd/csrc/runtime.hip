@@ -3326,7 +3326,7 @@ static int paged_layer(const PagedCache& c, int32_t layer, int32_t nq) {
 }
 
 static int paged_launch(const char* what, hipError_t e) {
-  if (e == hipErrorInvalidValue) return fail(VLA_EUNSUPPORTED, std::string(what) + ": more workgroups than a grid holds");
+  if (e == GRID_FULL) return fail(VLA_EUNSUPPORTED, std::string(what) + ": more workgroups than a grid holds");
   if (e != hipSuccess) return fail(VLA_EHIP, std::string(what) + ": " + hipGetErrorString(e));
   return VLA_OK;
 }
