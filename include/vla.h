@@ -540,8 +540,8 @@ int vla_pages_reserve(const vla_pages* c, const vla_rows* r, void* stream);
 /* Norm, rotate and store one layer's new rows: q [n_rows][nq heads], k and v
  * [n_rows][kv_heads], rows ld* elements apart (a multiple of 16 bytes, as are
  * the base addresses), so slices of a fused QKV product can be given. Queries
- * go to q_out (which may be q itself with the same ldq), keys and values to
- * the cache's slots. pos (int32 [n_rows]) holds the rows' positions; NULL: the
+ * go to q_out (which may be q itself with the same ldq, and else overlaps none
+ * of q, k and v), keys and values to the cache's slots. pos (int32 [n_rows]) holds the rows' positions; NULL: the
  * slot. Norm, rotation and mean are fp32 and rounded once. A row whose
  * position is outside the table is left out (VLA_PAGES_BAD); K and V of a slot
  * without a page are not stored (VLA_PAGES_OUT). */
@@ -561,8 +561,8 @@ int vla_qk_norm_rope(const vla_pages* c, int32_t layer, const vla_rows* r, const
  * a row sees they make that row's results infinite or NaN. Sums and the
  * softmax are fp32. q and out have rows ldq and ldo elements apart (base and
  * rows on 16 bytes; out must not overlap q). scratch: scratch_bytes of device
- * memory, at least what vla_tree_attention_scratch says, 16-byte aligned,
- * contents of no matter; calls that may overlap need their own. The sums'
+ * memory, at least what vla_tree_attention_scratch says, 16-byte aligned, apart
+ * from q and out, contents of no matter; calls that may overlap need their own. The sums'
  * order depends on the batch's lengths and shapes alone. */
 int vla_tree_attention(const vla_pages* c, int32_t layer, const vla_rows* r, const uint32_t* mask, int32_t mask_words,
                        int32_t nq, float scale, const void* q, int64_t ldq, void* out, int64_t ldo, void* scratch,

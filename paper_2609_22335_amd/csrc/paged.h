@@ -49,6 +49,7 @@ struct RopeNormDesc {
   int n_pos = 0, rot = 0;
   const int32_t* pos = nullptr;
 };
+bool rope_norm_fits(const RopeNormDesc& d);  // (a grid holds it)
 hipError_t launch_rope_norm(const RopeNormDesc& d, hipStream_t st);
 
 struct TreeAttnDesc {
@@ -69,6 +70,7 @@ hipError_t launch_tree_attn(const TreeAttnDesc& d, hipStream_t st);
 
 hipError_t launch_pages_init(const PagedCache& c, hipStream_t st);
 hipError_t launch_pages_reserve(const PagedCache& c, const PagedRows& r, hipStream_t st);
+bool fork_fits(const PagedCache& c, int n);
 hipError_t launch_pages_fork(const PagedCache& c, int n, const int32_t* src, const int32_t* dst, int32_t* made,
                              hipStream_t st);
 hipError_t launch_pages_commit(const PagedCache& c, const PagedRows& r, const int32_t* kept, const int32_t* n_kept,

@@ -137,26 +137,37 @@ __global__ __launch_bounds__(256) void k_rope_norm(RopeNormDesc d, int parts) {
   }
 }
 
+// Lanes to a head, and what a launch is made of.
+struct RopeNormGrid {
+  int lph, parts;
+  bool many;
+  long long wgs;
+  explicit RopeNormGrid(const RopeNormDesc& d) {
+    const int np = d.c.hd / (d.c.dtype == DT_BF16 ? 16 : 8);  // lanes that a head keeps busy
+    lph = np <= 2 ? 2 : np <= 4 ? 4 : np <= 8 ? 8 : 16;
+    const int hpw = 64 / lph, groups = (d.nq + hpw - 1) / hpw + 2 * ((d.c.nkv + hpw - 1) / hpw);
+    many = (long long)d.r.n_rows * groups > MANY_WAVES;
+    parts = many ? (groups + 2) / 3 : groups;
+    wgs = ((long long)d.r.n_rows * parts + 3) / 4;
+  }
+};
+bool rope_norm_fits(const RopeNormDesc& d) { return launchable(RopeNormGrid(d).wgs, 256); }
+
 template <typename T, int LPH>
-static hipError_t rope_norm_l(const RopeNormDesc& d, hipStream_t st) {
-  const int hpw = 64 / LPH;
-  const int groups = (d.nq + hpw - 1) / hpw + 2 * ((d.c.nkv + hpw - 1) / hpw);
-  const bool many = (long long)d.r.n_rows * groups > MANY_WAVES;
-  const int parts = many ? (groups + 2) / 3 : groups;
-  const long long wgs = ((long long)d.r.n_rows * parts + 3) / 4;
-  if (!launchable(wgs, 256)) return GRID_FULL;
-  if (many) hipLaunchKernelGGL((k_rope_norm<T, LPH, 3>), dim3((unsigned)wgs), dim3(256), 0, st, d, parts);
-  else hipLaunchKernelGGL((k_rope_norm<T, LPH, 1>), dim3((unsigned)wgs), dim3(256), 0, st, d, parts);
+static hipError_t rope_norm_l(const RopeNormDesc& d, const RopeNormGrid& g, hipStream_t st) {
+  if (g.many) hipLaunchKernelGGL((k_rope_norm<T, LPH, 3>), dim3((unsigned)g.wgs), dim3(256), 0, st, d, g.parts);
+  else hipLaunchKernelGGL((k_rope_norm<T, LPH, 1>), dim3((unsigned)g.wgs), dim3(256), 0, st, d, g.parts);
   return hipGetLastError();
 }
 
 template <typename T>
 static hipError_t rope_norm_t(const RopeNormDesc& d, hipStream_t st) {
-  const int np = d.c.hd / (2 * El<T>::VEC);  // lanes that a head keeps busy
-  return np <= 2   ? rope_norm_l<T, 2>(d, st)
-         : np <= 4 ? rope_norm_l<T, 4>(d, st)
-         : np <= 8 ? rope_norm_l<T, 8>(d, st)
-                   : rope_norm_l<T, 16>(d, st);
+  const RopeNormGrid g(d);
+  if (!launchable(g.wgs, 256)) return GRID_FULL;
+  return g.lph == 2   ? rope_norm_l<T, 2>(d, g, st)
+         : g.lph == 4 ? rope_norm_l<T, 4>(d, g, st)
+         : g.lph == 8 ? rope_norm_l<T, 8>(d, g, st)
+                      : rope_norm_l<T, 16>(d, g, st);
 }
 
 hipError_t launch_rope_norm(const RopeNormDesc& d, hipStream_t st) {
@@ -470,12 +481,14 @@ __global__ __launch_bounds__(256) void k_pages_copy(PagedCache c, const int32_t*
   }
 }
 
+static int copy_groups(const PagedCache& c) { return (c.layers * c.nkv + FORK_HEADS - 1) / FORK_HEADS; }
+bool fork_fits(const PagedCache& c, int n) { return launchable((long long)n * copy_groups(c), 256); }
 hipError_t launch_pages_fork(const PagedCache& c, int n, const int32_t* src, const int32_t* dst, int32_t* made,
                              hipStream_t st) {
   if (n <= 0) return hipSuccess;
-  const int groups = (c.layers * c.nkv + FORK_HEADS - 1) / FORK_HEADS;
+  const int groups = copy_groups(c);
   const long long wgs = (long long)n * groups;
-  if (!launchable(wgs, 256)) return GRID_FULL;
+  if (!fork_fits(c, n)) return GRID_FULL;
   if (few_to_deal(c, n)) hipLaunchKernelGGL(k_pages_fork<PT_FEW>, dim3(1), dim3(PT_FEW), 0, st, c, n, src, dst, made);
   else hipLaunchKernelGGL(k_pages_fork<PT_MANY>, dim3(1), dim3(PT_MANY), 0, st, c, n, src, dst, made);
   hipError_t e = hipGetLastError();

@@ -3319,6 +3319,38 @@ static int paged_operand(const PagedCache& c, const char* what, const void* p, i
   return VLA_OK;
 }
 
+// Rows of w bytes, ld bytes apart (ld >= w; of a single row ld does not count).
+struct ByteRows {
+  const void* p;
+  int64_t ld, w, n;
+};
+// Whether two such arrays share a byte. Slices of one tensor's rows lie within
+// each other's spans and need not.
+static bool meet(const ByteRows& a, const ByteRows& b) {
+  if (a.n <= 0 || b.n <= 0) return false;
+  const int64_t la = a.n > 1 ? a.ld : a.w, lb = b.n > 1 ? b.ld : b.w;
+  const int64_t d = (int64_t)((uintptr_t)b.p - (uintptr_t)a.p);  // b's row j: bytes d + j lb .. of a's
+  if (d >= (a.n - 1) * la + a.w || d + (b.n - 1) * lb + b.w <= 0) return false;
+  auto down = [](int64_t x, int64_t y) { return x >= 0 ? x / y : -((-x + y - 1) / y); };
+  if (a.n > 1 && b.n > 1 && la == lb) {
+    // b's row j begins `off` bytes into a's row j + r and may reach into the next
+    const int64_t r = down(d, la), off = d - r * la;
+    auto both = [&](int64_t q) { return std::max<int64_t>(0, -q) < std::min(b.n, a.n - q); };  // some j, j + q
+    return (off < a.w && both(r)) || (off + b.w > la && both(r + 1));
+  }
+  // a's rows, one at a time: the first and the last of b's that each could meet
+  for (int64_t i = std::max<int64_t>(0, down(d - a.w, la)); i < a.n && i * la < d + (b.n - 1) * lb + b.w; ++i) {
+    const int64_t lo = std::max<int64_t>(0, down(i * la - d - b.w, lb) + 1);
+    const int64_t hi = std::min(b.n - 1, down(i * la + a.w - 1 - d, lb));
+    if (lo <= hi) return true;
+  }
+  return false;
+}
+static ByteRows paged_bytes(const PagedCache& c, const PagedRows& r, const void* p, int64_t ld, int64_t heads) {
+  const int64_t esz = c.dtype == DT_BF16 ? 2 : 4;
+  return ByteRows{p, ld * esz, heads * c.hd * esz, r.n_rows};
+}
+
 static int paged_layer(const PagedCache& c, int32_t layer, int32_t nq) {
   if (layer < 0 || layer >= c.layers) return fail(VLA_EINVAL, "layer outside the cache");
   if (nq <= 0 || nq % c.nkv || nq > (1 << 16)) return fail(VLA_EINVAL, "nq must be a multiple of kv_heads");
@@ -3405,6 +3437,12 @@ int vla_qk_norm_rope(const vla_pages* p, int32_t layer, const vla_rows* rows, co
     d.n_pos = n->n_pos;
     d.rot = n->rot_dim;
     d.pos = pos;
+    if (!rope_norm_fits(d)) return paged_launch("qk_norm_rope", GRID_FULL);
+    const ByteRows o = paged_bytes(d.c, d.r, q_out, ldo, nq);
+    if (q_out != q && meet(o, paged_bytes(d.c, d.r, q, ldq, nq)))
+      return fail(VLA_EINVAL, "q_out overlaps q (it may be q itself)");
+    if (meet(o, paged_bytes(d.c, d.r, k, ldk, d.c.nkv)) || meet(o, paged_bytes(d.c, d.r, v, ldv, d.c.nkv)))
+      return fail(VLA_EINVAL, "q_out overlaps k or v");
     return paged_launch("qk_norm_rope", launch_rope_norm(d, (hipStream_t)stream));
   })
 }
@@ -3445,11 +3483,14 @@ int vla_tree_attention(const vla_pages* p, int32_t layer, const vla_rows* rows, 
     if (d.r.n_rows == 0 || d.r.n_ent == 0) return VLA_OK;  // nothing is read or written
     VLA_TRY(paged_operand(d.c, "q", q, ldq, nq));
     VLA_TRY(paged_operand(d.c, "out", out, ldo, nq));
-    if (out == q) return fail(VLA_EINVAL, "out must not be q");
+    const ByteRows o = paged_bytes(d.c, d.r, out, ldo, nq), in = paged_bytes(d.c, d.r, q, ldq, nq);
+    if (meet(o, in)) return fail(VLA_EINVAL, "out must not be q or overlap it");
     VLA_TRY(device_cus(&d.cus));
     const size_t need = tree_attn_scratch(d);
     if (!scratch || !aligned16(scratch) || scratch_bytes < 0 || (size_t)scratch_bytes < need)
       return fail(VLA_EINVAL, "scratch: needs " + std::to_string(need) + " bytes, 16-byte aligned");
+    const ByteRows work{scratch, 0, (int64_t)need, 1};
+    if (meet(o, work) || meet(in, work)) return fail(VLA_EINVAL, "scratch overlaps q or out");
     d.mask = mask;
     d.mask_words = mask ? mask_words : 0;
     d.scale = scale;
@@ -3470,6 +3511,10 @@ int vla_pages_fork(const vla_pages* p, int32_t n, const int32_t* src, const int3
     if (n < 0 || n > (1 << 24)) return fail(VLA_EINVAL, "n must be in 0 .. 2^24");
     if (n == 0) return VLA_OK;
     if (!src || !dst || !made) return fail(VLA_EINVAL, "NULL argument");
+    if (!fork_fits(c, n)) return paged_launch("pages fork", GRID_FULL);
+    const ByteRows m{made, 0, (int64_t)n * 4, 1};
+    if (meet(m, ByteRows{src, 0, m.w, 1}) || meet(m, ByteRows{dst, 0, m.w, 1}))
+      return fail(VLA_EINVAL, "made must be an array of its own");
     return paged_launch("pages fork", launch_pages_fork(c, n, src, dst, made, (hipStream_t)stream));
   })
 }
