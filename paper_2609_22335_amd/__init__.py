@@ -572,7 +572,7 @@ def _heads(x, what: str, pages, n: int, heads=None) -> int:
             raise _einval(f"{what}: a tensor is on {x.device}, the cache on {pages._dev}")
         raise _einval(f"{what}: a row's heads must be contiguous")
     # (a single row has no stride that counts)
-    return stride[0] if n > 1 else max(stride[0], shape[1] * hd)
+    return stride[0] if n > 1 else shape[1] * hd
 
 
 def _ints(x, what: str, pages, shape) -> int:
