@@ -12,6 +12,7 @@ there is no fallback path.
 from __future__ import annotations
 
 import ctypes
+import operator
 import os
 from typing import Dict, Iterable, Optional, Sequence, Tuple
 
@@ -467,6 +468,17 @@ def _dev(x, what: str, dtype: str, shape=None):
     return x.device
 
 
+def _int32(x, what: str) -> int:
+    """An integer that the library can hold (ctypes would cut it off)."""
+    try:
+        n = int(x) if isinstance(x, float) and x.is_integer() else operator.index(x)
+    except TypeError:
+        raise _einval(f"{what} must be an integer, got {x!r}") from None
+    if not -2 ** 31 <= n < 2 ** 31:
+        raise _einval(f"{what} is {n}, which 32 bits do not hold")
+    return n
+
+
 def _one_device(pairs):
     first = None
     for what, dev in pairs:
@@ -510,11 +522,11 @@ def make_rows(start, n_rows: int, seqs=None) -> vla_rows:
     dev = _dev(start, "start", "int32")
     if len(start.shape) != 1 or start.shape[0] < 1:
         raise _einval("start must be [n_entries + 1]")
-    n = int(start.shape[0]) - 1
+    n, n_rows = int(start.shape[0]) - 1, _int32(n_rows, "n_rows")
     if seqs is not None:
         _one_device([("start", dev), ("seqs", _dev(seqs, "seqs", "int32", (n,)))])
-    r = vla_rows(int(n_rows), n, _ptr(start), _ptr(seqs))
-    r._src, r._dev, r._n, r._entries = (start, seqs), dev, int(n_rows), n
+    r = vla_rows(n_rows, n, _ptr(start), _ptr(seqs))
+    r._src, r._dev, r._n, r._entries = (start, seqs), dev, n_rows, n
     return r
 
 
@@ -526,13 +538,13 @@ def make_rope_norm(cos=None, sin=None, q_gain=None, k_gain=None, gain_plus_one: 
         raise _einval("a rotation needs both tables")
     pairs, n_pos, rot = [], 0, 0
     if cos is not None:
-        if len(cos.shape) != 2:
+        if len(getattr(cos, "shape", ())) != 2:
             raise _einval("cos must be [n_pos, rot_dim / 2]")
-        pairs += [("cos", _dev(cos, "cos", "float32")), ("sin", _dev(sin, "sin", "float32", cos.shape))]
+        pairs += [("cos", _dev(cos, "cos", "float32")), ("sin", _dev(sin, "sin", "float32", tuple(cos.shape)))]
         n_pos, rot = int(cos.shape[0]), 2 * int(cos.shape[1])
     for what, g in (("q_gain", q_gain), ("k_gain", k_gain)):
         if g is not None:
-            if len(g.shape) != 1:
+            if len(getattr(g, "shape", ())) != 1:
                 raise _einval(f"{what} must be [head_dim]")
             pairs.append((what, _dev(g, what, "float32")))
     p = vla_rope_norm(_ptr(q_gain), _ptr(k_gain), 1 if gain_plus_one else 0, float(eps), _ptr(cos), _ptr(sin),
@@ -558,6 +570,8 @@ def _at(pages, *others) -> None:
 def _heads(x, what: str, pages, n: int, heads=None) -> int:
     """[n, heads, head_dim] of the cache's type on its device, a row's heads
     side by side; the row stride."""
+    if not hasattr(x, "get_device"):
+        raise _einval(f"{what} must be a device (cuda) tensor")
     shape, stride, hd = x.shape, x.stride(), pages._hd
     if (x.get_device() != pages._index or x.dtype != pages._type or len(shape) != 3 or shape[0] != n
             or shape[2] != hd or (heads is not None and shape[1] != heads) or stride[2] != 1
@@ -614,7 +628,7 @@ def vla_qk_norm_rope(pages: vla_pages, layer: int, rows: vla_rows, rope: vla_rop
         if g != pages._hd:
             raise _einval(f"{what} holds {g} elements, head_dim is {pages._hd}")
     _at(pages, rows._dev, rope._dev)
-    _check(_lib.vla_qk_norm_rope(ctypes.byref(pages), layer, ctypes.byref(rows), ctypes.byref(rope),
+    _check(_lib.vla_qk_norm_rope(ctypes.byref(pages), _int32(layer, "layer"), ctypes.byref(rows), ctypes.byref(rope),
                                  _ints(pos, "pos", pages, (n,)), nq, q.data_ptr(), ldq, k.data_ptr(), ldk,
                                  v.data_ptr(), ldv, q_out.data_ptr(), ldo, stream or None))
 
@@ -622,7 +636,8 @@ def vla_qk_norm_rope(pages: vla_pages, layer: int, rows: vla_rows, rope: vla_rop
 def vla_tree_attention_scratch(pages: vla_pages, rows: vla_rows, nq: int) -> int:
     n = ctypes.c_int64()
     _at(pages, rows._dev)
-    _check(_lib.vla_tree_attention_scratch(ctypes.byref(pages), ctypes.byref(rows), int(nq), ctypes.byref(n)))
+    _check(_lib.vla_tree_attention_scratch(ctypes.byref(pages), ctypes.byref(rows), _int32(nq, "nq"),
+                                           ctypes.byref(n)))
     return n.value
 
 
@@ -637,14 +652,14 @@ def vla_tree_attention(pages: vla_pages, layer: int, rows: vla_rows, q, out, scr
     ldo = _heads(out, "out", pages, n, nq)
     words, bits = 0, None
     if mask is not None:
-        if len(mask.shape) != 2:
-            raise _einval(f"mask must be [{n}, words], got {tuple(mask.shape)}")
+        if len(getattr(mask, "shape", ())) != 2:
+            raise _einval(f"mask must be [{n}, words], got {tuple(getattr(mask, 'shape', ()))}")
         words = mask.shape[1]
         bits = _ints(mask, "mask", pages, (n, words))
     if _dev(scratch, "scratch", "uint8") != pages._dev:
         raise _einval(f"scratch: a tensor is on {scratch.device}, the cache on {pages._dev}")
     _at(pages, rows._dev)
-    _check(_lib.vla_tree_attention(ctypes.byref(pages), layer, ctypes.byref(rows), bits, words, nq,
+    _check(_lib.vla_tree_attention(ctypes.byref(pages), _int32(layer, "layer"), ctypes.byref(rows), bits, words, nq,
                                    pages._scale if scale is None else scale, q.data_ptr(), ldq, out.data_ptr(), ldo,
                                    scratch.data_ptr(), scratch.numel(), stream or None))
 
@@ -675,7 +690,8 @@ def vla_ctx_to_pages(model: int, ctx: int, pages: vla_pages, seq: int, stream: i
     """Returns the number of rows stored (the prefix)."""
     n = ctypes.c_int32()
     _at(pages)
-    _check(_lib.vla_ctx_to_pages(model, ctx, ctypes.byref(pages), int(seq), ctypes.byref(n), stream or None))
+    _check(_lib.vla_ctx_to_pages(model, ctx, ctypes.byref(pages), _int32(seq, "seq"), ctypes.byref(n),
+                                 stream or None))
     return n.value
 
 
