@@ -189,18 +189,18 @@ constexpr int PT_FEW = 256, PT_MANY = 1024;
 inline bool few_to_deal(const PagedCache& c, int n) { return n <= PT_FEW && c.n_pages <= 4 * 8 * PT_FEW; }
 
 // Exclusive prefix of x over the workgroup, and the total.
-template <int PT>
-__device__ __forceinline__ int block_scan(int x, int* total) {
-  __shared__ int sW[PT / 64];
+template <int PT, typename I>
+__device__ __forceinline__ I block_scan(I x, I* total) {
+  __shared__ I sW[PT / 64];
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-  const int s = wave_scan(x);
+  const I s = wave_scan(x);
   __syncthreads();  // the last call's sums are read
   if (lane == 63) sW[wv] = s;
   __syncthreads();
-  int before = 0, all = 0;
+  I before = 0, all = 0;
 #pragma unroll
   for (int i = 0; i < PT / 64; ++i) {
-    const int v = sW[i];
+    const I v = sW[i];
     before += i < wv ? v : 0;
     all += v;
   }
@@ -231,7 +231,7 @@ __device__ __forceinline__ int take_free(const PagedCache& c, unsigned bits0, in
     unsigned bits = base == 0 ? bits0 : free_bits(c, base);
     if (first < p0) bits &= p0 - first < 8 ? ~0u << (p0 - first) : 0u;
     int total;
-    int rank = found + block_scan<PT>(__popc(bits), &total);
+    int rank = found + block_scan<PT>((int)__popc(bits), &total);
     for (; bits && rank < want; bits &= bits - 1, ++rank) list[rank] = first + __ffs(bits) - 1;
     found += total;
   }
@@ -294,8 +294,11 @@ __global__ __launch_bounds__(PT) void k_pages_reserve(PagedCache c, PagedRows r)
       }
       if (again) need = 0;
     }
-    int total;
-    const int off = block_scan<PT>(need, &total);
+    // (64 bits: where start descends, entries name the same rows again and again.
+    // No more are given than the pool has, so the offsets may end at 2^31 - 1.)
+    long long sum;
+    const long long at = block_scan<PT>((long long)need, &sum);
+    const int off = (int)std::min(at, 0x7FFFFFFFll), total = (int)std::min(sum, 0x7FFFFFFFll);
     sOff[tid] = off;
     __syncthreads();
     int given = 0;
