@@ -557,9 +557,11 @@ int vla_qk_norm_rope(const vla_pages* c, int32_t layer, const vla_rows* r, const
  * to drafts 0 .. i. One row an entry and no mask is plain decoding, many rows
  * and no mask a causal chunk of a prompt. The drafts' K and V have been stored
  * before; slots without a page are not seen; a row that sees nothing is zero.
- * Masked slots may hold anything, infinities and NaN among it; in a slot that
- * a row sees they make that row's results infinite or NaN. Sums and the
- * softmax are fp32. q and out have rows ldq and ldo elements apart (base and
+ * Masked slots may hold anything, infinities and NaN among it. In a slot that
+ * a row sees, a V that is not finite makes the row's results in its column
+ * infinite or NaN, and K enters by its score: NaN and plus infinity make the
+ * row NaN, minus infinity is as good as a mask (a row without other scores is
+ * zero). Sums and the softmax are fp32. q and out have rows ldq and ldo elements apart (base and
  * rows on 16 bytes; out must not overlap q). scratch: scratch_bytes of device
  * memory, at least what vla_tree_attention_scratch says, 16-byte aligned, apart
  * from q and out, contents of no matter; calls that may overlap need their own. The sums'
