@@ -561,7 +561,11 @@ int vla_qk_norm_rope(const vla_pages* c, int32_t layer, const vla_rows* r, const
  * a row sees, a V that is not finite makes the row's results in its column
  * infinite or NaN, and K enters by its score: NaN and plus infinity make the
  * row NaN, minus infinity is as good as a mask (a row without other scores is
- * zero). Sums and the softmax are fp32. q and out have rows ldq and ldo elements apart (base and
+ * zero). Sums and the softmax are fp32. In bf16 the probabilities that multiply
+ * V are rounded, to one bf16 value (an error of at most 2^-8 of each) where
+ * n_rows * nq / kv_heads is above 128 n_entries (head dims up to 64: 192), else
+ * to the sum of two (2^-16); the sum that divides takes them unrounded. fp32
+ * keeps them. q and out have rows ldq and ldo elements apart (base and
  * rows on 16 bytes; out must not overlap q). scratch: scratch_bytes of device
  * memory, at least what vla_tree_attention_scratch says, 16-byte aligned, apart
  * from q and out, contents of no matter; calls that may overlap need their own. The sums'
