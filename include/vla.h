@@ -560,8 +560,8 @@ int vla_qk_norm_rope(const vla_pages* c, int32_t layer, const vla_rows* r, const
  * Masked slots may hold anything, infinities and NaN among it. In a slot that
  * a row sees, a V that is not finite makes the row's results in its column
  * infinite or NaN, and K enters by its score: NaN and plus infinity make the
- * row NaN, minus infinity is as good as a mask (a row without other scores is
- * zero). Sums and the softmax are fp32. In bf16 the probabilities that multiply
+ * row NaN, minus infinity beside a finite V is as good as a mask (a row without
+ * other scores is zero). Sums and the softmax are fp32. In bf16 the probabilities that multiply
  * V are rounded, to one bf16 value (an error of at most 2^-8 of each) where
  * n_rows * nq / kv_heads is above 128 n_entries (head dims up to 64: 192), else
  * to the sum of two (2^-16); the sum that divides takes them unrounded. fp32
@@ -606,8 +606,9 @@ int vla_pages_release(const vla_pages* c, int32_t n, const int32_t* seqs, void* 
  * vla_vlm_prefill wrote them) as new rows of sequence seq: row i to slot
  * lens[seq] + i, for which the sequence holds pages (vla_pages_reserve;
  * without: VLA_PAGES_OUT). vla_pages_commit then keeps them like any step's
- * rows, and the LM can answer from there. pages' dtype, layers, kv_heads and
- * head_dim are the model's. *rows (host, may be NULL) receives the number of
+ * rows, and new rows can attend to them; the layers that make those rows'
+ * queries, keys and values are the caller's (no entry point runs the LM on
+ * them). pages' dtype, layers, kv_heads and head_dim are the model's. *rows (host, may be NULL) receives the number of
  * rows. Asynchronous; ordered after the prefill by the caller. */
 int vla_ctx_to_pages(vla_model* m, const vla_ctx* c, const vla_pages* pages, int32_t seq, int32_t* rows, void* stream);
 
