@@ -578,6 +578,38 @@ int vla_tree_attention(const vla_pages* c, int32_t layer, const vla_rows* r, con
  * the size depends on the current device's CU count). */
 int vla_tree_attention_scratch(const vla_pages* c, const vla_rows* r, int32_t nq, int64_t* bytes);
 
+/* How products of queries and keys become scores, and which slots a row sees.
+ * A committed slot's place is its number, a row's place (and that of the draft
+ * that it is) lens + depth of its sequence. */
+typedef struct vla_scores {
+  float scale;          /* s = scale q k; positive                                  */
+  float cap;            /* > 0: s <- cap tanh(s / cap); 0: not capped               */
+  const float* slopes;  /* fp32 [nq]: s <- s - slopes[h] |row's place - key's|, or NULL */
+  int32_t window;       /* > 0: keys `window` or more places before a row are not   */
+                        /*   seen; 0: all                                           */
+  const int32_t* depth; /* int32 [n_rows]: how far behind the committed slots a row */
+                        /*   is (negative: 0), or NULL: an entry's row i at i       */
+  const int32_t* span;  /* int32 [n_rows][2], or NULL: the row sees slots span[0] .. */
+                        /*   span[1] - 1 of its sequence (its committed ones and    */
+                        /*   the step's drafts), before or behind itself            */
+} vla_scores;
+
+/* vla_tree_attention with shaped scores. Without a mask and a span a row sees
+ * drafts 0 .. i; a span takes the place of that rule (documents packed into
+ * one sequence, prefixes that see all of themselves), a mask and a span hold
+ * both, and the window holds beside either. lse (fp32 [n_rows][nq], or NULL)
+ * gets the logarithm of the sum of the exponentials of a row's scores, minus
+ * infinity for a row that sees nothing. A capped score is at most the cap, that
+ * of an infinite product too; in bf16 caches a capped score is off by
+ * up to 2^-20 of the cap. Everything else is as at vla_tree_attention: rows, padding,
+ * masked slots, sums, rounding; lse overlaps none of q, out and scratch. */
+int vla_score_attention(const vla_pages* c, int32_t layer, const vla_rows* r, const vla_scores* s, const uint32_t* mask,
+                        int32_t mask_words, int32_t nq, const void* q, int64_t ldq, void* out, int64_t ldo, float* lse,
+                        void* scratch, int64_t scratch_bytes, void* stream);
+
+/* Bytes of scratch (as vla_tree_attention_scratch). */
+int vla_score_attention_scratch(const vla_pages* c, const vla_rows* r, int32_t nq, int64_t* bytes);
+
 /* Branch: sequence dst[i] becomes a copy of src[i] (committed slots only).
  * Full pages are shared, the used slots of the last page are copied in every
  * layer to a page of the child's own. A pair is fit when both are sequences of

@@ -87,6 +87,11 @@ class vla_rope_norm(ctypes.Structure):
                 ("n_pos", ctypes.c_int32), ("rot_dim", ctypes.c_int32)]
 
 
+class vla_scores(ctypes.Structure):
+    _fields_ = [("scale", ctypes.c_float), ("cap", ctypes.c_float), ("slopes", ctypes.c_void_p),
+                ("window", ctypes.c_int32), ("depth", ctypes.c_void_p), ("span", ctypes.c_void_p)]
+
+
 PAGES_OUT, PAGES_BAD = 1, 2  # bits of a paged cache's status
 
 DEBUG_EPI = {"bias": 0, "t": 1, "gelu": 2, "swish": 3, "geglu": 4, "qkv_rope": 5, "qkv_plain": 6, "step": 7,
@@ -152,6 +157,8 @@ def _load():
         "vla_qk_norm_rope": [P, I32, P, P, P, I32, P, I64, P, I64, P, I64, P, I64, P],
         "vla_tree_attention": [P, I32, P, P, I32, I32, ctypes.c_float, P, I64, P, I64, P, I64, P],
         "vla_tree_attention_scratch": [P, P, I32, ctypes.POINTER(I64)],
+        "vla_score_attention": [P, I32, P, P, P, I32, I32, P, I64, P, I64, P, P, I64, P],
+        "vla_score_attention_scratch": [P, P, I32, ctypes.POINTER(I64)],
         "vla_pages_fork": [P, I32, P, P, P, P],
         "vla_pages_commit": [P, P, P, P, P],
         "vla_pages_release": [P, I32, P, P],
@@ -512,6 +519,8 @@ def make_pages(k, v, table, lens, held, refs, status) -> vla_pages:
     p._src = (k, v, table, lens, held, refs, status)
     # what the calls compare their operands with
     p._dev, p._index, p._type, p._ints = dev, dev.index, k.dtype, table.dtype
+    import torch
+    p._floats = torch.float32
     p._nkv, p._hd, p._scale = nkv, hd, hd ** -0.5
     return p
 
@@ -552,6 +561,27 @@ def make_rope_norm(cos=None, sin=None, q_gain=None, k_gain=None, gain_plus_one: 
     p._src, p._dev = (cos, sin, q_gain, k_gain), _one_device(pairs)
     p._gains = [(what, int(g.shape[0])) for what, g in (("q_gain", q_gain), ("k_gain", k_gain)) if g is not None]
     return p
+
+
+def make_scores(pages: vla_pages, scale=None, cap: float = 0.0, slopes=None, window: int = 0, depth=None,
+                span=None) -> vla_scores:
+    """A vla_scores for rows over this cache: scale (None: 1 /
+    sqrt(head_dim)), cap (0: none), slopes float32 [nq], window (0: none),
+    depth int32 [n_rows], span int32 [n_rows, 2]."""
+    pairs = [("pages", pages._dev)]
+    for what, x, kind, dims in (("slopes", slopes, "float32", 1), ("depth", depth, "int32", 1),
+                                ("span", span, "int32", 2)):
+        if x is not None:
+            if len(getattr(x, "shape", ())) != dims or (dims == 2 and x.shape[1] != 2):
+                raise _einval(f"{what} must be {'[nq]' if what == 'slopes' else '[n_rows]' if dims == 1 else '[n_rows, 2]'}")
+            pairs.append((what, _dev(x, what, kind)))
+    _one_device(pairs)
+    s = vla_scores(pages._scale if scale is None else float(scale), float(cap), _ptr(slopes),
+                   _int32(window, "window"), _ptr(depth), _ptr(span))
+    s._src, s._dev = (slopes, depth, span), pages._dev
+    s._nq = None if slopes is None else int(slopes.shape[0])
+    s._rows = [(what, int(x.shape[0])) for what, x in (("depth", depth), ("span", span)) if x is not None]
+    return s
 
 
 # A decoding step makes a call of these per layer and kernel, so each check is
@@ -641,6 +671,42 @@ def vla_tree_attention_scratch(pages: vla_pages, rows: vla_rows, nq: int) -> int
     return n.value
 
 
+def _mask(mask, pages, n: int) -> tuple:
+    """A mask's pointer and words to a row (None: neither)."""
+    if mask is None:
+        return None, 0
+    if len(getattr(mask, "shape", ())) != 2:
+        raise _einval(f"mask must be [{n}, words], got {tuple(getattr(mask, 'shape', ()))}")
+    return _ints(mask, "mask", pages, (n, mask.shape[1])), mask.shape[1]
+
+
+def _floats(x, what: str, pages, shape):
+    """float32 of this shape on the cache's device; its pointer (None: None)."""
+    if x is None:
+        return None
+    if not (hasattr(x, "get_device") and x.get_device() == pages._index and x.dtype == pages._floats
+            and tuple(x.shape) == shape and x.is_contiguous()):
+        dev = _dev(x, what, "float32", shape)
+        raise _einval(f"{what}: a tensor is on {dev}, the cache on {pages._dev}")
+    return x.data_ptr()
+
+
+def _scratch(x, pages) -> tuple:
+    """uint8 on the cache's device; its pointer and bytes."""
+    if _dev(x, "scratch", "uint8") != pages._dev:
+        raise _einval(f"scratch: a tensor is on {x.device}, the cache on {pages._dev}")
+    return x.data_ptr(), x.numel()
+
+
+def _scores(scores, n: int, nq: int) -> None:
+    """The arrays of a vla_scores fit n rows of nq heads."""
+    if scores._nq is not None and scores._nq != nq:
+        raise _einval(f"slopes holds {scores._nq} elements, q has {nq} heads")
+    for what, m in scores._rows:
+        if m != n:
+            raise _einval(f"{what} holds {m} rows, there are {n}")
+
+
 def vla_tree_attention(pages: vla_pages, layer: int, rows: vla_rows, q, out, scratch, mask=None, scale=None,
                        stream: int = 0) -> None:
     """q and out [n_rows, nq, head_dim] (rows may be strided), scratch uint8
@@ -662,6 +728,32 @@ def vla_tree_attention(pages: vla_pages, layer: int, rows: vla_rows, q, out, scr
     _check(_lib.vla_tree_attention(ctypes.byref(pages), _int32(layer, "layer"), ctypes.byref(rows), bits, words, nq,
                                    pages._scale if scale is None else scale, q.data_ptr(), ldq, out.data_ptr(), ldo,
                                    scratch.data_ptr(), scratch.numel(), stream or None))
+
+
+def vla_score_attention_scratch(pages: vla_pages, rows: vla_rows, nq: int) -> int:
+    n = ctypes.c_int64()
+    _at(pages, rows._dev)
+    _check(_lib.vla_score_attention_scratch(ctypes.byref(pages), ctypes.byref(rows), _int32(nq, "nq"),
+                                            ctypes.byref(n)))
+    return n.value
+
+
+def vla_score_attention(pages: vla_pages, layer: int, rows: vla_rows, scores: vla_scores, q, out, scratch, lse=None,
+                        mask=None, stream: int = 0) -> None:
+    """As vla_tree_attention, with scores from make_scores and lse float32
+    [n_rows, nq] or None."""
+    n = rows._n
+    ldq = _heads(q, "q", pages, n)
+    nq = q.shape[1]
+    ldo = _heads(out, "out", pages, n, nq)
+    bits, words = _mask(mask, pages, n)
+    _scores(scores, n, nq)
+    sums = _floats(lse, "lse", pages, (n, nq))
+    work = _scratch(scratch, pages)
+    _at(pages, rows._dev, scores._dev)
+    _check(_lib.vla_score_attention(ctypes.byref(pages), _int32(layer, "layer"), ctypes.byref(rows),
+                                    ctypes.byref(scores), bits, words, nq, q.data_ptr(), ldq, out.data_ptr(), ldo, sums,
+                                    *work, stream or None))
 
 
 def vla_pages_fork(pages: vla_pages, src, dst, made, stream: int = 0) -> None:
@@ -702,6 +794,6 @@ def exported_symbols() -> Iterable[str]:
             "vla_param_count", "vla_param_info", "vla_export_param", "vla_ctx_export_kv", "vla_ctx_export_cross", "vla_ctx_export_cog", "vla_wavelog_enable", "vla_wavelog_read",
             "vla_debug_gemm", "vla_debug_gemm_epi", "vla_debug_gemm_fold", "vla_debug_gemm_ln", "vla_gemm_noalloc", "vla_debug_attention", "vla_debug_attention_cache", "vla_debug_norm", "vla_debug_generate",
             "vla_debug_gemm_plan", "vla_pages_init", "vla_pages_reserve", "vla_qk_norm_rope", "vla_tree_attention",
-            "vla_tree_attention_scratch", "vla_pages_fork", "vla_pages_commit", "vla_pages_release", "vla_ctx_to_pages",
+            "vla_tree_attention_scratch", "vla_score_attention", "vla_score_attention_scratch", "vla_pages_fork", "vla_pages_commit", "vla_pages_release", "vla_ctx_to_pages",
             "vla_kernel_timer",
             "vla_kernel_timer_read", "vla_last_error"]

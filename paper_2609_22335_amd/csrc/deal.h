@@ -1,6 +1,6 @@
 // Who works on what in the attention over pages: the tiles of a batch's
 // entries, and each workgroup's share of their blocks of keys. Plain arithmetic
-// on lengths, for the device (tree.hip) and, where a test goes through every
+// on lengths, for the device (tree_dev.h) and, where a test goes through every
 // workgroup's share, for the host.
 #pragma once
 #include <hip/hip_runtime.h>
@@ -45,10 +45,17 @@ __host__ __device__ __forceinline__ uint32_t floor_sum(uint32_t n, uint32_t m, u
 // causal tile ends with its last row's own slot, so tile rt has
 // ceil((len + 1 + floor((BM (rt + 1) - 1) / group)) / unit) units, which is
 // floor((BM rt + BM - 1 + group (len + unit)) / (group unit)).
-template <int BM>
+//
+// With a window (WIN, slide()) a tile begins with the unit of the first slot
+// that its first row sees, floor((max(0, len - back + 1 + floor(BM rt / group)))
+// / unit), which from the tile on whose window begins inside the slots is
+// floor((BM rt + group (len - back + 1)) / (group unit)).
+template <int BM, bool WIN = false>
 struct Geo {
   int tiles, M, group, len, end, unit;
   bool flat;  // every tile reads all keys
+  int back;    // slots of the window (0: none)
+  bool fixed;  // rows' places are not their order: every tile begins with the entry's first
   __host__ __device__ __forceinline__ void set(int group_, bool causal, const Entry& x, int unit_) {
     group = group_;
     unit = unit_;
@@ -58,6 +65,26 @@ struct Geo {
     const long long e = (long long)x.len + x.n;
     end = e < x.cap ? (int)e : x.cap;
     flat = !causal || e > x.cap;  // (drafts without pages: no row sees them)
+    if constexpr (WIN) back = 0, fixed = true;
+  }
+  // A window of `window` slots (0: none) for rows whose places are their order
+  // or, with still set, lie somewhere behind the committed slots.
+  __host__ __device__ __forceinline__ void slide(int window, bool still) {
+    const long long e = (long long)len + M / group;
+    back = e > end || window >= e ? 0 : window;
+    fixed = still;
+  }
+  __host__ __device__ __forceinline__ int skip(int rt) const {  // units before the tile's first
+    if (!WIN || back == 0) return 0;
+    const int at = len - back + 1 + (fixed ? 0 : (int)((unsigned)(BM * rt) / (unsigned)group));
+    return at > 0 ? at / unit : 0;
+  }
+  // those of the tiles before rt
+  __host__ __device__ __forceinline__ int skipped(int rt) const {
+    if (!WIN || back == 0) return 0;
+    if (fixed) return rt * skip(0);
+    const int c = len - back + 1, i0 = c >= 0 ? 0 : (int)((unsigned)(-c * group + BM - 1) / (unsigned)BM);
+    return rt <= i0 ? 0 : (int)floor_sum(rt - i0, group * unit, BM, group * c + BM * i0);
   }
   // (a tile without keys has one unit, which writes its zeros)
   __host__ __device__ __forceinline__ int all() const { return end > 0 ? (end + unit - 1) / unit : 1; }
@@ -66,16 +93,27 @@ struct Geo {
     const int last = (rt + 1) * BM < M ? (rt + 1) * BM - 1 : M - 1;
     return len + last / group + 1;
   }
-  __host__ __device__ __forceinline__ int units(int rt) const { return flat ? all() : (tile_end(rt) + unit - 1) / unit; }
+  __host__ __device__ __forceinline__ int units(int rt) const {
+    return (flat ? all() : (tile_end(rt) + unit - 1) / unit) - skip(rt);
+  }
   // units of the tiles before rt (rt < tiles)
   __host__ __device__ __forceinline__ int before(int rt) const {
-    if (flat) return rt * all();
-    return (int)floor_sum(rt, group * unit, BM, BM - 1 + group * (len + unit));
+    if (flat) return rt * all() - skipped(rt);
+    return (int)floor_sum(rt, group * unit, BM, BM - 1 + group * (len + unit)) - skipped(rt);
   }
   __host__ __device__ __forceinline__ int sum() const { return tiles == 0 ? 0 : before(tiles - 1) + units(tiles - 1); }
   // the tile that holds unit u of the head's: units grow by a line, their sum
   // by a parabola, whose root is close
   __host__ __device__ __forceinline__ int find(int u) const {
+    if (WIN && back) {  // (neither a line nor a parabola: halves)
+      int lo = 0, hi = tiles - 1;
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (before(mid) <= u) lo = mid;
+        else hi = mid - 1;
+      }
+      return lo;
+    }
     if (flat) return u / all();
     if (tiles <= 1) return 0;
     const float first = (float)units(0), grow = (float)(units(tiles - 1) - units(0)) / (float)(tiles - 1);
@@ -102,18 +140,21 @@ struct Tile {
   int n, cap;         // (of its entry)
   int parts;          // with the first of several parts: how many, else 0
   bool whole, causal;
+  bool first;         // the tile's first part
 };
 struct Run {
   long long u, u_end;  // this run's next and last unit
   long long quota;     // units of a run
   int w;               // this run (behind the last: none)
   int per;             // blocks of a unit
+  int back;            // (as in Batch)
+  bool fixed;
 };
 
 // The run's part of tile rt, from unit u0 of its nu on.
-template <int BM, int BN>
-__host__ __device__ __forceinline__ Tile cut(Run& r, const Geo<BM>& g, const Entry& x, int head, int rt, int u0, int nu,
-                                             bool causal) {
+template <int BM, int BN, bool WIN>
+__host__ __device__ __forceinline__ Tile cut(Run& r, const Geo<BM, WIN>& g, const Entry& x, int head, int rt, int u0,
+                                             int nu, bool causal) {
   const int u1 = (int)(nu - u0 < r.u_end - r.u ? nu : u0 + (r.u_end - r.u));
   Tile t{};
   t.head = head;
@@ -127,10 +168,12 @@ __host__ __device__ __forceinline__ Tile cut(Run& r, const Geo<BM>& g, const Ent
   t.group = g.group;
   t.causal = causal;
   t.kend = g.tile_end(rt);
-  t.b0 = u0 * r.per;
+  const int s = g.skip(rt);
+  t.b0 = (s + u0) * r.per;
   const int nb = t.kend > 0 ? (t.kend + BN - 1) / BN : 1;
-  t.b1 = u1 * r.per < nb ? u1 * r.per : nb;
+  t.b1 = (s + u1) * r.per < nb ? (s + u1) * r.per : nb;
   t.whole = u0 == 0 && u1 == nu;
+  t.first = u0 == 0;
   t.parts = t.whole || u0 > 0 ? 0 : (int)(r.quota == 1 ? r.u + nu - 1 : (r.u + nu - 1) / r.quota) - r.w + 1;
   r.u += u1 - u0;
   return t;
@@ -140,6 +183,8 @@ __host__ __device__ __forceinline__ Tile cut(Run& r, const Geo<BM>& g, const Ent
 struct Batch {
   int n_ent, nkv, group, wgs;
   bool causal;
+  int back = 0;        // slots of a window (0: none), for Geo::slide()
+  bool fixed = false;
 };
 
 // All entries' units stand in a row and are dealt out in equal runs, so that
@@ -154,9 +199,10 @@ struct Batch {
 // count(causal, unit) works out their tiles and units (and returns the sum),
 // tiles() sums their tiles, at(u) is the lane whose units hold the chunk's unit
 // u, and entry(), units() and before() are what that lane has.
-template <int BM, int BN, int LONG, typename Lanes>
+template <int BM, int BN, int LONG, bool WIN = false, typename Lanes>
 __host__ __device__ __forceinline__ Tile deal(Run& r, bool first, const Batch& a, int wg, Lanes& lanes) {
   const int n_ent = a.n_ent, nkv = a.nkv;
+  if constexpr (WIN) r.back = a.back, r.fixed = a.fixed;
   long long base = 0, total = 0;
   // One loop over the entries, in passes: 0 counts blocks and tiles, 1 counts
   // units of several blocks, 2 finds the unit. (One copy of the code: what a
@@ -223,8 +269,9 @@ __host__ __device__ __forceinline__ Tile deal(Run& r, bool first, const Batch& a
   const Entry x = lanes.entry(el);
   const int persum = lanes.units(el);
   const long long at = r.u - (base + lanes.before(el));
-  Geo<BM> g;
+  Geo<BM, WIN> g;
   g.set(a.group, a.causal, x, BN * per);
+  if constexpr (WIN) g.slide(a.back, a.fixed);
   // (a head's units fit 31 bits; most entries' do as well. Divisions are long,
   // and a short call waits for each: one head and one tile need none.)
   const int head = nkv == 1 ? 0 : at >> 31 ? (int)(at / persum) : (int)((uint32_t)at / (uint32_t)persum);
@@ -235,20 +282,21 @@ __host__ __device__ __forceinline__ Tile deal(Run& r, bool first, const Batch& a
     u0 = rem - g.before(rt);
     nu = g.units(rt);
   }
-  return cut<BM, BN>(r, g, x, head, rt, u0, nu, a.causal);
+  return cut<BM, BN, WIN>(r, g, x, head, rt, u0, nu, a.causal);
 }
 // The tile behind t in the run, which holds it from its first unit on: the
 // next of its head, or of the next head; behind the entry's last head it is for
 // deal() to find (more: false).
-template <int BM, int BN>
+template <int BM, int BN, bool WIN = false>
 __host__ __device__ __forceinline__ bool more(Run& r, Tile& t, int nkv) {
   const Entry x = {t.seq, t.row0, t.n, t.len, t.cap};
-  Geo<BM> g;
+  Geo<BM, WIN> g;
   g.set(t.group, t.causal, x, BN * r.per);
+  if constexpr (WIN) g.slide(r.back, r.fixed);
   const bool same = t.rt + 1 < g.tiles;
   const int head = same ? t.head : t.head + 1, rt = same ? t.rt + 1 : 0;
   if (head >= nkv) return false;
-  t = cut<BM, BN>(r, g, x, head, rt, 0, g.units(rt), t.causal);
+  t = cut<BM, BN, WIN>(r, g, x, head, rt, 0, g.units(rt), t.causal);
   return true;
 }
 

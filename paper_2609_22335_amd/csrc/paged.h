@@ -52,6 +52,15 @@ struct RopeNormDesc {
 bool rope_norm_fits(const RopeNormDesc& d);  // (a grid holds it)
 hipError_t launch_rope_norm(const RopeNormDesc& d, hipStream_t st);
 
+// How products of queries and keys become scores, and what rows see.
+struct ScoreDesc {
+  float scale = 0.f, cap = 0.f;     // cap 0: none
+  const float* slopes = nullptr;    // [nq] or null
+  int window = 0;                   // 0: none
+  const int32_t* depth = nullptr;   // [n_rows] or null
+  const int32_t* span = nullptr;    // [n_rows][2] or null
+};
+
 struct TreeAttnDesc {
   PagedCache c;
   PagedRows r;
@@ -61,12 +70,14 @@ struct TreeAttnDesc {
   long long ldq = 0, ldo = 0;
   const uint32_t* mask = nullptr;  // [n_rows][mask_words] or null: causal
   int mask_words = 0;
-  float scale = 0.f;
+  ScoreDesc s;           // (launch_tree_attn: the scale alone)
+  float* lse = nullptr;  // [n_rows][nq] or null (launch_score_attn)
   void* scratch = nullptr;
   int cus = 256;
 };
 size_t tree_attn_scratch(const TreeAttnDesc& d);
 hipError_t launch_tree_attn(const TreeAttnDesc& d, hipStream_t st);
+hipError_t launch_score_attn(const TreeAttnDesc& d, hipStream_t st);
 
 hipError_t launch_pages_init(const PagedCache& c, hipStream_t st);
 hipError_t launch_pages_reserve(const PagedCache& c, const PagedRows& r, hipStream_t st);

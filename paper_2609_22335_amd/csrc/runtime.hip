@@ -3476,6 +3476,32 @@ int vla_tree_attention_scratch(const vla_pages* p, const vla_rows* rows, int32_t
   })
 }
 
+// The operands of an attention whose d->c, r, nq and s are set.
+static int tree_operands(TreeAttnDesc* d, const uint32_t* mask, int32_t mask_words, const void* q, int64_t ldq,
+                         void* out, int64_t ldo, void* scratch, int64_t scratch_bytes) {
+  VLA_TRY(paged_operand(d->c, "q", q, ldq, d->nq));
+  VLA_TRY(paged_operand(d->c, "out", out, ldo, d->nq));
+  const ByteRows o = paged_bytes(d->c, d->r, out, ldo, d->nq), in = paged_bytes(d->c, d->r, q, ldq, d->nq);
+  if (meet(o, in)) return fail(VLA_EINVAL, "out must not be q or overlap it");
+  VLA_TRY(device_cus(&d->cus));
+  const size_t need = tree_attn_scratch(*d);
+  if (!scratch || !aligned16(scratch) || scratch_bytes < 0 || (size_t)scratch_bytes < need)
+    return fail(VLA_EINVAL, "scratch: needs " + std::to_string(need) + " bytes, 16-byte aligned");
+  const ByteRows work{scratch, 0, (int64_t)need, 1};
+  if (meet(o, work) || meet(in, work)) return fail(VLA_EINVAL, "scratch overlaps q or out");
+  const ByteRows sums{d->lse, 0, d->lse ? (int64_t)d->r.n_rows * d->nq * 4 : 0, 1};
+  if (d->lse && (meet(sums, o) || meet(sums, in) || meet(sums, work)))
+    return fail(VLA_EINVAL, "lse overlaps q, out or scratch");
+  d->mask = mask;
+  d->mask_words = mask ? mask_words : 0;
+  d->q = q;
+  d->ldq = ldq;
+  d->out = out;
+  d->ldo = ldo;
+  d->scratch = scratch;
+  return VLA_OK;
+}
+
 int vla_tree_attention(const vla_pages* p, int32_t layer, const vla_rows* rows, const uint32_t* mask,
                        int32_t mask_words, int32_t nq, float scale, const void* q, int64_t ldq, void* out,
                        int64_t ldo, void* scratch, int64_t scratch_bytes, void* stream) {
@@ -3485,25 +3511,43 @@ int vla_tree_attention(const vla_pages* p, int32_t layer, const vla_rows* rows, 
     if (mask && (mask_words <= 0 || mask_words > (1 << 24))) return fail(VLA_EINVAL, "mask_words");
     if (!(scale > 0.f) || !std::isfinite(scale)) return fail(VLA_EINVAL, "scale must be positive and finite");
     if (d.r.n_rows == 0 || d.r.n_ent == 0) return VLA_OK;  // nothing is read or written
-    VLA_TRY(paged_operand(d.c, "q", q, ldq, nq));
-    VLA_TRY(paged_operand(d.c, "out", out, ldo, nq));
-    const ByteRows o = paged_bytes(d.c, d.r, out, ldo, nq), in = paged_bytes(d.c, d.r, q, ldq, nq);
-    if (meet(o, in)) return fail(VLA_EINVAL, "out must not be q or overlap it");
-    VLA_TRY(device_cus(&d.cus));
-    const size_t need = tree_attn_scratch(d);
-    if (!scratch || !aligned16(scratch) || scratch_bytes < 0 || (size_t)scratch_bytes < need)
-      return fail(VLA_EINVAL, "scratch: needs " + std::to_string(need) + " bytes, 16-byte aligned");
-    const ByteRows work{scratch, 0, (int64_t)need, 1};
-    if (meet(o, work) || meet(in, work)) return fail(VLA_EINVAL, "scratch overlaps q or out");
-    d.mask = mask;
-    d.mask_words = mask ? mask_words : 0;
-    d.scale = scale;
-    d.q = q;
-    d.ldq = ldq;
-    d.out = out;
-    d.ldo = ldo;
-    d.scratch = scratch;
+    d.s.scale = scale;
+    VLA_TRY(tree_operands(&d, mask, mask_words, q, ldq, out, ldo, scratch, scratch_bytes));
     return paged_launch("tree_attention", launch_tree_attn(d, (hipStream_t)stream));
+  })
+}
+
+static int paged_scores(const vla_scores* s, ScoreDesc* d) {
+  if (!s) return fail(VLA_EINVAL, "scores is NULL");
+  if (!(s->scale > 0.f) || !std::isfinite(s->scale)) return fail(VLA_EINVAL, "scale must be positive and finite");
+  if (!(s->cap >= 0.f) || !std::isfinite(s->cap) || (s->cap > 0.f && !std::isfinite(4.f * s->scale / s->cap)))
+    return fail(VLA_EINVAL, "scores: cap must be 0 or positive, finite, and not so small that scale / cap is not");
+  if (s->window < 0) return fail(VLA_EINVAL, "scores: window must not be negative");
+  d->scale = s->scale;
+  d->cap = s->cap;
+  d->slopes = s->slopes;
+  d->window = s->window;
+  d->depth = s->depth;
+  d->span = s->span;
+  return VLA_OK;
+}
+
+int vla_score_attention_scratch(const vla_pages* p, const vla_rows* rows, int32_t nq, int64_t* bytes) {
+  return vla_tree_attention_scratch(p, rows, nq, bytes);
+}
+
+int vla_score_attention(const vla_pages* p, int32_t layer, const vla_rows* rows, const vla_scores* s,
+                        const uint32_t* mask, int32_t mask_words, int32_t nq, const void* q, int64_t ldq, void* out,
+                        int64_t ldo, float* lse, void* scratch, int64_t scratch_bytes, void* stream) {
+  ABI_GUARD({
+    TreeAttnDesc d;
+    VLA_TRY(tree_desc(p, rows, layer, nq, &d));
+    VLA_TRY(paged_scores(s, &d.s));
+    if (mask && (mask_words <= 0 || mask_words > (1 << 24))) return fail(VLA_EINVAL, "mask_words");
+    if (d.r.n_rows == 0 || d.r.n_ent == 0) return VLA_OK;  // nothing is read or written
+    d.lse = lse;
+    VLA_TRY(tree_operands(&d, mask, mask_words, q, ldq, out, ldo, scratch, scratch_bytes));
+    return paged_launch("score_attention", launch_score_attn(d, (hipStream_t)stream));
   })
 }
 
