@@ -610,6 +610,26 @@ int vla_score_attention(const vla_pages* c, int32_t layer, const vla_rows* r, co
 /* Bytes of scratch (as vla_tree_attention_scratch). */
 int vla_score_attention_scratch(const vla_pages* c, const vla_rows* r, int32_t nq, int64_t* bytes);
 
+/* The attention weight that slots receive: for every slot i of an entry's
+ * sequence and every KV head h,
+ *   sum over the entry's rows and the heads of the group of exp(score - lse),
+ * scores and what rows see as at vla_score_attention with the same s and mask,
+ * lse (fp32 [n_rows][nq]) what that call wrote. mass is fp32 [layers][n_seqs]
+ * [kv_heads][max_pages page_len], a slot's place in its sequence last; the call
+ * works on its layer's part. Committed slots add the sum to what they have.
+ * This step's drafts get it anew, whatever they held; with a mask (of a tree,
+ * whose drafts move when they are committed) they get 0. All other slots, those
+ * of other sequences too, are left as they are. A row whose lse is not finite
+ * gives nothing. Sums are fp32; their order depends on the batch's lengths and
+ * shapes alone. scratch as at vla_tree_attention; mass overlaps none of q, lse
+ * and scratch. */
+int vla_attention_mass(const vla_pages* c, int32_t layer, const vla_rows* r, const vla_scores* s, const uint32_t* mask,
+                       int32_t mask_words, int32_t nq, const void* q, int64_t ldq, const float* lse, float* mass,
+                       void* scratch, int64_t scratch_bytes, void* stream);
+
+/* Bytes of scratch (may be 0; host only, but depends on the current device). */
+int vla_attention_mass_scratch(const vla_pages* c, const vla_rows* r, int32_t nq, int64_t* bytes);
+
 /* Branch: sequence dst[i] becomes a copy of src[i] (committed slots only).
  * Full pages are shared, the used slots of the last page are copied in every
  * layer to a page of the child's own. A pair is fit when both are sequences of

@@ -159,6 +159,8 @@ def _load():
         "vla_tree_attention_scratch": [P, P, I32, ctypes.POINTER(I64)],
         "vla_score_attention": [P, I32, P, P, P, I32, I32, P, I64, P, I64, P, P, I64, P],
         "vla_score_attention_scratch": [P, P, I32, ctypes.POINTER(I64)],
+        "vla_attention_mass": [P, I32, P, P, P, I32, I32, P, I64, P, P, P, I64, P],
+        "vla_attention_mass_scratch": [P, P, I32, ctypes.POINTER(I64)],
         "vla_pages_fork": [P, I32, P, P, P, P],
         "vla_pages_commit": [P, P, P, P, P],
         "vla_pages_release": [P, I32, P, P],
@@ -520,7 +522,7 @@ def make_pages(k, v, table, lens, held, refs, status) -> vla_pages:
     # what the calls compare their operands with
     p._dev, p._index, p._type, p._ints = dev, dev.index, k.dtype, table.dtype
     import torch
-    p._floats = torch.float32
+    p._floats, p._mass = torch.float32, (layers, n_seqs, nkv, wide * page)
     p._nkv, p._hd, p._scale = nkv, hd, hd ** -0.5
     return p
 
@@ -691,6 +693,12 @@ def _floats(x, what: str, pages, shape):
     return x.data_ptr()
 
 
+def _some(x, what: str):
+    if x is None:
+        raise _einval(f"{what} must be a device (cuda) tensor")
+    return x
+
+
 def _scratch(x, pages) -> tuple:
     """uint8 on the cache's device; its pointer and bytes."""
     if _dev(x, "scratch", "uint8") != pages._dev:
@@ -756,6 +764,31 @@ def vla_score_attention(pages: vla_pages, layer: int, rows: vla_rows, scores: vl
                                     *work, stream or None))
 
 
+def vla_attention_mass_scratch(pages: vla_pages, rows: vla_rows, nq: int) -> int:
+    n = ctypes.c_int64()
+    _at(pages, rows._dev)
+    _check(_lib.vla_attention_mass_scratch(ctypes.byref(pages), ctypes.byref(rows), _int32(nq, "nq"), ctypes.byref(n)))
+    return n.value
+
+
+def vla_attention_mass(pages: vla_pages, layer: int, rows: vla_rows, scores: vla_scores, q, lse, mass, scratch,
+                       mask=None, stream: int = 0) -> None:
+    """q [n_rows, nq, head_dim] (rows may be strided), lse float32 [n_rows,
+    nq], mass float32 [layers, n_seqs, kv_heads, max_pages * page_len]."""
+    n = rows._n
+    ldq = _heads(q, "q", pages, n)
+    nq = q.shape[1]
+    bits, words = _mask(mask, pages, n)
+    _scores(scores, n, nq)
+    sums = _floats(_some(lse, "lse"), "lse", pages, (n, nq))
+    to = _floats(_some(mass, "mass"), "mass", pages, pages._mass)
+    work = _scratch(scratch, pages)
+    _at(pages, rows._dev, scores._dev)
+    _check(_lib.vla_attention_mass(ctypes.byref(pages), _int32(layer, "layer"), ctypes.byref(rows),
+                                   ctypes.byref(scores), bits, words, nq, q.data_ptr(), ldq, sums, to, *work,
+                                   stream or None))
+
+
 def vla_pages_fork(pages: vla_pages, src, dst, made, stream: int = 0) -> None:
     """src, dst, made: int32 [n]."""
     n = _list(src, "src")
@@ -794,6 +827,7 @@ def exported_symbols() -> Iterable[str]:
             "vla_param_count", "vla_param_info", "vla_export_param", "vla_ctx_export_kv", "vla_ctx_export_cross", "vla_ctx_export_cog", "vla_wavelog_enable", "vla_wavelog_read",
             "vla_debug_gemm", "vla_debug_gemm_epi", "vla_debug_gemm_fold", "vla_debug_gemm_ln", "vla_gemm_noalloc", "vla_debug_attention", "vla_debug_attention_cache", "vla_debug_norm", "vla_debug_generate",
             "vla_debug_gemm_plan", "vla_pages_init", "vla_pages_reserve", "vla_qk_norm_rope", "vla_tree_attention",
-            "vla_tree_attention_scratch", "vla_score_attention", "vla_score_attention_scratch", "vla_pages_fork", "vla_pages_commit", "vla_pages_release", "vla_ctx_to_pages",
+            "vla_tree_attention_scratch", "vla_score_attention", "vla_score_attention_scratch", "vla_attention_mass",
+            "vla_attention_mass_scratch", "vla_pages_fork", "vla_pages_commit", "vla_pages_release", "vla_ctx_to_pages",
             "vla_kernel_timer",
             "vla_kernel_timer_read", "vla_last_error"]

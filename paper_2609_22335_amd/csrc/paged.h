@@ -79,6 +79,13 @@ size_t tree_attn_scratch(const TreeAttnDesc& d);
 hipError_t launch_tree_attn(const TreeAttnDesc& d, hipStream_t st);
 hipError_t launch_score_attn(const TreeAttnDesc& d, hipStream_t st);
 
+struct MassDesc {
+  TreeAttnDesc t;         // (out and ldo do not count; lse is read)
+  float* mass = nullptr;  // [layers][n_seqs][nkv][max_pages page]
+};
+size_t mass_scratch(const MassDesc& d);
+hipError_t launch_mass(const MassDesc& d, hipStream_t st);
+
 hipError_t launch_pages_init(const PagedCache& c, hipStream_t st);
 hipError_t launch_pages_reserve(const PagedCache& c, const PagedRows& r, hipStream_t st);
 bool fork_fits(const PagedCache& c, int n);

@@ -3551,6 +3551,54 @@ int vla_score_attention(const vla_pages* p, int32_t layer, const vla_rows* rows,
   })
 }
 
+// A cache's weights of slots, whole.
+static ByteRows mass_bytes(const PagedCache& c, const float* mass) {
+  const int64_t w = (int64_t)c.layers * c.n_seqs * c.nkv * ((int64_t)c.max_pages << c.page_lg) * 4;
+  return ByteRows{mass, 0, w, 1};
+}
+
+int vla_attention_mass_scratch(const vla_pages* p, const vla_rows* rows, int32_t nq, int64_t* bytes) {
+  ABI_GUARD({
+    if (!bytes) return fail(VLA_EINVAL, "bytes is NULL");
+    MassDesc d;
+    VLA_TRY(tree_desc(p, rows, 0, nq, &d.t));
+    VLA_TRY(device_cus(&d.t.cus));
+    *bytes = (int64_t)mass_scratch(d);
+    return VLA_OK;
+  })
+}
+
+int vla_attention_mass(const vla_pages* p, int32_t layer, const vla_rows* rows, const vla_scores* s,
+                       const uint32_t* mask, int32_t mask_words, int32_t nq, const void* q, int64_t ldq,
+                       const float* lse, float* mass, void* scratch, int64_t scratch_bytes, void* stream) {
+  ABI_GUARD({
+    MassDesc d;
+    VLA_TRY(tree_desc(p, rows, layer, nq, &d.t));
+    VLA_TRY(paged_scores(s, &d.t.s));
+    if (mask && (mask_words <= 0 || mask_words > (1 << 24))) return fail(VLA_EINVAL, "mask_words");
+    if (d.t.r.n_rows == 0 || d.t.r.n_ent == 0) return VLA_OK;  // nothing is read or written
+    VLA_TRY(paged_operand(d.t.c, "q", q, ldq, nq));
+    if (!lse || !mass) return fail(VLA_EINVAL, "lse or mass is NULL");
+    VLA_TRY(device_cus(&d.t.cus));
+    const size_t need = mass_scratch(d);
+    if (scratch_bytes < 0 || (need && (!scratch || !aligned16(scratch) || (size_t)scratch_bytes < need)))
+      return fail(VLA_EINVAL, "scratch: needs " + std::to_string(need) + " bytes, 16-byte aligned");
+    const ByteRows to = mass_bytes(d.t.c, mass), work{scratch, 0, (int64_t)need, 1};
+    const ByteRows in = paged_bytes(d.t.c, d.t.r, q, ldq, nq), sums{lse, 0, (int64_t)d.t.r.n_rows * nq * 4, 1};
+    if (meet(to, in) || meet(to, sums)) return fail(VLA_EINVAL, "mass overlaps q or lse");
+    if (need && (meet(work, to) || meet(work, in) || meet(work, sums)))
+      return fail(VLA_EINVAL, "scratch overlaps q, lse or mass");
+    d.t.mask = mask;
+    d.t.mask_words = mask ? mask_words : 0;
+    d.t.q = q;
+    d.t.ldq = ldq;
+    d.t.lse = const_cast<float*>(lse);
+    d.t.scratch = scratch;
+    d.mass = mass;
+    return paged_launch("attention_mass", launch_mass(d, (hipStream_t)stream));
+  })
+}
+
 int vla_pages_fork(const vla_pages* p, int32_t n, const int32_t* src, const int32_t* dst, int32_t* made,
                    void* stream) {
   ABI_GUARD({

@@ -598,25 +598,29 @@ __device__ __forceinline__ void add_odd_values(const Tile& t, int kb, uint32_t s
 // more than the score's own rounding (y^2 below 1/4: what is cut off is less
 // than 2^-23 of y).
 template <typename T>
+__device__ __forceinline__ void cap_scores(f32x16& s, const Args& a) {
+#pragma unroll
+  for (int j = 0; j < 16; ++j) {
+    const float z = s[j] * a.k1;  // 2 y log2(e)
+    float v = __builtin_fmaf(-2.f * a.cap2, __builtin_amdgcn_rcpf(ex2(z) + 1.f), a.cap2);
+    if constexpr (sizeof(T) == 4) {
+      const float y = z * 0.34657359f, y2 = y * y;  // (ln 2 / 2)
+      float p = 0.0035921280f;                      // 21844 / 6081075
+      p = __builtin_fmaf(p, y2, -0.0088632355f);    // -1382 / 155925
+      p = __builtin_fmaf(p, y2, 0.021869488f);      // 62 / 2835
+      p = __builtin_fmaf(p, y2, -0.053968254f);     // -17 / 315
+      p = __builtin_fmaf(p, y2, 0.13333333f);       // 2 / 15
+      p = __builtin_fmaf(p, y2, -0.33333333f);      // -1 / 3
+      v = y2 < 0.25f ? a.cap2 * __builtin_fmaf(y * y2, p, y) : v;
+    }
+    s[j] = v;
+  }
+}
+template <typename T>
 __device__ __forceinline__ void shape(f32x16& s, const Args& a, const Tile& t, int kb, const Row& x) {
   const int h4 = 4 * (int)((threadIdx.x >> 5) & 1);
   if (a.cap2 > 0.f) {
-#pragma unroll
-    for (int j = 0; j < 16; ++j) {
-      const float z = s[j] * a.k1;  // 2 y log2(e)
-      float v = __builtin_fmaf(-2.f * a.cap2, __builtin_amdgcn_rcpf(ex2(z) + 1.f), a.cap2);
-      if constexpr (sizeof(T) == 4) {
-        const float y = z * 0.34657359f, y2 = y * y;  // (ln 2 / 2)
-        float p = 0.0035921280f;                      // 21844 / 6081075
-        p = __builtin_fmaf(p, y2, -0.0088632355f);    // -1382 / 155925
-        p = __builtin_fmaf(p, y2, 0.021869488f);      // 62 / 2835
-        p = __builtin_fmaf(p, y2, -0.053968254f);     // -17 / 315
-        p = __builtin_fmaf(p, y2, 0.13333333f);       // 2 / 15
-        p = __builtin_fmaf(p, y2, -0.33333333f);      // -1 / 3
-        v = y2 < 0.25f ? a.cap2 * __builtin_fmaf(y * y2, p, y) : v;
-      }
-      s[j] = v;
-    }
+    cap_scores<T>(s, a);
   } else {
 #pragma unroll
     for (int j = 0; j < 16; ++j) s[j] *= a.c2;

@@ -108,3 +108,44 @@ def test_score_attention(V, T, hd, nq, nkv, page, cap, bias, window, span, tree,
     off = np.abs(gl[ok] - ln[ok]) / ltol[ok]
     assert np.all(off <= 1), float(np.nanmax(off))
     d.same()
+
+
+def weights_dev(rng, m, layers=2):
+    slots = m.max_pages * m.page
+    return rng.random((layers, m.n_seqs, m.dims[2], slots)).astype(np.float32)
+
+
+@pytest.mark.parametrize("T,hd,nq,nkv,page,cap,bias,window,span,tree,lens,rows", CASES + [
+    (T16, 128, 4, 1, 16, 0.0, False, 0, None, None, [3000], [1]),
+    (T16, 64, 8, 8, 16, 0.0, False, 0, None, None, [2000, 130], [1, 1]),
+    (T16, 128, 8, 1, 64, 0.0, False, 0, None, None, [0], [700]),
+    (T32, 64, 3, 1, 16, 0.0, False, 0, None, None, [0, 129], [200, 5]),
+])
+def test_attention_mass(V, T, hd, nq, nkv, page, cap, bias, window, span, tree, lens, rows):
+    say(f"mass {T} hd={hd} nq={nq} nkv={nkv} page={page} cap={cap} bias={bias} window={window} span={span} "
+        f"tree={tree} lens={lens} rows={rows}")
+    rng = np.random.default_rng(hd * 5 + nq * 3 + len(lens) + sum(lens) + window)
+    m, order, counts, start, n_rows, q, sc = batch(V, rng, T, hd, nq, nkv, page, cap, bias, window, span, tree, lens, rows)
+    d = Dev(V, m, T)
+    qd = torch.from_numpy(q).to(T).cuda()
+    lse = S.attention(m, T is T32, 1, order, start, counts, q, sc, 1)[2].astype(np.float32)
+    lse[rng.random(lse.shape) < 0.05] = np.nan
+    lse[rng.random(lse.shape) < 0.05] = np.inf
+    mask = None if sc.bits is None else torch.from_numpy(pack(sc.bits)).cuda()
+    r = V.make_rows(i32(start), n_rows, i32(order))
+    scratch = torch.full((max(16, V.vla_attention_mass_scratch(d.p, r, nq)),), 255, dtype=torch.uint8, device="cuda")
+    before = weights_dev(rng, m)
+    # drafts' slots may hold anything
+    for s in range(len(lens)):
+        before[1, s, :, lens[s]:lens[s] + rows[s]] = np.nan
+    mass = torch.from_numpy(before).cuda()
+    V.vla_attention_mass(d.p, 1, r, sc.make(V, d.p, torch), qd, torch.from_numpy(lse).cuda(), mass, scratch, mask=mask)
+    want, tol = S.mass(m, T is T32, 1, order, start, counts, q, sc, lse, before[1])
+    torch.cuda.synchronize()
+    got = mass.cpu().numpy()
+    assert np.array_equal(got[0], before[0])
+    left = tol == 0
+    assert np.array_equal(got[1][left], before[1][left])
+    off = np.abs(got[1][~left].astype(np.float64) - want[~left]) / tol[~left]
+    assert np.all(off <= 1), float(np.nanmax(off))
+    d.same()
