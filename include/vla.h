@@ -630,6 +630,36 @@ int vla_attention_mass(const vla_pages* c, int32_t layer, const vla_rows* r, con
 /* Bytes of scratch (may be 0; host only, but depends on the current device). */
 int vla_attention_mass_scratch(const vla_pages* c, const vla_rows* r, int32_t nq, int64_t* bytes);
 
+/* Cut sequences back to their weightiest slots. seqs and keep: int32 [n]; a
+ * sequence with more than keep[i] committed slots keeps its first `first`, its
+ * last `last` and of the others those with the largest weight, the sum of mass
+ * (as vla_attention_mass makes it) over layers and KV heads in 64 bits; of
+ * equal ones the lower slots, and so of the first and last where they are more
+ * than keep[i]. Weights that are negative or not a number count as 0. The kept
+ * slots close ranks in their order, K and V in every layer, and the pages
+ * behind them, those for drafts too, are free again where no other sequence
+ * holds them; a shared page that would have to change is replaced by one of the
+ * sequence's own, and a sequence for which there is none free stays as it is
+ * (VLA_PAGES_OUT). Since keys stay as they were rotated, later rows go on with
+ * the positions that they would have had; spans, windows and slopes count slots
+ * as they lie now.
+ *
+ * kept (int32 [n][max_pages page_len]) gets, in its row i, the old slots of the
+ * sequence's new ones, ascending (all of them where nothing was cut), and keeps
+ * the rest. mass_out gets the sequence's weights in the same way in every layer
+ * and head, and 0 behind them up to the end of the pages that it had; it may be
+ * mass itself, or else overlaps it nowhere. Entries whose sequence is not in 0
+ * .. n_seqs - 1 are skipped, so is a sequence that was listed before, and one
+ * whose keep is negative (VLA_PAGES_BAD). scratch: vla_pages_evict_scratch
+ * bytes, 16-byte aligned. kept, scratch and mass_out are apart from each other
+ * and from seqs and keep. */
+int vla_pages_evict(const vla_pages* c, int32_t n, const int32_t* seqs, const int32_t* keep, int32_t first,
+                    int32_t last, const float* mass, float* mass_out, int32_t* kept, void* scratch,
+                    int64_t scratch_bytes, void* stream);
+
+/* Bytes of scratch for n sequences (host only). */
+int vla_pages_evict_scratch(const vla_pages* c, int32_t n, int64_t* bytes);
+
 /* Branch: sequence dst[i] becomes a copy of src[i] (committed slots only).
  * Full pages are shared, the used slots of the last page are copied in every
  * layer to a page of the child's own. A pair is fit when both are sequences of

@@ -161,6 +161,8 @@ def _load():
         "vla_score_attention_scratch": [P, P, I32, ctypes.POINTER(I64)],
         "vla_attention_mass": [P, I32, P, P, P, I32, I32, P, I64, P, P, P, I64, P],
         "vla_attention_mass_scratch": [P, P, I32, ctypes.POINTER(I64)],
+        "vla_pages_evict": [P, I32, P, P, I32, I32, P, P, P, P, I64, P],
+        "vla_pages_evict_scratch": [P, I32, ctypes.POINTER(I64)],
         "vla_pages_fork": [P, I32, P, P, P, P],
         "vla_pages_commit": [P, P, P, P, P],
         "vla_pages_release": [P, I32, P, P],
@@ -789,6 +791,28 @@ def vla_attention_mass(pages: vla_pages, layer: int, rows: vla_rows, scores: vla
                                    stream or None))
 
 
+def vla_pages_evict_scratch(pages: vla_pages, n: int) -> int:
+    b = ctypes.c_int64()
+    _at(pages)
+    _check(_lib.vla_pages_evict_scratch(ctypes.byref(pages), _int32(n, "n"), ctypes.byref(b)))
+    return b.value
+
+
+def vla_pages_evict(pages: vla_pages, seqs, keep, mass, mass_out, kept, scratch, first: int = 0, last: int = 0,
+                    stream: int = 0) -> None:
+    """seqs and keep int32 [n], mass and mass_out float32 [layers, n_seqs,
+    kv_heads, max_pages * page_len] (may be one tensor), kept int32 [n,
+    max_pages * page_len]."""
+    n = _list(seqs, "seqs")
+    inp, out = (_floats(_some(x, what), what, pages, pages._mass) for what, x in (("mass", mass), ("mass_out", mass_out)))
+    to = _ints(_some(kept, "kept"), "kept", pages, (n[0], pages._mass[3]))
+    work = _scratch(scratch, pages)
+    _at(pages)
+    _check(_lib.vla_pages_evict(ctypes.byref(pages), n[0], _ints(seqs, "seqs", pages, n),
+                                _ints(_some(keep, "keep"), "keep", pages, n), _int32(first, "first"),
+                                _int32(last, "last"), inp, out, to, *work, stream or None))
+
+
 def vla_pages_fork(pages: vla_pages, src, dst, made, stream: int = 0) -> None:
     """src, dst, made: int32 [n]."""
     n = _list(src, "src")
@@ -828,6 +852,6 @@ def exported_symbols() -> Iterable[str]:
             "vla_debug_gemm", "vla_debug_gemm_epi", "vla_debug_gemm_fold", "vla_debug_gemm_ln", "vla_gemm_noalloc", "vla_debug_attention", "vla_debug_attention_cache", "vla_debug_norm", "vla_debug_generate",
             "vla_debug_gemm_plan", "vla_pages_init", "vla_pages_reserve", "vla_qk_norm_rope", "vla_tree_attention",
             "vla_tree_attention_scratch", "vla_score_attention", "vla_score_attention_scratch", "vla_attention_mass",
-            "vla_attention_mass_scratch", "vla_pages_fork", "vla_pages_commit", "vla_pages_release", "vla_ctx_to_pages",
+            "vla_attention_mass_scratch", "vla_pages_evict", "vla_pages_evict_scratch", "vla_pages_fork", "vla_pages_commit", "vla_pages_release", "vla_ctx_to_pages",
             "vla_kernel_timer",
             "vla_kernel_timer_read", "vla_last_error"]

@@ -46,7 +46,8 @@ def build(verbose: bool = False) -> str:
          os.path.join(CSRC, "gen.cpp"), "-o", gen_o],
     ]
     objs = [gen_o]
-    for src in ("kernels.hip", "runtime.hip", "paged.hip", "tree.hip", "scores.hip", "mass.hip"):
+    for src in ("kernels.hip", "runtime.hip", "paged.hip", "tree.hip", "scores.hip", "mass.hip",
+                "evict.hip"):
         o = os.path.join(BUILD, src.replace(".hip", ".o"))
         jobs.append([HIPCC, *HIP_FLAGS, "-c", os.path.join(CSRC, src), "-o", o])
         objs.append(o)

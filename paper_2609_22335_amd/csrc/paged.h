@@ -95,6 +95,20 @@ hipError_t launch_pages_commit(const PagedCache& c, const PagedRows& r, const in
                                hipStream_t st);
 hipError_t launch_pages_release(const PagedCache& c, int n, const int32_t* seqs, hipStream_t st);
 
+struct EvictDesc {
+  PagedCache c;
+  int n = 0;
+  const int32_t *seqs = nullptr, *keep = nullptr;  // [n]
+  int first = 0, last = 0;
+  const float* mass = nullptr;  // [layers][n_seqs][nkv][max_pages page]
+  float* mass_out = nullptr;    // likewise; may be mass
+  int32_t* kept = nullptr;      // [n][max_pages page]
+  void* scratch = nullptr;
+};
+size_t evict_scratch(const PagedCache& c, int n);
+bool evict_fits(const PagedCache& c, int n);  // (grids hold it)
+hipError_t launch_pages_evict(const EvictDesc& d, hipStream_t st);
+
 // The prefix rows 0 .. rows - 1 of a context (K and V in the KV-cache layout,
 // nb 32-key blocks per KV head, layers lk / lv elements apart) to the slots
 // behind sequence seq's committed ones, in every layer.

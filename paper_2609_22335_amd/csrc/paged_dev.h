@@ -119,6 +119,59 @@ __device__ __forceinline__ int page_of(const PagedCache& c, int s, int slot, int
 __device__ __forceinline__ size_t slot_elem(const PagedCache& c, int layer, int p, int j, int at) {
   return ((((size_t)layer * c.n_pages + p) * c.nkv + j) * c.page + at) * c.hd;
 }
+// Exclusive prefix of x over the workgroup, and the total.
+template <int PT, typename I>
+__device__ __forceinline__ I block_scan(I x, I* total) {
+  __shared__ I sW[PT / 64];
+  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+  const I s = wave_scan(x);
+  __syncthreads();  // the last call's sums are read
+  if (lane == 63) sW[wv] = s;
+  __syncthreads();
+  I before = 0, all = 0;
+#pragma unroll
+  for (int i = 0; i < PT / 64; ++i) {
+    const I v = sW[i];
+    before += i < wv ? v : 0;
+    all += v;
+  }
+  *total = all;
+  return before + s - x;
+}
+
+// Which of the thread's eight pages of the 8 PT from `base` on are free.
+__device__ __forceinline__ unsigned free_bits(const PagedCache& c, int base) {
+  const int first = base + 8 * threadIdx.x;
+  unsigned bits = 0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int p = first + j < c.n_pages ? first + j : c.n_pages - 1;
+    if (c.refs[p] == 0 && first + j < c.n_pages) bits |= 1u << j;
+  }
+  return bits;
+}
+// The next `want` (<= PT) free pages from page *pos on, ascending, into list;
+// returns how many there are and moves *pos behind the last one taken. Pages
+// that this launch gave out lie before *pos, so refs may be read as it was;
+// bits0 is free_bits(0), which a kernel reads while it has nothing else.
+template <int PT>
+__device__ __forceinline__ int take_free(const PagedCache& c, unsigned bits0, int* pos, int want, int* list) {
+  int found = 0, p0 = *pos;
+  for (int base = p0 & ~(8 * PT - 1); found < want && base < c.n_pages; base += 8 * PT) {
+    const int first = base + 8 * threadIdx.x;
+    unsigned bits = base == 0 ? bits0 : free_bits(c, base);
+    if (first < p0) bits &= p0 - first < 8 ? ~0u << (p0 - first) : 0u;
+    int total;
+    int rank = found + block_scan<PT>((int)__popc(bits), &total);
+    for (; bits && rank < want; bits &= bits - 1, ++rank) list[rank] = first + __ffs(bits) - 1;
+    found += total;
+  }
+  __syncthreads();
+  const int got = found < want ? found : want;
+  *pos = found < want ? c.n_pages : got ? list[got - 1] + 1 : p0;
+  return got;
+}
+
 __device__ __forceinline__ void flag(const PagedCache& c, int bit) { atomicOr(c.status, bit); }
 
 }  // namespace pg

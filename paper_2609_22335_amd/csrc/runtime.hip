@@ -3361,6 +3361,9 @@ static int paged_layer(const PagedCache& c, int32_t layer, int32_t nq) {
 // 3.7 ms, 65,536 in 227 ms), which must not hold the GPU for long.
 constexpr int FORK_MOST = 1 << 17;
 
+// Sequences of an eviction.
+constexpr int EVICT_MOST = 1 << 14;
+
 static int paged_launch(const char* what, hipError_t e) {
   if (e == GRID_FULL) return fail(VLA_EUNSUPPORTED, std::string(what) + ": more workgroups than a grid holds");
   if (e != hipSuccess) return fail(VLA_EHIP, std::string(what) + ": " + hipGetErrorString(e));
@@ -3596,6 +3599,61 @@ int vla_attention_mass(const vla_pages* p, int32_t layer, const vla_rows* rows, 
     d.t.scratch = scratch;
     d.mass = mass;
     return paged_launch("attention_mass", launch_mass(d, (hipStream_t)stream));
+  })
+}
+
+static int evict_size(const vla_pages* p, int32_t n, PagedCache* c) {
+  VLA_TRY(paged_cache(p, c));
+  if (n < 0) return fail(VLA_EINVAL, "n must not be negative");
+  // (every entry looks through those before it, and one workgroup deals the pages)
+  if (n > EVICT_MOST) return fail(VLA_EUNSUPPORTED, "pages evict: at most 2^14 sequences a call");
+  if (!evict_fits(*c, n)) return paged_launch("pages evict", GRID_FULL);
+  return VLA_OK;
+}
+
+int vla_pages_evict_scratch(const vla_pages* p, int32_t n, int64_t* bytes) {
+  ABI_GUARD({
+    if (!bytes) return fail(VLA_EINVAL, "bytes is NULL");
+    PagedCache c;
+    VLA_TRY(evict_size(p, n, &c));
+    *bytes = (int64_t)evict_scratch(c, n);
+    return VLA_OK;
+  })
+}
+
+int vla_pages_evict(const vla_pages* p, int32_t n, const int32_t* seqs, const int32_t* keep, int32_t first,
+                    int32_t last, const float* mass, float* mass_out, int32_t* kept, void* scratch,
+                    int64_t scratch_bytes, void* stream) {
+  ABI_GUARD({
+    EvictDesc d;
+    VLA_TRY(evict_size(p, n, &d.c));
+    if (first < 0 || last < 0) return fail(VLA_EINVAL, "first and last must not be negative");
+    if (n == 0) return VLA_OK;
+    if (!seqs || !keep || !mass || !mass_out || !kept) return fail(VLA_EINVAL, "NULL argument");
+    const size_t need = evict_scratch(d.c, n);
+    if (!scratch || !aligned16(scratch) || scratch_bytes < 0 || (size_t)scratch_bytes < need)
+      return fail(VLA_EINVAL, "scratch: needs " + std::to_string(need) + " bytes, 16-byte aligned");
+    const ByteRows in = mass_bytes(d.c, mass), out = mass_bytes(d.c, mass_out), work{scratch, 0, (int64_t)need, 1};
+    const ByteRows list{kept, 0, (int64_t)n * ((int64_t)d.c.max_pages << d.c.page_lg) * 4, 1};
+    const ByteRows from{seqs, 0, (int64_t)n * 4, 1}, most{keep, 0, (int64_t)n * 4, 1};
+    if (mass_out != mass && meet(in, out)) return fail(VLA_EINVAL, "mass_out overlaps mass and is not mass");
+    const ByteRows* wrote[3] = {&out, &list, &work};
+    for (int i = 0; i < 3; ++i) {
+      if (meet(*wrote[i], from) || meet(*wrote[i], most) || (i > 0 && meet(*wrote[i], in)))
+        return fail(VLA_EINVAL, "mass_out, kept or scratch overlaps what the call reads");
+      for (int j = 0; j < i; ++j)
+        if (meet(*wrote[i], *wrote[j])) return fail(VLA_EINVAL, "mass_out, kept and scratch must not overlap");
+    }
+    d.n = n;
+    d.seqs = seqs;
+    d.keep = keep;
+    d.first = first;
+    d.last = last;
+    d.mass = mass;
+    d.mass_out = mass_out;
+    d.kept = kept;
+    d.scratch = scratch;
+    return paged_launch("pages evict", launch_pages_evict(d, (hipStream_t)stream));
   })
 }
 
