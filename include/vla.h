@@ -630,6 +630,54 @@ int vla_attention_mass(const vla_pages* c, int32_t layer, const vla_rows* r, con
 /* Bytes of scratch (may be 0; host only, but depends on the current device). */
 int vla_attention_mass_scratch(const vla_pages* c, const vla_rows* r, int32_t nq, int64_t* bytes);
 
+/* Drafted tokens and what they are judged by. A step's entry has its decided
+ * token in its first row and its drafts behind it; probs' row t is the target's
+ * distribution of what follows row t's token. */
+typedef struct vla_drafts {
+  int32_t dtype;          /* VLA_F32 or VLA_BF16: probs and drafted               */
+  int32_t vocab;
+  const int32_t* tokens;  /* [n_rows] (an entry's first: not read)                */
+  const int32_t* parent;  /* [n_rows]: the row (of the entry) that a draft follows, */
+                          /*   which stands before it; NULL: the row before       */
+  const void* probs;      /* [n_rows][vocab]                                      */
+  int64_t ld_probs;       /* elements between rows, >= vocab                      */
+  const void* drafted;    /* [n_rows][vocab]: what the drafts that follow a row   */
+  int64_t ld_drafted;     /*   were drawn from, each on its own; NULL: the drafts  */
+                          /*   were chosen without chance                         */
+  const float* uniform;   /* fp32 [n_rows] in [0, 1): a draft's number, and in the */
+                          /*   first row the one that the next token is drawn with */
+                          /*   NULL: only the likeliest tokens are kept           */
+} vla_drafts;
+
+/* Which drafts are kept, and the token behind them, so that what an entry
+ * answers is distributed as the target alone would have it. The walk begins at
+ * the entry's first row, with p = its probs, and takes its drafts in order.
+ * One that follows the row the walk is at, with token x and number u, is kept
+ * when u q(x) Z < r(x), r = max(p - S q, 0), S = 0 and Z = 1 at first (drafted
+ * given), or when u Z < r(x), r = p, Z = 1 at first (drafted NULL); the walk
+ * then goes on from it. If it is not, S grows by Z and Z becomes the sum of r,
+ * or r(x) is taken from Z and becomes 0. Where the walk ends, next is the first
+ * token t for which r(0) + ... + r(t) passes u times the sum of r, u the first
+ * row's number; of p, where r is 0 everywhere. With uniform NULL a draft is kept
+ * when it is the likeliest token of the row that it follows (the lowest of
+ * several), and next is the last row's. All of it is computed in 64 bits;
+ * probabilities are taken as they are given, negative ones and NaN as 0.
+ *
+ * kept[start[e] + j] gets, for j < n_kept[e], the rows (of the entry, ascending,
+ * 0 first) that are kept, and -1 behind them, as vla_pages_commit takes it.
+ * n_kept and next: int32 [n_entries]. A draft whose parent does not stand before
+ * it or whose token is outside the vocabulary is passed over, and next is -1
+ * where p has no sum or an infinite one, or no likeliest token (VLA_PAGES_BAD
+ * each). An entry without rows has n_kept 0 and next -1. Of c the sequences
+ * (which entries are padding) and the status count. scratch:
+ * vla_verify_drafts_scratch bytes, 16-byte aligned; kept, n_kept, next and
+ * scratch overlap nothing else of the call. */
+int vla_verify_drafts(const vla_pages* c, const vla_rows* r, const vla_drafts* d, int32_t* kept, int32_t* n_kept,
+                      int32_t* next, void* scratch, int64_t scratch_bytes, void* stream);
+
+/* Bytes of scratch (host only). */
+int vla_verify_drafts_scratch(const vla_pages* c, const vla_rows* r, int32_t vocab, int64_t* bytes);
+
 /* Cut sequences back to their weightiest slots. seqs and keep: int32 [n]; a
  * sequence with more than keep[i] committed slots keeps its first `first`, its
  * last `last` and of the others those with the largest weight, the sum of mass

@@ -92,6 +92,12 @@ class vla_scores(ctypes.Structure):
                 ("window", ctypes.c_int32), ("depth", ctypes.c_void_p), ("span", ctypes.c_void_p)]
 
 
+class vla_drafts(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("vocab", ctypes.c_int32), ("tokens", ctypes.c_void_p),
+                ("parent", ctypes.c_void_p), ("probs", ctypes.c_void_p), ("ld_probs", ctypes.c_int64),
+                ("drafted", ctypes.c_void_p), ("ld_drafted", ctypes.c_int64), ("uniform", ctypes.c_void_p)]
+
+
 PAGES_OUT, PAGES_BAD = 1, 2  # bits of a paged cache's status
 
 DEBUG_EPI = {"bias": 0, "t": 1, "gelu": 2, "swish": 3, "geglu": 4, "qkv_rope": 5, "qkv_plain": 6, "step": 7,
@@ -163,6 +169,8 @@ def _load():
         "vla_attention_mass_scratch": [P, P, I32, ctypes.POINTER(I64)],
         "vla_pages_evict": [P, I32, P, P, I32, I32, P, P, P, P, I64, P],
         "vla_pages_evict_scratch": [P, I32, ctypes.POINTER(I64)],
+        "vla_verify_drafts": [P, P, P, P, P, P, P, I64, P],
+        "vla_verify_drafts_scratch": [P, P, I32, ctypes.POINTER(I64)],
         "vla_pages_fork": [P, I32, P, P, P, P],
         "vla_pages_commit": [P, P, P, P, P],
         "vla_pages_release": [P, I32, P, P],
@@ -791,6 +799,51 @@ def vla_attention_mass(pages: vla_pages, layer: int, rows: vla_rows, scores: vla
                                    stream or None))
 
 
+def vla_verify_drafts_scratch(pages: vla_pages, rows: vla_rows, vocab: int) -> int:
+    n = ctypes.c_int64()
+    _at(pages, rows._dev)
+    _check(_lib.vla_verify_drafts_scratch(ctypes.byref(pages), ctypes.byref(rows), _int32(vocab, "vocab"),
+                                          ctypes.byref(n)))
+    return n.value
+
+
+def _probs(x, what: str, pages, n: int, like=None) -> int:
+    """[n, vocab] of float32 or bfloat16 (and of `like`'s type and width) on the
+    cache's device, a row's values side by side; the row stride."""
+    if not hasattr(x, "get_device") or not getattr(x, "is_cuda", False):
+        raise _einval(f"{what} must be a device (cuda) tensor")
+    if len(x.shape) != 2 or x.shape[0] != n or (like is not None and x.shape[1] != like.shape[1]):
+        raise _einval(f"{what} must be [{n}, {'vocab' if like is None else like.shape[1]}], got {tuple(x.shape)}")
+    kind = str(x.dtype).replace("torch.", "")
+    if kind not in ("float32", "bfloat16") or (like is not None and x.dtype != like.dtype):
+        raise _einval(f"{what} must be {'float32 or bfloat16' if like is None else like.dtype}, got {x.dtype}")
+    if x.get_device() != pages._index:
+        raise _einval(f"{what}: a tensor is on {x.device}, the cache on {pages._dev}")
+    if x.stride()[1] != 1 and x.shape[1] > 1:
+        raise _einval(f"{what}: a row's values must be contiguous")
+    return x.stride()[0] if n > 1 else x.shape[1]
+
+
+def vla_verify_drafts(pages: vla_pages, rows: vla_rows, tokens, probs, kept, n_kept, next, scratch, parent=None,
+                      drafted=None, uniform=None, stream: int = 0) -> None:
+    """tokens, parent (or None) and kept int32 [n_rows], probs and drafted (or
+    None) [n_rows, vocab] (float32 or bfloat16; rows may be strided), uniform
+    float32 [n_rows] or None, n_kept and next int32 [n_entries]."""
+    n, m = (rows._n,), (rows._entries,)
+    ldp = _probs(probs, "probs", pages, n[0])
+    ldq = 0 if drafted is None else _probs(drafted, "drafted", pages, n[0], probs)
+    kind = VLA_F32 if probs.dtype == pages._floats else VLA_BF16
+    d = vla_drafts(kind, probs.shape[1], _ints(_some(tokens, "tokens"), "tokens", pages, n),
+                   _ints(parent, "parent", pages, n), probs.data_ptr(), ldp, _ptr(drafted), ldq,
+                   _floats(uniform, "uniform", pages, n))
+    work = _scratch(scratch, pages)
+    _at(pages, rows._dev)
+    _check(_lib.vla_verify_drafts(ctypes.byref(pages), ctypes.byref(rows), ctypes.byref(d),
+                                  _ints(_some(kept, "kept"), "kept", pages, n),
+                                  _ints(_some(n_kept, "n_kept"), "n_kept", pages, m),
+                                  _ints(_some(next, "next"), "next", pages, m), *work, stream or None))
+
+
 def vla_pages_evict_scratch(pages: vla_pages, n: int) -> int:
     b = ctypes.c_int64()
     _at(pages)
@@ -852,6 +905,7 @@ def exported_symbols() -> Iterable[str]:
             "vla_debug_gemm", "vla_debug_gemm_epi", "vla_debug_gemm_fold", "vla_debug_gemm_ln", "vla_gemm_noalloc", "vla_debug_attention", "vla_debug_attention_cache", "vla_debug_norm", "vla_debug_generate",
             "vla_debug_gemm_plan", "vla_pages_init", "vla_pages_reserve", "vla_qk_norm_rope", "vla_tree_attention",
             "vla_tree_attention_scratch", "vla_score_attention", "vla_score_attention_scratch", "vla_attention_mass",
-            "vla_attention_mass_scratch", "vla_pages_evict", "vla_pages_evict_scratch", "vla_pages_fork", "vla_pages_commit", "vla_pages_release", "vla_ctx_to_pages",
+            "vla_attention_mass_scratch", "vla_pages_evict", "vla_pages_evict_scratch",
+            "vla_verify_drafts", "vla_verify_drafts_scratch", "vla_pages_fork", "vla_pages_commit", "vla_pages_release", "vla_ctx_to_pages",
             "vla_kernel_timer",
             "vla_kernel_timer_read", "vla_last_error"]

@@ -47,7 +47,7 @@ def build(verbose: bool = False) -> str:
     ]
     objs = [gen_o]
     for src in ("kernels.hip", "runtime.hip", "paged.hip", "tree.hip", "scores.hip", "mass.hip",
-                "evict.hip"):
+                "evict.hip", "verify.hip"):
         o = os.path.join(BUILD, src.replace(".hip", ".o"))
         jobs.append([HIPCC, *HIP_FLAGS, "-c", os.path.join(CSRC, src), "-o", o])
         objs.append(o)

@@ -109,6 +109,22 @@ size_t evict_scratch(const PagedCache& c, int n);
 bool evict_fits(const PagedCache& c, int n);  // (grids hold it)
 hipError_t launch_pages_evict(const EvictDesc& d, hipStream_t st);
 
+struct DraftsDesc {
+  PagedCache c;
+  PagedRows r;
+  int dtype = 0, vocab = 0;
+  const int32_t *tokens = nullptr, *parent = nullptr;
+  const void *probs = nullptr, *drafted = nullptr;  // [n_rows][vocab], rows ldp and ldq apart
+  long long ldp = 0, ldq = 0;
+  const float* uniform = nullptr;
+  int32_t *kept = nullptr, *n_kept = nullptr, *next = nullptr;
+  void* scratch = nullptr;
+  int32_t* best = nullptr;  // (in scratch) [n_rows]
+};
+size_t verify_scratch(const DraftsDesc& d);
+bool verify_fits(const DraftsDesc& d);
+hipError_t launch_verify(const DraftsDesc& d, hipStream_t st);
+
 // The prefix rows 0 .. rows - 1 of a context (K and V in the KV-cache layout,
 // nb 32-key blocks per KV head, layers lk / lv elements apart) to the slots
 // behind sequence seq's committed ones, in every layer.

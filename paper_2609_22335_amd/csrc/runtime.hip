@@ -3602,6 +3602,71 @@ int vla_attention_mass(const vla_pages* p, int32_t layer, const vla_rows* rows, 
   })
 }
 
+static int drafts_size(const vla_pages* p, const vla_rows* rows, int32_t vocab, DraftsDesc* d) {
+  VLA_TRY(paged_cache(p, &d->c));
+  VLA_TRY(paged_rows(rows, &d->r));
+  if (vocab <= 0 || vocab > (1 << 28)) return fail(VLA_EINVAL, "vocab must be in 1 .. 2^28");
+  d->vocab = vocab;
+  if (!verify_fits(*d)) return paged_launch("verify drafts", GRID_FULL);
+  return VLA_OK;
+}
+
+int vla_verify_drafts_scratch(const vla_pages* p, const vla_rows* rows, int32_t vocab, int64_t* bytes) {
+  ABI_GUARD({
+    if (!bytes) return fail(VLA_EINVAL, "bytes is NULL");
+    DraftsDesc d;
+    VLA_TRY(drafts_size(p, rows, vocab, &d));
+    *bytes = (int64_t)verify_scratch(d);
+    return VLA_OK;
+  })
+}
+
+int vla_verify_drafts(const vla_pages* p, const vla_rows* rows, const vla_drafts* x, int32_t* kept, int32_t* n_kept,
+                      int32_t* next, void* scratch, int64_t scratch_bytes, void* stream) {
+  ABI_GUARD({
+    DraftsDesc d;
+    if (!x) return fail(VLA_EINVAL, "drafts is NULL");
+    VLA_TRY(drafts_size(p, rows, x->vocab, &d));
+    if (x->dtype != VLA_F32 && x->dtype != VLA_BF16) return fail(VLA_EINVAL, "drafts: dtype");
+    if (x->drafted && !x->uniform) return fail(VLA_EINVAL, "drafts: drafted needs uniform");
+    if (d.r.n_rows == 0 || d.r.n_ent == 0) return VLA_OK;  // nothing is read or written
+    if (!x->tokens || !x->probs || !kept || !n_kept || !next) return fail(VLA_EINVAL, "NULL argument");
+    const int64_t esz = x->dtype == VLA_BF16 ? 2 : 4, n = d.r.n_rows;
+    if (x->ld_probs < x->vocab || x->ld_probs > ((int64_t)1 << 31) || (uintptr_t)x->probs % esz)
+      return fail(VLA_EINVAL, "drafts: probs' row stride or alignment");
+    if (x->drafted && (x->ld_drafted < x->vocab || x->ld_drafted > ((int64_t)1 << 31) || (uintptr_t)x->drafted % esz))
+      return fail(VLA_EINVAL, "drafts: drafted's row stride or alignment");
+    const size_t need = verify_scratch(d);
+    if (!scratch || !aligned16(scratch) || scratch_bytes < 0 || (size_t)scratch_bytes < need)
+      return fail(VLA_EINVAL, "scratch: needs " + std::to_string(need) + " bytes, 16-byte aligned");
+    const ByteRows out[4] = {{kept, 0, n * 4, 1}, {n_kept, 0, (int64_t)d.r.n_ent * 4, 1},
+                             {next, 0, (int64_t)d.r.n_ent * 4, 1}, {scratch, 0, (int64_t)need, 1}};
+    const ByteRows in[5] = {{x->tokens, 0, n * 4, 1}, {x->parent, 0, x->parent ? n * 4 : 0, x->parent ? 1 : 0},
+                            {x->uniform, 0, n * 4, x->uniform ? 1 : 0},
+                            {x->probs, x->ld_probs * esz, x->vocab * esz, n},
+                            {x->drafted, x->ld_drafted * esz, x->vocab * esz, x->drafted ? n : 0}};
+    for (int i = 0; i < 4; ++i) {
+      for (const ByteRows& b : in)
+        if (meet(out[i], b)) return fail(VLA_EINVAL, "kept, n_kept, next or scratch overlaps what the call reads");
+      for (int j = 0; j < i; ++j)
+        if (meet(out[i], out[j])) return fail(VLA_EINVAL, "kept, n_kept, next and scratch must not overlap");
+    }
+    d.dtype = x->dtype == VLA_BF16 ? DT_BF16 : DT_F32;
+    d.tokens = x->tokens;
+    d.parent = x->parent;
+    d.probs = x->probs;
+    d.ldp = x->ld_probs;
+    d.drafted = x->drafted;
+    d.ldq = x->ld_drafted;
+    d.uniform = x->uniform;
+    d.kept = kept;
+    d.n_kept = n_kept;
+    d.next = next;
+    d.scratch = scratch;
+    return paged_launch("verify drafts", launch_verify(d, (hipStream_t)stream));
+  })
+}
+
 static int evict_size(const vla_pages* p, int32_t n, PagedCache* c) {
   VLA_TRY(paged_cache(p, c));
   if (n < 0) return fail(VLA_EINVAL, "n must not be negative");

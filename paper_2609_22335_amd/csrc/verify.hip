@@ -1,0 +1,341 @@
+// Verification of drafted tokens against a target's probabilities. An entry's
+// walk is one workgroup's: which child of a node is kept hangs on one number of
+// the target (and one of the draft's) each, and only where a child is refused,
+// or the walk ends, does a row of probabilities have to be read whole.
+#include <algorithm>
+
+#include "paged_dev.h"
+
+namespace vla {
+using namespace pg;
+
+namespace {
+
+constexpr int VT = 1024, VW = VT / 64;  // threads and waves of a walk
+constexpr int ROWS = 512;               // drafts whose numbers are fetched at a time
+constexpr int GONE = 64;                // refused tokens of a node that the LDS holds
+
+template <typename T>
+__device__ __forceinline__ float value(const T* p) {
+  if constexpr (sizeof(T) == 2) return __uint_as_float((uint32_t)*p << 16);
+  else return *p;
+}
+
+// A row's elements t0 .. t0 + VEC - 1, t0 from -VEC + 1 on: one load where all
+// of them are the row's and aligned; others are 0.
+template <typename T>
+__device__ __forceinline__ void load_some(const T* row, int t0, int V, bool aligned, float (&x)[El<T>::VEC]) {
+  constexpr int N = El<T>::VEC;
+  if (aligned && t0 >= 0 && t0 + N <= V) {
+    unpack(*(const u32x4*)(row + t0), x);
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = t0 + i >= 0 && t0 + i < V ? value(row + t0 + i) : 0.f;
+  }
+}
+
+// What is left of a node's target: max(p - sub q, 0) (drafts drawn from q), or
+// p without the tokens that were refused (drafts chosen without chance).
+template <typename T>
+struct Left {
+  const T *p, *q;  // q null: `gone` counts
+  int V;
+  double sub;
+  const int *gone, *more;  // the first GONE refused tokens, and all others
+  int n_gone;
+  bool pa, qa;  // 16-byte loads at t0 + skew
+  int skew;     // elements by which p's rows are behind 16 bytes
+
+  __device__ __forceinline__ void set(const T* p_, const T* q_, int V_) {
+    constexpr int N = El<T>::VEC;
+    p = p_, q = q_, V = V_;
+    sub = 0, n_gone = 0;
+    skew = (int)(((uintptr_t)p / sizeof(T)) % N);
+    pa = true;
+    qa = q && ((uintptr_t)q / sizeof(T)) % N == (unsigned)skew;
+  }
+  __device__ __forceinline__ int refused(int j) const { return j < GONE ? gone[j] : more[j]; }
+  // groups of VEC elements; group k has elements VEC k - skew on
+  __device__ __forceinline__ int groups() const { return (V + skew + El<T>::VEC - 1) / El<T>::VEC; }
+  __device__ __forceinline__ void get(int k, double (&r)[El<T>::VEC]) const {
+    constexpr int N = El<T>::VEC;
+    const int t0 = k * N - skew;
+    float x[N];
+    load_some(p, t0, V, pa, x);
+    if (q) {
+      float y[N];
+      load_some(q, t0, V, qa, y);
+#pragma unroll
+      for (int i = 0; i < N; ++i) r[i] = fmax((double)x[i] - sub * (double)y[i], 0.0);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) r[i] = fmax((double)x[i], 0.0);
+      for (int j = 0; j < n_gone; ++j) {
+        const int at = refused(j) - t0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) r[i] = at == i ? 0.0 : r[i];
+      }
+    }
+  }
+};
+
+__device__ __forceinline__ double wave_sum(double x) {
+#pragma unroll
+  for (int d = 32; d; d /= 2) x += __shfl_xor(x, d);
+  return x;
+}
+
+// Sums of the groups [k0, k1), a wave to each of VW equal parts: into part[],
+// and their sum (the same in every thread).
+template <typename T>
+__device__ __forceinline__ double sum_parts(const Left<T>& l, int k0, int k1, double* part) {
+  constexpr int N = El<T>::VEC;
+  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+  const int per = ((k1 - k0 + VW - 1) / VW + 63) & ~63, a = k0 + wv * per, b = min(a + per, k1);
+  double s = 0;
+#pragma unroll 4
+  for (int k = a + lane; k < b; k += 64) {
+    double r[N];
+    l.get(k, r);
+#pragma unroll
+    for (int i = 0; i < N; ++i) s += r[i];
+  }
+  s = wave_sum(s);
+  __syncthreads();  // the last sums are read
+  if (lane == 0) part[wv] = s;
+  __syncthreads();
+  double all = 0;
+#pragma unroll
+  for (int i = 0; i < VW; ++i) all += part[i];
+  return all;
+}
+
+// The first token whose running sum passes u times the total: the part that
+// holds it, a sixteenth of that, and there element by element. -1 where the
+// total is 0 or not finite.
+template <typename T>
+__device__ __forceinline__ int draw(const Left<T>& l, double u, double* part, int* out) {
+  constexpr int N = El<T>::VEC;
+  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+  int k0 = 0, k1 = l.groups();
+  double total = sum_parts(l, k0, k1, part);
+  if (!(total > 0) || !(total < INFINITY)) return -1;
+  const double want = u * total;
+  double before = 0;
+  while (true) {
+    const int per = ((k1 - k0 + VW - 1) / VW + 63) & ~63;
+    // (the last part with anything in it, should roundings leave none)
+    int pick = 0;
+    double base = before, run = before;
+    for (int i = 0; i < VW; ++i) {
+      const double x = part[i];
+      if (x > 0) {
+        pick = i, base = run;
+        run += x;
+        if (run > want) break;
+      }
+    }
+    k0 += pick * per;
+    k1 = min(k0 + per, k1);
+    before = base;
+    if (per <= 64) break;
+    sum_parts(l, k0, k1, part);
+  }
+  // at most 64 groups: one wave
+  if (wv == 0) {
+    double r[N], s = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) r[i] = 0;
+    if (k0 + lane < k1) l.get(k0 + lane, r);
+#pragma unroll
+    for (int i = 0; i < N; ++i) s += r[i];
+    double run = s;  // inclusive over the lanes
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const double y = __shfl_up(run, d);
+      if (lane >= d) run += y;
+    }
+    run = before + (run - s);
+    int hit = 0x7FFFFFFF, last = -1;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      run += r[i];
+      const int t = (k0 + lane) * N - l.skew + i;
+      if (r[i] > 0) {
+        last = t;
+        if (run > want && hit == 0x7FFFFFFF) hit = t;
+      }
+    }
+#pragma unroll
+    for (int d = 32; d; d /= 2) hit = min(hit, __shfl_xor(hit, d)), last = max(last, __shfl_xor(last, d));
+    if (lane == 0) *out = hit == 0x7FFFFFFF ? last : hit;
+  }
+  __syncthreads();
+  return *out;
+}
+
+// The likeliest token of every row (the lowest, where several are); -1: none.
+template <typename T>
+__global__ __launch_bounds__(256) void k_likeliest(DraftsDesc d) {
+  constexpr int N = El<T>::VEC;
+  __shared__ float sV[4];
+  __shared__ int sI[4];
+  const int row = blockIdx.x, lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+  const T* p = (const T*)d.probs + (size_t)row * d.ldp;
+  const int skew = (int)(((uintptr_t)p / sizeof(T)) % N), groups = (d.vocab + skew + N - 1) / N;
+  float best = -INFINITY;
+  int at = 0x7FFFFFFF;
+#pragma unroll 4
+  for (int k = threadIdx.x; k < groups; k += 256) {
+    float x[N];
+    const int t0 = k * N - skew;
+    load_some(p, t0, d.vocab, true, x);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (x[i] > best && t0 + i >= 0 && t0 + i < d.vocab) best = x[i], at = t0 + i;
+  }
+  auto join = [&](float v, int i) {
+    if (v > best || (v == best && i < at)) best = v, at = i;
+  };
+#pragma unroll
+  for (int s = 32; s; s /= 2) {
+    const float v = __shfl_xor(best, s);
+    const int i = __shfl_xor(at, s);
+    join(v, i);
+  }
+  if (lane == 0) sV[wv] = best, sI[wv] = at;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int w = 1; w < 4; ++w) join(sV[w], sI[w]);
+    d.best[row] = at == 0x7FFFFFFF ? -1 : at;
+  }
+}
+
+// The walk. Drafts come by in their order; one whose parent is the node that
+// the walk is at is tried, and taken or refused. (A node's children stand
+// behind it, so none is passed by.)
+template <typename T>
+__global__ __launch_bounds__(VT) void k_verify(DraftsDesc d) {
+  __shared__ int sPar[ROWS], sTok[ROWS];
+  __shared__ float sU[ROWS], sP[ROWS], sQ[ROWS];
+  __shared__ double sPart[VW];
+  __shared__ int sGone[GONE], sOut;
+  const int e = blockIdx.x, tid = threadIdx.x;
+  const Entry x = entry_of(d.c, d.r, e);
+  if (x.seq < 0) return;
+  if (x.n == 0) {
+    if (tid == 0) d.n_kept[e] = 0, d.next[e] = -1;
+    return;
+  }
+  const T *P = (const T*)d.probs + (size_t)x.row0 * d.ldp, *Q = (const T*)d.drafted;
+  if (Q) Q += (size_t)x.row0 * d.ldq;
+  const bool greedy = !d.uniform;
+  int32_t* kept = d.kept + x.row0;
+  Left<T> left;
+  int node = 0, count = 1;
+  double z = 1;  // what is left of the node's target
+  bool odd = false;
+  int32_t* gone = d.best + x.row0;  // (not used for likeliest tokens then)
+  left.gone = sGone, left.more = gone;
+  left.set(P, Q, d.vocab);
+  if (tid == 0) kept[0] = 0;
+  for (int c0 = 1; c0 < x.n; c0 += ROWS) {
+    const int m = min(ROWS, x.n - c0);
+    __syncthreads();
+    for (int k = tid; k < m; k += VT) {
+      const int i = c0 + k, row = x.row0 + i;
+      int par = d.parent ? d.parent[row] : i - 1;
+      const int tok = d.tokens[row];
+      if (par < 0 || par >= i) par = -1;
+      const bool in = par >= 0 && tok >= 0 && tok < d.vocab;
+      odd = odd || !in;
+      sPar[k] = par;
+      sTok[k] = in ? tok : -1;
+      if (greedy) {
+        sP[k] = in && d.best[x.row0 + par] == tok ? 1.f : 0.f;
+      } else {
+        sU[k] = d.uniform[row];
+        sP[k] = in ? value(P + (size_t)par * d.ldp + tok) : 0.f;
+        sQ[k] = in && Q ? value(Q + (size_t)par * d.ldq + tok) : 0.f;
+      }
+      kept[i] = -1;
+    }
+    __syncthreads();
+    for (int k = 0; k < m; ++k) {
+      if (sPar[k] != node || sTok[k] < 0) continue;
+      bool yes;
+      double mine = 0;
+      if (greedy) {
+        yes = sP[k] > 0.f;
+      } else if (Q) {
+        mine = fmax((double)sP[k] - left.sub * (double)sQ[k], 0.0);
+        yes = (double)sU[k] * (double)sQ[k] * z < mine;
+      } else {
+        mine = fmax((double)sP[k], 0.0);
+        for (int j = 0; j < left.n_gone; ++j) mine = left.refused(j) == sTok[k] ? 0.0 : mine;
+        yes = (double)sU[k] * z < mine;
+      }
+      if (yes) {
+        node = c0 + k;
+        left.set(P + (size_t)node * d.ldp, Q ? Q + (size_t)node * d.ldq : nullptr, d.vocab);
+        z = 1;
+        if (tid == 0) kept[count] = node;
+        ++count;
+      } else if (!greedy) {
+        if (Q) {
+          left.sub += z;
+          z = sum_parts(left, 0, left.groups(), sPart);
+        } else if (mine > 0) {
+          z -= mine;
+          __syncthreads();
+          if (tid == 0) {
+            if (left.n_gone < GONE) sGone[left.n_gone] = sTok[k];
+            else gone[left.n_gone] = sTok[k];
+          }
+          __syncthreads();
+          ++left.n_gone;
+        }
+      }
+    }
+  }
+  int token;
+  if (greedy) {
+    token = d.best[x.row0 + node];
+  } else {
+    const double u = d.uniform[x.row0];
+    token = draw(left, u, sPart, &sOut);
+    if (token < 0 && (left.sub > 0 || left.n_gone)) {  // nothing is left: all of the target
+      left.sub = 0, left.n_gone = 0, left.q = nullptr;
+      __syncthreads();
+      token = draw(left, u, sPart, &sOut);
+    }
+  }
+  odd = odd || token < 0;
+  if (odd) flag(d.c, PG_BAD);
+  if (tid == 0) d.n_kept[e] = count, d.next[e] = token;
+}
+
+template <typename T>
+hipError_t verify(const DraftsDesc& d, hipStream_t st) {
+  if (!d.uniform) {
+    hipLaunchKernelGGL(k_likeliest<T>, dim3(d.r.n_rows), dim3(256), 0, st, d);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL(k_verify<T>, dim3(d.r.n_ent), dim3(VT), 0, st, d);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t verify_scratch(const DraftsDesc& d) { return ((size_t)d.r.n_rows * 4 + 15) & ~(size_t)15; }
+bool verify_fits(const DraftsDesc& d) { return launchable(d.r.n_rows, 256) && launchable(d.r.n_ent, VT); }
+
+hipError_t launch_verify(const DraftsDesc& x, hipStream_t st) {
+  if (x.r.n_ent <= 0 || x.r.n_rows <= 0) return hipSuccess;
+  DraftsDesc d = x;
+  d.best = (int32_t*)d.scratch;
+  return d.dtype == DT_BF16 ? verify<uint16_t>(d, st) : verify<float>(d, st);
+}
+
+}  // namespace vla
