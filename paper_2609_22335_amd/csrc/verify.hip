@@ -43,28 +43,26 @@ struct Left {
   double sub;
   const int *gone, *more;  // the first GONE refused tokens, and all others
   int n_gone;
-  bool pa, qa;  // 16-byte loads at t0 + skew
-  int skew;     // elements by which p's rows are behind 16 bytes
+  bool qa;   // q's row lies as p's does, so that both are loaded in groups
+  int skew;  // elements by which p's row is behind 16 bytes
 
   __device__ __forceinline__ void set(const T* p_, const T* q_, int V_) {
     constexpr int N = El<T>::VEC;
     p = p_, q = q_, V = V_;
     sub = 0, n_gone = 0;
     skew = (int)(((uintptr_t)p / sizeof(T)) % N);
-    pa = true;
     qa = q && ((uintptr_t)q / sizeof(T)) % N == (unsigned)skew;
   }
   __device__ __forceinline__ int refused(int j) const { return j < GONE ? gone[j] : more[j]; }
   // groups of VEC elements; group k has elements VEC k - skew on
   __device__ __forceinline__ int groups() const { return (V + skew + El<T>::VEC - 1) / El<T>::VEC; }
-  __device__ __forceinline__ void get(int k, double (&r)[El<T>::VEC]) const {
+  // groups first .. last - 1 can be loaded whole
+  __device__ __forceinline__ int first() const { return skew > 0; }
+  __device__ __forceinline__ int last() const { return !q || qa ? (V + skew) / El<T>::VEC : 0; }
+  __device__ __forceinline__ void rest(int t0, const float (&x)[El<T>::VEC], const float (&y)[El<T>::VEC],
+                                       double (&r)[El<T>::VEC]) const {
     constexpr int N = El<T>::VEC;
-    const int t0 = k * N - skew;
-    float x[N];
-    load_some(p, t0, V, pa, x);
     if (q) {
-      float y[N];
-      load_some(q, t0, V, qa, y);
 #pragma unroll
       for (int i = 0; i < N; ++i) r[i] = fmax((double)x[i] - sub * (double)y[i], 0.0);
     } else {
@@ -72,10 +70,78 @@ struct Left {
       for (int i = 0; i < N; ++i) r[i] = fmax((double)x[i], 0.0);
       for (int j = 0; j < n_gone; ++j) {
         const int at = refused(j) - t0;
+        if ((unsigned)at < (unsigned)N) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) r[i] = at == i ? 0.0 : r[i];
+          for (int i = 0; i < N; ++i) r[i] = at == i ? 0.0 : r[i];
+        }
       }
     }
+  }
+  __device__ __forceinline__ void get(int k, double (&r)[El<T>::VEC]) const {
+    constexpr int N = El<T>::VEC;
+    const int t0 = k * N - skew;
+    float x[N], y[N];
+    load_some(p, t0, V, true, x);
+    if (q) load_some(q, t0, V, qa, y);
+    rest(t0, x, y, r);
+  }
+  // the sum of the groups that this lane has of k0 .. k1 - 1
+  __device__ __forceinline__ double sum(int k0, int k1) const {
+    constexpr int N = El<T>::VEC, U = sizeof(T) == 4 ? 3 : 2;
+    const int lane = threadIdx.x & 63, a = max(k0, first()), b = min(k1, last());
+    double s[2] = {0, 0};
+    auto add = [&](const double (&r)[N]) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) s[i & 1] += r[i];
+    };
+    int k = k0;
+    if (a < b) {
+      if (k0 + lane < a) {
+        double r[N];
+        get(k0 + lane, r);
+        add(r);
+      }
+      k = a;
+      // (the next loads are out while these are added up)
+      u32x4 u[2][U], w[2][U];
+      auto fetch = [&](int at, int e) {
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+          const int t0 = (at + 64 * i + lane) * N - skew;
+          u[e][i] = *(const u32x4*)(p + t0);
+          if (q) w[e][i] = *(const u32x4*)(q + t0);
+        }
+      };
+      auto work = [&](int at, int e) {
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+          float x[N], y[N];
+          double r[N];
+          unpack(u[e][i], x);
+          if (q) unpack(w[e][i], y);
+          rest((at + 64 * i + lane) * N - skew, x, y, r);
+          add(r);
+        }
+      };
+      if (k + 64 * U <= b) fetch(k, 0);
+      while (k + 64 * U <= b) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const bool more = k + 128 * U <= b;
+          if (more) fetch(k + 64 * U, e ^ 1);
+          __builtin_amdgcn_sched_barrier(0);
+          work(k, e);
+          k += 64 * U;
+          if (!more) break;
+        }
+      }
+    }
+    for (k += lane; k < k1; k += 64) {
+      double r[N];
+      get(k, r);
+      add(r);
+    }
+    return s[0] + s[1];
   }
 };
 
@@ -89,18 +155,9 @@ __device__ __forceinline__ double wave_sum(double x) {
 // and their sum (the same in every thread).
 template <typename T>
 __device__ __forceinline__ double sum_parts(const Left<T>& l, int k0, int k1, double* part) {
-  constexpr int N = El<T>::VEC;
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
   const int per = ((k1 - k0 + VW - 1) / VW + 63) & ~63, a = k0 + wv * per, b = min(a + per, k1);
-  double s = 0;
-#pragma unroll 4
-  for (int k = a + lane; k < b; k += 64) {
-    double r[N];
-    l.get(k, r);
-#pragma unroll
-    for (int i = 0; i < N; ++i) s += r[i];
-  }
-  s = wave_sum(s);
+  const double s = wave_sum(a < b ? l.sum(a, b) : 0.0);
   __syncthreads();  // the last sums are read
   if (lane == 0) part[wv] = s;
   __syncthreads();
@@ -110,15 +167,14 @@ __device__ __forceinline__ double sum_parts(const Left<T>& l, int k0, int k1, do
   return all;
 }
 
-// The first token whose running sum passes u times the total: the part that
-// holds it, a sixteenth of that, and there element by element. -1 where the
-// total is 0 or not finite.
+// The first token whose running sum passes u times the total (whose parts are in
+// part[] already): the part that holds it, a sixteenth of that, and there
+// element by element. -1 where the total is 0 or not finite.
 template <typename T>
-__device__ __forceinline__ int draw(const Left<T>& l, double u, double* part, int* out) {
+__device__ __forceinline__ int draw(const Left<T>& l, double u, double total, double* part, int* out) {
   constexpr int N = El<T>::VEC;
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
   int k0 = 0, k1 = l.groups();
-  double total = sum_parts(l, k0, k1, part);
   if (!(total > 0) || !(total < INFINITY)) return -1;
   const double want = u * total;
   double before = 0;
@@ -303,11 +359,13 @@ __global__ __launch_bounds__(VT) void k_verify(DraftsDesc d) {
     token = d.best[x.row0 + node];
   } else {
     const double u = d.uniform[x.row0];
-    token = draw(left, u, sPart, &sOut);
+    // (in a node whose drafts were refused, the last of those sums)
+    const double total = Q && left.sub > 0 ? z : sum_parts(left, 0, left.groups(), sPart);
+    token = draw(left, u, total, sPart, &sOut);
     if (token < 0 && (left.sub > 0 || left.n_gone)) {  // nothing is left: all of the target
       left.sub = 0, left.n_gone = 0, left.q = nullptr;
       __syncthreads();
-      token = draw(left, u, sPart, &sOut);
+      token = draw(left, u, sum_parts(left, 0, left.groups(), sPart), sPart, &sOut);
     }
   }
   odd = odd || token < 0;
