@@ -677,10 +677,10 @@ __device__ __forceinline__ void soften(f32x16 (&s)[NS], float c2, float& mx, flo
     }
 }
 
-__device__ __forceinline__ void hide(f32x16& s, uint32_t see) {
+__device__ __forceinline__ void hide(f32x16& s, uint32_t see, float none = -INFINITY) {
   const uint32_t half = see >> (4 * ((threadIdx.x >> 5) & 1));
 #pragma unroll
-  for (int j = 0; j < 16; ++j) s[j] = (half >> (8 * (j / 4) + j % 4)) & 1u ? s[j] : -INFINITY;
+  for (int j = 0; j < 16; ++j) s[j] = (half >> (8 * (j / 4) + j % 4)) & 1u ? s[j] : none;
 }
 
 // The lane's query (row m of the tile's rows, clamped to the last).
@@ -949,7 +949,11 @@ __device__ __forceinline__ void finish(const Tile& t, int slot, int wv, int m, f
 // 32 heads on 8, 277 us against 293 at head dim 64 and 387 against 390 (0.85
 // PFLOP/s, two sequences) at 128; 8 on 1 at head dim 256, one workgroup on a
 // CU, 381 against 435.
-template <int HDP, bool SH>
+// With CURVED (scores capped and not biased) the scores are kept as
+// r = 1 / (e^{2 y} + 1), which is worked out beside the products of V: cap tanh y
+// = cap (1 - 2 r), one product and sum before the exponential as for plain
+// scores, and the largest score is the smallest r.
+template <int HDP, bool SH, bool CURVED>
 __global__ __launch_bounds__(256, (many_waves<uint16_t, HDP>())) void k_tree_many(Args a) {
   typedef uint16_t T;
   constexpr int BM = 128, BN = 32, RB = HDP * 2, NQ = RB / 32, NDT = HDP / 32;
@@ -1045,12 +1049,14 @@ __global__ __launch_bounds__(256, (many_waves<uint16_t, HDP>())) void k_tree_man
       const uint32_t see = seen_bits<SH>(t, kb, me);
       return hole ? see & ld.paged(kb) : see;
     };
+    auto top = [&](float x, float y) { return CURVED ? fminf(x, y) : fmaxf(x, y); };
     auto cover = [&](f32x16& x, uint32_t see) {  // scores that their rows do not see
-      hide(x, see);
+      hide(x, see, CURVED ? INFINITY : -INFINITY);
       bm = x[0];
 #pragma unroll
-      for (int j = 1; j < 16; ++j) bm = fmaxf(bm, x[j]);
+      for (int j = 1; j < 16; ++j) bm = top(bm, x[j]);
     };
+    auto bend = [&](float x) { return __builtin_amdgcn_rcpf(ex2(x * a.k1) + 1.f); };
     // (as soften())
     auto raise = [&] {
       bm = max_x32(bm) * (SH ? 1.f : a.c2);
@@ -1070,7 +1076,8 @@ __global__ __launch_bounds__(256, (many_waves<uint16_t, HDP>())) void k_tree_man
     auto soft = [&](f32x16& cur, int j0, int j1) {
 #pragma unroll
       for (int j = j0; j < j1; ++j) {
-        cur[j] = SH ? ex2(cur[j] - ref) : ex2(__builtin_fmaf(cur[j], a.c2, -ref));
+        cur[j] = ex2(CURVED ? __builtin_fmaf(cur[j], -2.f * a.cap2, a.cap2 - ref)
+                            : SH ? cur[j] - ref : __builtin_fmaf(cur[j], a.c2, -ref));
         l += cur[j];
         if (j & 1) p[j >> 3][(j >> 1) & 3] = bf2(cur[j - 1], cur[j]);
         asm volatile("" : "+v"(l));  // (here, not behind the step's branches)
@@ -1110,6 +1117,10 @@ __global__ __launch_bounds__(256, (many_waves<uint16_t, HDP>())) void k_tree_man
         soft(cur, JQ + dt * (16 - JQ) / NDT, JQ + (dt + 1) * (16 - JQ) / NDT);
         if (dt == 0) ld.issue(a.k, stage(P), pk, wv);
         if (dt == 1) ld.issue(a.v, stage(P) + 32 * RB, pv, wv);
+        if constexpr (CURVED) {
+#pragma unroll
+          for (int j = 8 * dt / NDT; j < 8 * (dt + 1) / NDT; ++j) nxt[j] = bend(nxt[j]);
+        }
         fence();
       }
 #pragma unroll
@@ -1118,17 +1129,21 @@ __global__ __launch_bounds__(256, (many_waves<uint16_t, HDP>())) void k_tree_man
 #pragma unroll
         for (int i = 4 * dt / NDT; i < 4 * (dt + 1) / NDT; ++i) read_k(sn, i);
 #pragma unroll
-        for (int j = 16 * dt / NDT; j < 16 * (dt + 1) / NDT && !SH; ++j) bm = j ? fmaxf(bm, nxt[j]) : nxt[0];
+        for (int j = 16 * dt / NDT; j < 16 * (dt + 1) / NDT && (!SH || CURVED); ++j) {
+          if (CURVED && j >= 8) nxt[j] = bend(nxt[j]);
+          bm = j ? top(bm, nxt[j]) : nxt[0];
+        }
         asm volatile("" : "+v"(bm));
         fence();
       }
-      if constexpr (SH) {
+      if constexpr (SH && !CURVED) {
         shape<T>(nxt, a, t, (b + 1) * BN, me);
         bm = nxt[0];
 #pragma unroll
         for (int j = 1; j < 16; ++j) bm = fmaxf(bm, nxt[j]);
       }
       if (hidden) cover(nxt, see);
+      if constexpr (CURVED) bm = __builtin_fmaf(-2.f * a.cap2, bm, a.cap2);
       if (!PAIR && b + 1 < t.b1) raise();
     };
     // the first block's scores
@@ -1144,11 +1159,17 @@ __global__ __launch_bounds__(256, (many_waves<uint16_t, HDP>())) void k_tree_man
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) read_k((LB*)s1, i);
-    if constexpr (SH) shape<T>(s[0], a, t, t.b0 * BN, me);
+    if constexpr (CURVED) {
+#pragma unroll
+      for (int j = 0; j < 16; ++j) s[0][j] = bend(s[0][j]);
+    } else if constexpr (SH) {
+      shape<T>(s[0], a, t, t.b0 * BN, me);
+    }
     bm = s[0][0];
 #pragma unroll
-    for (int j = 1; j < 16; ++j) bm = fmaxf(bm, s[0][j]);
+    for (int j = 1; j < 16; ++j) bm = top(bm, s[0][j]);
     if (partly(t.b0) || hole) cover(s[0], seen(t.b0 * BN));
+    if constexpr (CURVED) bm = __builtin_fmaf(-2.f * a.cap2, bm, a.cap2);
     if (!PAIR) raise();
     for (int b = t.b0;; b += 4) {
       if (((b - t.b0) & 31) == 28) window(b + 4);
@@ -1473,7 +1494,10 @@ template <typename T, int HDP, bool SH>
 hipError_t run(const TreeAttnDesc& d, const Args& a, hipStream_t st) {
   const int rows = tile_rows(d);
   if (rows == 32) hipLaunchKernelGGL((k_tree_few<T, HDP, SH>), dim3(a.wgs), dim3(256), 0, st, a);
-  else if constexpr (sizeof(T) == 2) hipLaunchKernelGGL((k_tree_many<HDP, SH>), dim3(a.wgs), dim3(256), 0, st, a);
+  else if constexpr (sizeof(T) == 2) {
+    if (SH && a.cap2 > 0.f && !a.slopes) hipLaunchKernelGGL((k_tree_many<HDP, SH, SH>), dim3(a.wgs), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((k_tree_many<HDP, SH, false>), dim3(a.wgs), dim3(256), 0, st, a);
+  }
   else hipLaunchKernelGGL((k_tree_many32<HDP, SH>), dim3(a.wgs), dim3(256), 0, st, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
