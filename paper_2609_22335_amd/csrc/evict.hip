@@ -41,7 +41,7 @@ __device__ __forceinline__ Entry state_of(const PagedCache& c, int s) {
   return x;
 }
 
-// A slot's weight: the sum over layers and heads, in their order.
+// A slot's weight: the sum over layers and heads.
 __global__ __launch_bounds__(256) void k_evict_score(Ev e) {
   const PagedCache& c = e.d.c;
   const int i = blockIdx.y, slot = blockIdx.x * 256 + threadIdx.x;
@@ -49,10 +49,14 @@ __global__ __launch_bounds__(256) void k_evict_score(Ev e) {
   if (slot >= x.len || x.len <= e.d.keep[i]) return;
   const float* p = e.d.mass + (size_t)x.seq * c.nkv * e.slots + slot;
   const size_t layer = (size_t)c.n_seqs * c.nkv * e.slots;
+  // (the longer of the two is the inner loop, whose loads are out together)
+  const bool deep = c.layers > c.nkv;
+  const int n0 = deep ? c.nkv : c.layers, n1 = deep ? c.layers : c.nkv;
+  const size_t s0 = deep ? (size_t)e.slots : layer, s1 = deep ? layer : (size_t)e.slots;
   double sum = 0;
-  for (int l = 0; l < c.layers; ++l)
+  for (int i0 = 0; i0 < n0; ++i0)
 #pragma unroll 8
-    for (int h = 0; h < c.nkv; ++h) sum += p[l * layer + (size_t)h * e.slots];
+    for (int i1 = 0; i1 < n1; ++i1) sum += p[i0 * s0 + i1 * s1];
   e.score[(size_t)i * e.slots + slot] = sum;
 }
 
@@ -91,16 +95,30 @@ __global__ __launch_bounds__(PICK) void k_evict_pick(Ev e) {
     // (what is negative or not a number has the sign or lies above infinity)
     return v > 0x7FF0000000000000ull ? 0ull : v;
   };
+  // (of up to 4,096 slots the keys stay in registers)
+  constexpr int KEYS = 4;
+  u64 own[KEYS];
+#pragma unroll
+  for (int k = 0; k < KEYS; ++k) own[k] = per <= KEYS && j0 + k < j1 ? key(j0 + k) : 0;
+  auto each = [&](auto&& f) {
+    if (per <= KEYS) {
+#pragma unroll
+      for (int k = 0; k < KEYS; ++k)
+        if (j0 + k < j1) f(own[k], j0 + k);
+    } else {
+#pragma unroll 4
+      for (int j = j0; j < j1; ++j) f(key(j), j);
+    }
+  };
   int want = keep;  // of those whose upper bits are `prefix`
   u64 prefix = 0, mask = 0;
   if (keep > 0)
     for (int sh = 56; sh >= 0; sh -= 8) {
       if (tid < 256) sHist[tid] = 0;
       __syncthreads();
-      for (int j = j0; j < j1; ++j) {
-        const u64 k = key(j);
+      each([&](u64 k, int) {
         if ((k & mask) == prefix) atomicAdd(&sHist[(int)(k >> sh) & 255], 1);
-      }
+      });
       __syncthreads();
       if (tid < 64) {
         // bins from the top: lane l has 255 - 4 l and the three below
@@ -125,24 +143,23 @@ __global__ __launch_bounds__(PICK) void k_evict_pick(Ev e) {
   // ties go to the lower slots
   int over = 0, equal = 0;
   if (keep > 0)
-    for (int j = j0; j < j1; ++j) {
-      const u64 k = key(j) & mask;
-      over += k > prefix;
-      equal += k == prefix;
-    }
+    each([&](u64 k, int) {
+      over += (k & mask) > prefix;
+      equal += (k & mask) == prefix;
+    });
   if (tid == 0) sGap = x.len;
   int all;
   const int eq0 = block_scan<PICK>(equal, &all);
   const int mine = max(0, min(equal, want - eq0));
   int at = block_scan<PICK>(over + (keep > 0 ? mine : 0), &all), left = mine, gap = x.len;
   if (keep > 0)
-    for (int j = j0; j < j1; ++j) {
-      const u64 k = key(j) & mask;
+    each([&](u64 k, int j) {
+      k &= mask;
       const bool tie = k == prefix && left > 0;
       left -= tie;
       if (k > prefix || tie) kept[at++] = j;
       else gap = min(gap, j);
-    }
+    });
   else gap = 0;
   atomicMin(&sGap, gap);
   __syncthreads();
@@ -347,7 +364,7 @@ size_t evict_scratch(const PagedCache& c, int n) {
 }
 
 // Chunks of a row to a workgroup.
-static int part_of(const PagedCache& c, int n) { return width_of(c); }
+static int part_of(const PagedCache& c) { return width_of(c); }
 bool evict_fits(const PagedCache& c, int n) {
   const long long per = (long long)c.layers * c.nkv * (2 * (width_of(c) / 4) + 1);
   return launchable((long long)n * per, MOVE) && launchable((slots_of(c) + 255) / 256, 256) && n <= 65535;
@@ -363,7 +380,7 @@ hipError_t launch_pages_evict(const EvictDesc& d, hipStream_t st) {
   e.fresh = (int32_t*)p;
   p += up16((size_t)d.n * c.max_pages * 4);
   e.score = (double*)p;
-  const int width = width_of(c), part = part_of(c, d.n);
+  const int width = width_of(c), part = part_of(c);
   hipLaunchKernelGGL(k_evict_score, dim3((e.slots + 255) / 256, d.n), dim3(256), 0, st, e);
   hipLaunchKernelGGL(k_evict_pick, dim3(d.n), dim3(PICK), 0, st, e);
   hipLaunchKernelGGL(k_evict_pages, dim3(1), dim3(PICK), 0, st, e);

@@ -61,7 +61,7 @@ struct Row64 {
   // that a launch has `target`; a unit keeps CUT steps, which its start (keys,
   // first queries: two round trips) is worth.
   __device__ __forceinline__ int cuts(long long tiles, int target) const {
-    constexpr int CUT = 8;
+    constexpr int CUT = 2;
     if (tiles >= target) return 1;
     const int steps = (int)(((long long)most * a.group + QT - 1) / QT);
     return (int)min((target + tiles - 1) / tiles, (long long)((steps + CUT - 1) / CUT));

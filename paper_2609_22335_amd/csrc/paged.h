@@ -120,6 +120,7 @@ struct DraftsDesc {
   int32_t *kept = nullptr, *n_kept = nullptr, *next = nullptr;
   void* scratch = nullptr;
   int32_t* best = nullptr;  // (in scratch) [n_rows]
+  void* pre = nullptr;      // (in scratch) how far the walks have come, or null
 };
 size_t verify_scratch(const DraftsDesc& d);
 bool verify_fits(const DraftsDesc& d);

@@ -12,6 +12,7 @@ using namespace pg;
 namespace {
 
 constexpr int VT = 1024, VW = VT / 64;  // threads and waves of a walk
+constexpr int PARTS = 64, PT = 256;      // parts of a row that more workgroups than one go through, and their threads
 constexpr int ROWS = 512;               // drafts whose numbers are fetched at a time
 constexpr int GONE = 64;                // refused tokens of a node that the LDS holds
 
@@ -145,10 +146,36 @@ struct Left {
   }
 };
 
-__device__ __forceinline__ double wave_sum(double x) {
-#pragma unroll
-  for (int d = 32; d; d /= 2) x += __shfl_xor(x, d);
+// Groups of one of `parts` parts.
+__device__ __forceinline__ int part_of(int groups, int parts = VW) { return ((groups + parts - 1) / parts + 63) & ~63; }
+
+// Sums over the wave by shifts inside rows of 16 lanes and broadcasts of their
+// last ones, as wave_scan (an LDS round trip a step took 0.6 us each).
+template <int CTRL, int ROWS>
+__device__ __forceinline__ void sum_step(double& x) {
+  const long long v = __builtin_bit_cast(long long, x);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CTRL, ROWS, 0xf, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(v >> 32), CTRL, ROWS, 0xf, false);
+  x += __builtin_bit_cast(double, (long long)(((unsigned long long)hi << 32) | lo));
+}
+__device__ __forceinline__ double scan_sum(double x) {  // inclusive over the lanes
+  sum_step<0x111, 0xf>(x);
+  sum_step<0x112, 0xf>(x);
+  sum_step<0x114, 0xf>(x);
+  sum_step<0x118, 0xf>(x);
+  sum_step<0x142, 0xa>(x);
+  sum_step<0x143, 0xc>(x);
   return x;
+}
+__device__ __forceinline__ double wave_sum(double x) {
+  const long long v = __builtin_bit_cast(long long, scan_sum(x));
+  const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)v, 63), hi = __builtin_amdgcn_readlane((int)(v >> 32), 63);
+  return __builtin_bit_cast(double, (long long)(((unsigned long long)hi << 32) | lo));
+}
+// of n <= 64 values, a lane to each
+__device__ __forceinline__ double sum_of(const double* part, int n) {
+  const int lane = threadIdx.x & 63;
+  return wave_sum(lane < n ? part[lane] : 0.0);
 }
 
 // Sums of the groups [k0, k1), a wave to each of VW equal parts: into part[],
@@ -156,78 +183,69 @@ __device__ __forceinline__ double wave_sum(double x) {
 template <typename T>
 __device__ __forceinline__ double sum_parts(const Left<T>& l, int k0, int k1, double* part) {
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-  const int per = ((k1 - k0 + VW - 1) / VW + 63) & ~63, a = k0 + wv * per, b = min(a + per, k1);
+  const int per = part_of(k1 - k0), a = k0 + wv * per, b = min(a + per, k1);
   const double s = wave_sum(a < b ? l.sum(a, b) : 0.0);
   __syncthreads();  // the last sums are read
   if (lane == 0) part[wv] = s;
   __syncthreads();
-  double all = 0;
-#pragma unroll
-  for (int i = 0; i < VW; ++i) all += part[i];
-  return all;
+  return sum_of(part, VW);
 }
 
-// The first token whose running sum passes u times the total (whose parts are in
-// part[] already): the part that holds it, a sixteenth of that, and there
-// element by element. -1 where the total is 0 or not finite.
+// The first token whose running sum passes u times the total, whose `n` parts
+// (at most PARTS) are in part[]: the part that holds it, a sixteenth of that
+// while it has more groups than there are threads, and there element by element.
+// -1 where the total is 0 or not finite. (Should roundings leave none, the last
+// token with anything.)
 template <typename T>
-__device__ __forceinline__ int draw(const Left<T>& l, double u, double total, double* part, int* out) {
+__device__ __forceinline__ int draw(const Left<T>& l, double u, double total, int n, double* part, int* out) {
   constexpr int N = El<T>::VEC;
-  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-  int k0 = 0, k1 = l.groups();
+  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
   if (!(total > 0) || !(total < INFINITY)) return -1;
   const double want = u * total;
+  int k0 = 0, k1 = l.groups();
   double before = 0;
-  while (true) {
-    const int per = ((k1 - k0 + VW - 1) / VW + 63) & ~63;
-    // (the last part with anything in it, should roundings leave none)
-    int pick = 0;
-    double base = before, run = before;
-    for (int i = 0; i < VW; ++i) {
-      const double x = part[i];
-      if (x > 0) {
-        pick = i, base = run;
-        run += x;
-        if (run > want) break;
-      }
-    }
+  auto choose = [&](int parts) {
+    const int per = part_of(k1 - k0, parts);
+    const double x = lane < parts ? part[lane] : 0.0, run = before + scan_sum(x);
+    const unsigned long long some = __ballot(x > 0), past = __ballot(x > 0 && run > want);
+    const int pick = past ? __ffsll(past) - 1 : some ? 63 - __clzll(some) : 0;
+    const double below = __shfl(run - x, pick);
     k0 += pick * per;
     k1 = min(k0 + per, k1);
-    before = base;
-    if (per <= 64) break;
+    before = below;
+  };
+  if (k1 > VT) choose(n);
+  while (k1 - k0 > VT) {
     sum_parts(l, k0, k1, part);
+    choose(VW);
   }
-  // at most 64 groups: one wave
-  if (wv == 0) {
-    double r[N], s = 0;
+  // a group to a thread
+  double r[N], s = 0;
 #pragma unroll
-    for (int i = 0; i < N; ++i) r[i] = 0;
-    if (k0 + lane < k1) l.get(k0 + lane, r);
+  for (int i = 0; i < N; ++i) r[i] = 0;
+  if (k0 + tid < k1) l.get(k0 + tid, r);
 #pragma unroll
-    for (int i = 0; i < N; ++i) s += r[i];
-    double run = s;  // inclusive over the lanes
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const double y = __shfl_up(run, d);
-      if (lane >= d) run += y;
-    }
-    run = before + (run - s);
-    int hit = 0x7FFFFFFF, last = -1;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      run += r[i];
-      const int t = (k0 + lane) * N - l.skew + i;
-      if (r[i] > 0) {
-        last = t;
-        if (run > want && hit == 0x7FFFFFFF) hit = t;
-      }
-    }
-#pragma unroll
-    for (int d = 32; d; d /= 2) hit = min(hit, __shfl_xor(hit, d)), last = max(last, __shfl_xor(last, d));
-    if (lane == 0) *out = hit == 0x7FFFFFFF ? last : hit;
-  }
+  for (int i = 0; i < N; ++i) s += r[i];
+  double run = scan_sum(s);
   __syncthreads();
-  return *out;
+  if (lane == 63) part[wv] = run;
+  if (tid == 0) out[0] = 0x7FFFFFFF, out[1] = -1;
+  __syncthreads();
+  run = before + (sum_of(part, wv) + (run - s));
+  int hit = 0x7FFFFFFF, last = -1;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    run += r[i];
+    const int t = (k0 + tid) * N - l.skew + i;
+    if (r[i] > 0) {
+      last = t;
+      if (run > want && hit == 0x7FFFFFFF) hit = t;
+    }
+  }
+  if (hit != 0x7FFFFFFF) atomicMin(&out[0], hit);
+  if (last >= 0) atomicMax(&out[1], last);
+  __syncthreads();
+  return out[0] == 0x7FFFFFFF ? out[1] : out[0];
 }
 
 // The likeliest token of every row (the lowest, where several are); -1: none.
@@ -267,39 +285,83 @@ __global__ __launch_bounds__(256) void k_likeliest(DraftsDesc d) {
   }
 }
 
+// A walk up to the first sum over a row that it needs, by PARTS / 4 workgroups
+// an entry, and that sum in parts.
+struct Pre {
+  double sum[PARTS];
+  double sub;
+  int node, count;
+  int at;  // the draft to go on with (0: nothing of this counts)
+  int n_gone, gone[GONE];
+};
+
 // The walk. Drafts come by in their order; one whose parent is the node that
 // the walk is at is tried, and taken or refused. (A node's children stand
 // behind it, so none is passed by.)
-template <typename T>
-__global__ __launch_bounds__(VT) void k_verify(DraftsDesc d) {
+//
+// One CU reads 50 GB/s from the HBM, so where rows are long and entries few,
+// PARTS / 4 workgroups of four waves (PRE) walk an entry up to the first sum
+// over a row that it needs and work out a part of it with each wave; the walk
+// proper goes on from there. 64 chains over 131,072 tokens: 19 us (4 TB/s) and 8
+// in turn, against 33 without; over 50,001 tokens a CU's pass takes 3 us, no more
+// than the second launch.
+template <typename T, int NT, bool PRE>
+__global__ __launch_bounds__(NT) void k_verify(DraftsDesc d) {
   __shared__ int sPar[ROWS], sTok[ROWS];
   __shared__ float sU[ROWS], sP[ROWS], sQ[ROWS];
-  __shared__ double sPart[VW];
-  __shared__ int sGone[GONE], sOut;
-  const int e = blockIdx.x, tid = threadIdx.x;
-  const Entry x = entry_of(d.c, d.r, e);
-  if (x.seq < 0) return;
-  if (x.n == 0) {
-    if (tid == 0) d.n_kept[e] = 0, d.next[e] = -1;
+  __shared__ double sPart[PARTS];
+  __shared__ int sGone[GONE], sOut[2];
+  constexpr int WGS = PARTS / 4;
+  const int e = PRE ? blockIdx.x / WGS : blockIdx.x, part = PRE ? blockIdx.x % WGS : 0, tid = threadIdx.x;
+  // (as entry_of, without the sequence's state)
+  const int seq = d.r.seqs ? d.r.seqs[e] : e, first = d.r.start[e], end = d.r.start[e + 1];
+  if (seq < 0 || seq >= d.c.n_seqs) return;
+  const int row0 = min(max(first, 0), d.r.n_rows), n = max(min(end, d.r.n_rows) - row0, 0);
+  if (n == 0) {
+    if (!PRE && tid == 0) d.n_kept[e] = 0, d.next[e] = -1;
     return;
   }
-  const T *P = (const T*)d.probs + (size_t)x.row0 * d.ldp, *Q = (const T*)d.drafted;
-  if (Q) Q += (size_t)x.row0 * d.ldq;
+  const T *P = (const T*)d.probs + (size_t)row0 * d.ldp, *Q = (const T*)d.drafted;
+  if (Q) Q += (size_t)row0 * d.ldq;
   const bool greedy = !d.uniform;
-  int32_t* kept = d.kept + x.row0;
+  int32_t *kept = d.kept + row0, *gone = d.best + row0;  // (not used for likeliest tokens then)
+  Pre* pre = d.pre ? (Pre*)d.pre + e : nullptr;
   Left<T> left;
-  int node = 0, count = 1;
-  double z = 1;  // what is left of the node's target
-  bool odd = false;
-  int32_t* gone = d.best + x.row0;  // (not used for likeliest tokens then)
   left.gone = sGone, left.more = gone;
-  left.set(P, Q, d.vocab);
-  if (tid == 0) kept[0] = 0;
-  for (int c0 = 1; c0 < x.n; c0 += ROWS) {
-    const int m = min(ROWS, x.n - c0);
+  int node = 0, count = 1, at = 1, parts = VW;
+  double z = 1;         // what is left of the node's target
+  bool summed = false;  // z is the sum of what is left, its parts in sPart
+  bool odd = false;
+  if (!PRE && pre && pre->at > 0) {
+    node = pre->node, count = pre->count, at = pre->at;
+    left.set(P + (size_t)node * d.ldp, Q ? Q + (size_t)node * d.ldq : nullptr, d.vocab);
+    left.sub = pre->sub, left.n_gone = pre->n_gone;
+    if (tid < PARTS) sPart[tid] = pre->sum[tid];
+    if (tid < GONE) sGone[tid] = pre->gone[tid];
     __syncthreads();
-    for (int k = tid; k < m; k += VT) {
-      const int i = c0 + k, row = x.row0 + i;
+    parts = PARTS, summed = true;
+    z = sum_of(sPart, PARTS);
+    if (!d.parent && n <= ROWS) at = n;  // (a chain's node has one draft, and all have been looked at)
+  } else {
+    left.set(P, Q, d.vocab);
+    if (part == 0 && tid == 0) kept[0] = 0;
+  }
+  // PRE: this wave's part of what is left, and where the walk is
+  auto leave = [&](int next) {
+    const int wv = tid >> 6, mine = part * 4 + wv, groups = left.groups(), per = part_of(groups, PARTS);
+    const int a = min(mine * per, groups), b = min(a + per, groups);
+    const double s = wave_sum(a < b ? left.sum(a, b) : 0.0);
+    if ((tid & 63) == 0) pre->sum[mine] = s;
+    if (part == 0) {
+      if (tid < left.n_gone) pre->gone[tid] = sGone[tid];
+      if (tid == 0) pre->sub = left.sub, pre->node = node, pre->count = count, pre->at = next, pre->n_gone = left.n_gone;
+    }
+  };
+  for (int c0 = at; c0 < n; c0 += ROWS) {
+    const int m = min(ROWS, n - c0);
+    __syncthreads();
+    for (int k = tid; k < m; k += NT) {
+      const int i = c0 + k, row = row0 + i;
       int par = d.parent ? d.parent[row] : i - 1;
       const int tok = d.tokens[row];
       if (par < 0 || par >= i) par = -1;
@@ -308,13 +370,13 @@ __global__ __launch_bounds__(VT) void k_verify(DraftsDesc d) {
       sPar[k] = par;
       sTok[k] = in ? tok : -1;
       if (greedy) {
-        sP[k] = in && d.best[x.row0 + par] == tok ? 1.f : 0.f;
+        sP[k] = in && d.best[row0 + par] == tok ? 1.f : 0.f;
       } else {
         sU[k] = d.uniform[row];
         sP[k] = in ? value(P + (size_t)par * d.ldp + tok) : 0.f;
         sQ[k] = in && Q ? value(Q + (size_t)par * d.ldq + tok) : 0.f;
       }
-      kept[i] = -1;
+      if (part == 0 && (PRE || !pre || at == 1)) kept[i] = -1;
     }
     __syncthreads();
     for (int k = 0; k < m; ++k) {
@@ -334,15 +396,29 @@ __global__ __launch_bounds__(VT) void k_verify(DraftsDesc d) {
       if (yes) {
         node = c0 + k;
         left.set(P + (size_t)node * d.ldp, Q ? Q + (size_t)node * d.ldq : nullptr, d.vocab);
-        z = 1;
-        if (tid == 0) kept[count] = node;
+        z = 1, summed = false;
+        if (part == 0 && tid == 0) kept[count] = node;
         ++count;
       } else if (!greedy) {
         if (Q) {
           left.sub += z;
+          if constexpr (PRE) {
+            if (odd) flag(d.c, PG_BAD);
+            leave(c0 + k + 1);
+            // (drafts behind these rows are not kept either)
+            if (part == 0)
+              for (int i = c0 + m + tid; i < n; i += NT) kept[i] = -1;
+            return;
+          }
           z = sum_parts(left, 0, left.groups(), sPart);
+          parts = VW, summed = true;
         } else if (mine > 0) {
           z -= mine;
+          summed = false;
+          if (PRE && left.n_gone == GONE) {  // (more than the LDS holds)
+            if (part == 0 && tid == 0) pre->at = 0;
+            return;
+          }
           __syncthreads();
           if (tid == 0) {
             if (left.n_gone < GONE) sGone[left.n_gone] = sTok[k];
@@ -354,18 +430,22 @@ __global__ __launch_bounds__(VT) void k_verify(DraftsDesc d) {
       }
     }
   }
+  if constexpr (PRE) {
+    if (odd) flag(d.c, PG_BAD);
+    leave(n);
+    return;
+  }
   int token;
   if (greedy) {
-    token = d.best[x.row0 + node];
+    token = d.best[row0 + node];
   } else {
-    const double u = d.uniform[x.row0];
-    // (in a node whose drafts were refused, the last of those sums)
-    const double total = Q && left.sub > 0 ? z : sum_parts(left, 0, left.groups(), sPart);
-    token = draw(left, u, total, sPart, &sOut);
+    const double u = d.uniform[row0];
+    if (!summed) z = sum_parts(left, 0, left.groups(), sPart), parts = VW;
+    token = draw(left, u, z, parts, sPart, sOut);
     if (token < 0 && (left.sub > 0 || left.n_gone)) {  // nothing is left: all of the target
       left.sub = 0, left.n_gone = 0, left.q = nullptr;
-      __syncthreads();
-      token = draw(left, u, sum_parts(left, 0, left.groups(), sPart), sPart, &sOut);
+      z = sum_parts(left, 0, left.groups(), sPart);
+      token = draw(left, u, z, VW, sPart, sOut);
     }
   }
   odd = odd || token < 0;
@@ -380,19 +460,31 @@ hipError_t verify(const DraftsDesc& d, hipStream_t st) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL(k_verify<T>, dim3(d.r.n_ent), dim3(VT), 0, st, d);
+  if (d.pre) {
+    hipLaunchKernelGGL((k_verify<T, PT, true>), dim3(d.r.n_ent * (PARTS / 4)), dim3(PT), 0, st, d);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL((k_verify<T, VT, false>), dim3(d.r.n_ent), dim3(VT), 0, st, d);
   return hipGetLastError();
 }
 
 }  // namespace
 
-size_t verify_scratch(const DraftsDesc& d) { return ((size_t)d.r.n_rows * 4 + 15) & ~(size_t)15; }
+// Where VW workgroups to an entry begin the walk: rows too long for one CU, and
+// CUs that would be idle.
+static bool verify_pre(const DraftsDesc& d) { return d.vocab >= 65536 && d.r.n_ent <= 128; }
+static size_t best_bytes(const DraftsDesc& d) { return ((size_t)d.r.n_rows * 4 + 15) & ~(size_t)15; }
+size_t verify_scratch(const DraftsDesc& d) {
+  return best_bytes(d) + (verify_pre(d) ? (size_t)d.r.n_ent * sizeof(Pre) : 0);
+}
 bool verify_fits(const DraftsDesc& d) { return launchable(d.r.n_rows, 256) && launchable(d.r.n_ent, VT); }
 
 hipError_t launch_verify(const DraftsDesc& x, hipStream_t st) {
   if (x.r.n_ent <= 0 || x.r.n_rows <= 0) return hipSuccess;
   DraftsDesc d = x;
   d.best = (int32_t*)d.scratch;
+  if (d.uniform && verify_pre(d)) d.pre = (void*)((char*)d.scratch + best_bytes(d));
   return d.dtype == DT_BF16 ? verify<uint16_t>(d, st) : verify<float>(d, st);
 }
 

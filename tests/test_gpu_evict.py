@@ -1,7 +1,10 @@
 """Sequences of a paged cache cut back to their weightiest slots, on the GPU
 through the binding, against a plain model: which slots stay, where their K, V
 and weights go, which pages are freed, shared and replaced. All of it bit for
-bit; weights are summed in 64 bits on both sides, in the same order."""
+bit; weights are summed in 64 bits on both sides. (Of n weights in 32 bits
+the sums in two orders differ by n 2^-53 of them at most; weights here are drawn
+at random, or whole numbers whose sums have no error, so that no two sums lie
+that close without being equal.)"""
 import numpy as np
 import pytest
 import torch

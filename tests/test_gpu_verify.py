@@ -116,6 +116,12 @@ CASES = [
     (T32, 64, [700, 3], 30, False, False, 0),
     (T32, 64, [700, 3], 600, False, False, 0),
     (T32, 64, [600], 90, True, False, 2),
+    # rows that several workgroups begin with
+    (T32, 66001, [9, 4, 1, 0, 30], 3, True, False, 0),
+    (T32, 65536, [8, 8, 3], 0, True, False, 0),
+    (T32, 65537, [100], 90, False, False, 1),
+    (T16, 80003, [7, 12], 2, True, False, 0),
+    (T16, 65540, [5], 0, False, False, 4),
 ]
 
 
