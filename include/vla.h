@@ -600,8 +600,8 @@ typedef struct vla_scores {
  * both, and the window holds beside either. lse (fp32 [n_rows][nq], or NULL)
  * gets the logarithm of the sum of the exponentials of a row's scores, minus
  * infinity for a row that sees nothing. A capped score is at most the cap, that
- * of an infinite product too; in bf16 caches a capped score is off by
- * up to 2^-20 of the cap. Everything else is as at vla_tree_attention: rows, padding,
+ * of an infinite product too; in bf16 caches a score capped below
+ * 170 is off by up to 2^-20 of the cap. Everything else is as at vla_tree_attention: rows, padding,
  * masked slots, sums, rounding; lse overlaps none of q, out and scratch. */
 int vla_score_attention(const vla_pages* c, int32_t layer, const vla_rows* r, const vla_scores* s, const uint32_t* mask,
                         int32_t mask_words, int32_t nq, const void* q, int64_t ldq, void* out, int64_t ldo, float* lse,
@@ -688,7 +688,8 @@ int vla_verify_drafts_scratch(const vla_pages* c, const vla_rows* r, int32_t voc
  * behind them, those for drafts too, are free again where no other sequence
  * holds them; a shared page that would have to change is replaced by one of the
  * sequence's own, and a sequence for which there is none free stays as it is
- * (VLA_PAGES_OUT). Since keys stay as they were rotated, later rows go on with
+ * (VLA_PAGES_OUT). A kept slot whose table entry is no page cannot be moved: its
+ * new place holds what lay there (VLA_PAGES_OUT). Since keys stay as they were rotated, later rows go on with
  * the positions that they would have had; spans, windows and slopes count slots
  * as they lie now.
  *

@@ -249,6 +249,8 @@ __device__ __forceinline__ void move_rows(const Ev& e, int i, const Cut& x, int 
         if ((unsigned)pf < (unsigned)c.n_pages && (unsigned)pt < (unsigned)c.n_pages) {
           from = slot_elem(c, lh / c.nkv, pf, lh % c.nkv, old & (c.page - 1)) * esz;
           to = slot_elem(c, lh / c.nkv, pt, lh % c.nkv, r & (c.page - 1)) * esz;
+        } else {
+          flag(c, PG_OUT);
         }
       }
       sFrom[b][k] = from, sTo[b][k] = to;

@@ -561,7 +561,7 @@ __global__ __launch_bounds__(KT) void k_mass_join(MassArgs m) {
 // far apart that a step's offsets pass 31 bits take the other kernel.)
 bool mass_many(const MassDesc& d) {
   const long long rows = (long long)d.t.r.n_rows * (d.t.nq / d.t.c.nkv), esz = d.t.c.dtype == DT_BF16 ? 2 : 4;
-  return rows > (long long)QT * d.t.r.n_ent && d.t.ldq * esz <= (1ll << 31) / (QT + 2);
+  return rows > (long long)QT * d.t.r.n_ent && d.t.ldq * esz <= (1ll << 31) / (2 * QT + 2);
 }
 int mass_wgs(const MassDesc& d) {
   const bool wide = pad_hd(d.t.c.dtype, d.t.c.hd) * (d.t.c.dtype == DT_BF16 ? 2 : 4) > 256;

@@ -3486,15 +3486,15 @@ static int tree_operands(TreeAttnDesc* d, const uint32_t* mask, int32_t mask_wor
   VLA_TRY(paged_operand(d->c, "out", out, ldo, d->nq));
   const ByteRows o = paged_bytes(d->c, d->r, out, ldo, d->nq), in = paged_bytes(d->c, d->r, q, ldq, d->nq);
   if (meet(o, in)) return fail(VLA_EINVAL, "out must not be q or overlap it");
+  const ByteRows sums{d->lse, 0, (int64_t)d->r.n_rows * d->nq * 4, d->lse ? 1 : 0};
+  if (meet(sums, o) || meet(sums, in)) return fail(VLA_EINVAL, "lse overlaps q or out");
   VLA_TRY(device_cus(&d->cus));
   const size_t need = tree_attn_scratch(*d);
   if (!scratch || !aligned16(scratch) || scratch_bytes < 0 || (size_t)scratch_bytes < need)
     return fail(VLA_EINVAL, "scratch: needs " + std::to_string(need) + " bytes, 16-byte aligned");
   const ByteRows work{scratch, 0, (int64_t)need, 1};
   if (meet(o, work) || meet(in, work)) return fail(VLA_EINVAL, "scratch overlaps q or out");
-  const ByteRows sums{d->lse, 0, d->lse ? (int64_t)d->r.n_rows * d->nq * 4 : 0, 1};
-  if (d->lse && (meet(sums, o) || meet(sums, in) || meet(sums, work)))
-    return fail(VLA_EINVAL, "lse overlaps q, out or scratch");
+  if (meet(sums, work)) return fail(VLA_EINVAL, "lse overlaps scratch");
   d->mask = mask;
   d->mask_words = mask ? mask_words : 0;
   d->q = q;
@@ -3523,8 +3523,9 @@ int vla_tree_attention(const vla_pages* p, int32_t layer, const vla_rows* rows, 
 static int paged_scores(const vla_scores* s, ScoreDesc* d) {
   if (!s) return fail(VLA_EINVAL, "scores is NULL");
   if (!(s->scale > 0.f) || !std::isfinite(s->scale)) return fail(VLA_EINVAL, "scale must be positive and finite");
-  if (!(s->cap >= 0.f) || !std::isfinite(s->cap) || (s->cap > 0.f && !std::isfinite(4.f * s->scale / s->cap)))
-    return fail(VLA_EINVAL, "scores: cap must be 0 or positive, finite, and not so small that scale / cap is not");
+  // (both are held times log2(e), the second twice that)
+  if (!(s->cap >= 0.f) || !std::isfinite(4.f * s->cap) || (s->cap > 0.f && !std::isfinite(4.f * s->scale / s->cap)))
+    return fail(VLA_EINVAL, "scores: cap must be 0 or positive, and neither it nor scale / cap above 2^125");
   if (s->window < 0) return fail(VLA_EINVAL, "scores: window must not be negative");
   d->scale = s->scale;
   d->cap = s->cap;
@@ -3582,13 +3583,14 @@ int vla_attention_mass(const vla_pages* p, int32_t layer, const vla_rows* rows, 
     if (d.t.r.n_rows == 0 || d.t.r.n_ent == 0) return VLA_OK;  // nothing is read or written
     VLA_TRY(paged_operand(d.t.c, "q", q, ldq, nq));
     if (!lse || !mass) return fail(VLA_EINVAL, "lse or mass is NULL");
+    const ByteRows to = mass_bytes(d.t.c, mass), in = paged_bytes(d.t.c, d.t.r, q, ldq, nq);
+    const ByteRows sums{lse, 0, (int64_t)d.t.r.n_rows * nq * 4, 1};
+    if (meet(to, in) || meet(to, sums)) return fail(VLA_EINVAL, "mass overlaps q or lse");
     VLA_TRY(device_cus(&d.t.cus));
     const size_t need = mass_scratch(d);
     if (scratch_bytes < 0 || (need && (!scratch || !aligned16(scratch) || (size_t)scratch_bytes < need)))
       return fail(VLA_EINVAL, "scratch: needs " + std::to_string(need) + " bytes, 16-byte aligned");
-    const ByteRows to = mass_bytes(d.t.c, mass), work{scratch, 0, (int64_t)need, 1};
-    const ByteRows in = paged_bytes(d.t.c, d.t.r, q, ldq, nq), sums{lse, 0, (int64_t)d.t.r.n_rows * nq * 4, 1};
-    if (meet(to, in) || meet(to, sums)) return fail(VLA_EINVAL, "mass overlaps q or lse");
+    const ByteRows work{scratch, 0, (int64_t)need, 1};
     if (need && (meet(work, to) || meet(work, in) || meet(work, sums)))
       return fail(VLA_EINVAL, "scratch overlaps q, lse or mass");
     d.t.mask = mask;

@@ -594,16 +594,18 @@ __device__ __forceinline__ void add_odd_values(const Tile& t, int kb, uint32_t s
 
 // Scores q k of 32 keys from kb on become cap tanh(scale q k / cap) - slope
 // |distance|, in units of log2(e). tanh y = 1 - 2 / (e^{2 y} + 1), whose error
-// is up to 9 2^-24 of the cap; fp32 takes tanh's odd series where that would be
-// more than the score's own rounding (y^2 below 1/4: what is cut off is less
-// than 2^-23 of y).
+// is up to 9 2^-24 of the cap; fp32, and caps from CAP_LARGE on, take tanh's odd
+// series where that would be more than the score's own rounding (y^2 below 1/4:
+// what is cut off is less than 2^-23 of y).
+constexpr float CAP_LARGE = 256.f;  // of cap2: 2^-13 of a score's unit
 template <typename T>
 __device__ __forceinline__ void cap_scores(f32x16& s, const Args& a) {
+  const bool exact = sizeof(T) == 4 || a.cap2 >= CAP_LARGE;
 #pragma unroll
   for (int j = 0; j < 16; ++j) {
     const float z = s[j] * a.k1;  // 2 y log2(e)
     float v = __builtin_fmaf(-2.f * a.cap2, __builtin_amdgcn_rcpf(ex2(z) + 1.f), a.cap2);
-    if constexpr (sizeof(T) == 4) {
+    if (exact) {
       const float y = z * 0.34657359f, y2 = y * y;  // (ln 2 / 2)
       float p = 0.0035921280f;                      // 21844 / 6081075
       p = __builtin_fmaf(p, y2, -0.0088632355f);    // -1382 / 155925
@@ -1495,7 +1497,7 @@ hipError_t run(const TreeAttnDesc& d, const Args& a, hipStream_t st) {
   const int rows = tile_rows(d);
   if (rows == 32) hipLaunchKernelGGL((k_tree_few<T, HDP, SH>), dim3(a.wgs), dim3(256), 0, st, a);
   else if constexpr (sizeof(T) == 2) {
-    if (SH && a.cap2 > 0.f && !a.slopes) hipLaunchKernelGGL((k_tree_many<HDP, SH, SH>), dim3(a.wgs), dim3(256), 0, st, a);
+    if (SH && a.cap2 > 0.f && a.cap2 < CAP_LARGE && !a.slopes) hipLaunchKernelGGL((k_tree_many<HDP, SH, SH>), dim3(a.wgs), dim3(256), 0, st, a);
     else hipLaunchKernelGGL((k_tree_many<HDP, SH, false>), dim3(a.wgs), dim3(256), 0, st, a);
   }
   else hipLaunchKernelGGL((k_tree_many32<HDP, SH>), dim3(a.wgs), dim3(256), 0, st, a);

@@ -7,7 +7,7 @@ sum with 1, the reciprocal (1 step of at most 2) and the last product and sum
 make 9 2^-24 of the cap, in bf16; fp32 takes its odd series below |y| = 1/2,
 where seven roundings and the terms that are cut off (1.5 2^-24 of y) count
 against the score itself, and above, where tanh y > 0.46, 9 / 0.46 = 20 of
-them: 24 2^-24 |score|. The slope times the distance 3 2^-24 of it, and 4 2^-24
+them: 24 2^-24 |score|; so does bf16 with caps from 178 on. The slope times the distance 3 2^-24 of it, and 4 2^-24
 of |x| and of |x - max|, which is what the exponential takes. A weight is then
 off by a factor of e^delta.
 """
@@ -74,7 +74,7 @@ def scores(m, fp32, layer, s, a, c, q, h, sc):
     delta = np.matmul(np.abs(qh), np.abs(k).T) * sc.scale * (hd + 4) * E
     if sc.cap:
         x = sc.cap * np.tanh(x / sc.cap)
-        delta = delta + (24 * E * np.abs(x) if fp32 else 9 * E * sc.cap)
+        delta = delta + (24 * E * np.abs(x) if fp32 or sc.cap >= 178 else 9 * E * sc.cap)
     if sc.slopes is not None:
         b = sc.slopes[h * group:(h + 1) * group].astype(np.float64)[None, :, None] * np.abs(gap)[:, None, :]
         x = x - b

@@ -52,6 +52,14 @@ CASES = [
     (T32, 128, 8, 1, 64, 12.0, True, 60, None, None, [5, 200], [64, 100]),
     (T32, 64, 8, 1, 16, 1.0, True, 30, "docs", None, [70, 0], [150, 41]),
     (T32, 96, 6, 1, 16, 6.0, True, 11, None, "any", [33], [91]),
+    # caps that bend next to nothing
+    (T16, 128, 8, 2, 16, 1e4, False, 0, None, None, [300, 20], [1, 1]),
+    (T16, 64, 4, 1, 16, 1e4, False, 0, None, None, [100], [250]),
+    (T32, 64, 4, 1, 16, 1e6, False, 0, None, None, [100], [25]),
+    # groups that do not divide a step, or are longer than one
+    (T16, 64, 40, 1, 16, 0.0, True, 0, None, None, [150, 0], [1, 20]),
+    (T16, 128, 72, 1, 16, 7.0, False, 50, None, None, [90], [9]),
+    (T32, 64, 80, 1, 16, 0.0, False, 0, None, None, [130], [3]),
 ]
 
 

@@ -78,7 +78,7 @@ def run(V, T, probs, drafted, tokens, parent, u, start, seqs, n_seqs, pad=0):
         if x is None:
             return None
         t = torch.full((n, vocab + pad), float("nan"), dtype=T, device="cuda")
-        t[:, :vocab] = torch.from_numpy(x).to(T).cuda()
+        t[:, :vocab] = torch.from_numpy(np.array(x)).to(T).cuda()
         return t[:, :vocab]
 
     z = torch.zeros((1, 1, 1, 16, 32), dtype=T16, device="cuda")
