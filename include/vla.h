@@ -670,8 +670,9 @@ typedef struct vla_drafts {
  * where p has no sum or an infinite one, or no likeliest token (VLA_PAGES_BAD
  * each). An entry without rows has n_kept 0 and next -1. Of c the sequences
  * (which entries are padding) and the status count. scratch:
- * vla_verify_drafts_scratch bytes, 16-byte aligned; kept, n_kept, next and
- * scratch overlap nothing else of the call. */
+ * vla_verify_drafts_scratch bytes, 16-byte aligned, contents of no matter; calls
+ * that may overlap need their own. kept, n_kept, next and scratch overlap nothing
+ * else of the call. */
 int vla_verify_drafts(const vla_pages* c, const vla_rows* r, const vla_drafts* d, int32_t* kept, int32_t* n_kept,
                       int32_t* next, void* scratch, int64_t scratch_bytes, void* stream);
 
@@ -700,7 +701,8 @@ int vla_verify_drafts_scratch(const vla_pages* c, const vla_rows* r, int32_t voc
  * mass itself, or else overlaps it nowhere. Entries whose sequence is not in 0
  * .. n_seqs - 1 are skipped, so is a sequence that was listed before, and one
  * whose keep is negative (VLA_PAGES_BAD). scratch: vla_pages_evict_scratch
- * bytes, 16-byte aligned. kept, scratch and mass_out are apart from each other
+ * bytes, 16-byte aligned, contents of no matter; calls that may overlap need
+ * their own. kept, scratch and mass_out are apart from each other
  * and from seqs and keep. */
 int vla_pages_evict(const vla_pages* c, int32_t n, const int32_t* seqs, const int32_t* keep, int32_t first,
                     int32_t last, const float* mass, float* mass_out, int32_t* kept, void* scratch,
