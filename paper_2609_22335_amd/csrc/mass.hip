@@ -407,7 +407,7 @@ __global__ __launch_bounds__(256, (many_waves<T, HDP>())) void k_mass_few(MassAr
 // of 64 through two stages in the LDS, the next step on its way: one barrier to
 // a step, and the products of a step's second half beside the exponentials of
 // its first. Two chunks of 2,000 rows behind 2,000 to 6,000 slots, 32 heads on 8
-// of 128 (150 GFLOP): 225 us, 0.67 PFLOP/s; with steps of 32 and a third stage
+// of 128 (150 GFLOP): 221 us, 0.68 PFLOP/s; with steps of 32 and a third stage
 // 255 us, with queries through registers 641 us.
 template <typename T, int HDP>
 __global__ __launch_bounds__(256, (mass_waves<T, HDP>())) void k_mass_many(MassArgs m) {
@@ -424,11 +424,15 @@ __global__ __launch_bounds__(256, (mass_waves<T, HDP>())) void k_mass_many(MassA
   const long long tiles = row.count();
   if (tiles == 0) return;
   const int cuts = row.cuts(tiles, m.target);
-  const long long units = tiles * cuts, wgs = gridDim.x;
+  // Workgroups go round the eight XCDs: each takes an eighth of the units, so
+  // that its L2 serves a head's queries to neighbouring tiles (221 us against 225).
+  // Within it units go by in turn, since later slots are seen by fewer rows.
+  const long long units = tiles * cuts, share = (units + 7) >> 3, step_by = gridDim.x >> 3;
   row.begin();
   Spot s;
-  // (units in turn, since later slots are seen by fewer rows)
-  for (long long u = blockIdx.x; u < units; u += wgs) {
+  for (long long v = blockIdx.x >> 3; v < share; v += step_by) {
+    const long long u = (blockIdx.x & 7) * share + v;
+    if (u >= units) break;
     const long long tile = cuts > 1 ? u / cuts : u;
     if (!row.at(tile, s)) break;
     const Tile& t = s.t;
