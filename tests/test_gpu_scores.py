@@ -60,6 +60,15 @@ CASES = [
     (T16, 64, 40, 1, 16, 0.0, True, 0, None, None, [150, 0], [1, 20]),
     (T16, 128, 72, 1, 16, 7.0, False, 50, None, None, [90], [9]),
     (T32, 64, 80, 1, 16, 0.0, False, 0, None, None, [130], [3]),
+    # capped, not biased, in tiles of 128 rows at the other head dims
+    (T16, 64, 4, 1, 32, 9.0, False, 0, None, None, [50], [260]),
+    (T16, 160, 4, 2, 16, 12.0, False, 33, "prefix", None, [20], [200]),
+    (T16, 224, 3, 1, 16, 5.0, False, 0, None, "tree", [100], [90]),
+    # tiles that many workgroups share, with the slots before a window left out
+    (T16, 128, 8, 1, 64, 20.0, True, 20000, None, None, [30000], [2]),
+    (T16, 64, 4, 1, 64, 20.0, False, 5000, None, None, [8000], [260]),
+    (T16, 128, 16, 4, 64, 0.0, True, 0, None, None, [5000, 300, 9000], [1, 1, 1]),
+    (T32, 64, 4, 2, 32, 0.0, False, 3000, None, None, [6000, 40], [1, 200]),
 ]
 
 

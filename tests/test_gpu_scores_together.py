@@ -66,7 +66,8 @@ class Call:
 
 
 @pytest.mark.parametrize("T,rows,window,cap", [(T16, [1], 0, 0.0), (T16, [1, 2, 3], 30, 9.0), (T16, [40, 0, 70], 20, 0.0),
-                                               (T32, [1, 0, 30], 50, 3.0)])
+                                               (T32, [1, 0, 30], 50, 3.0), (T16, [1] * 8 + [40], 25, 0.0),
+                                               (T32, [1] * 8 + [30], 0, 5.0)])
 def test_more_entries_than_lanes(V, T, rows, window, cap):
     say(f"scores many entries {T} rows={rows} window={window}")
     rng = np.random.default_rng(sum(rows) + window)

@@ -69,12 +69,12 @@ def tree(rng, n, width):
     return [-1] + [int(rng.integers(max(0, i - 2 * width), max(1, i - width + 1))) if i > width else 0 for i in range(1, n)]
 
 
-def run(V, T, probs, drafted, tokens, parent, u, start, seqs, n_seqs, pad=0):
+def run(V, T, probs, drafted, tokens, parent, u, start, seqs, n_seqs, pad=0, skew=0):
     """The call on whole arrays (numpy), its rows `pad` values apart from one
-    another."""
+    another (the drafts' distributions' `skew` more)."""
     n, vocab = probs.shape
 
-    def wide(x):
+    def wide(x, pad=pad):
         if x is None:
             return None
         t = torch.full((n, vocab + pad), float("nan"), dtype=T, device="cuda")
@@ -89,7 +89,7 @@ def run(V, T, probs, drafted, tokens, parent, u, start, seqs, n_seqs, pad=0):
     count, after = (torch.full((len(seqs),), -7, dtype=torch.int32, device="cuda") for _ in range(2))
     scratch = torch.full((V.vla_verify_drafts_scratch(pages, r, vocab),), 255, dtype=torch.uint8, device="cuda")
     V.vla_verify_drafts(pages, r, i32(tokens), wide(probs), kept, count, after, scratch,
-                        parent=None if parent is None else i32(parent), drafted=wide(drafted),
+                        parent=None if parent is None else i32(parent), drafted=wide(drafted, pad + skew),
                         uniform=None if u is None else torch.from_numpy(u).cuda())
     torch.cuda.synchronize()
     return kept.cpu().numpy(), count.cpu().numpy(), after.cpu().numpy(), int(status.item())
@@ -171,6 +171,25 @@ def test_verify(V, T, vocab, rows, width, drafted, greedy, pad):
         assert got[3] == 0
     # (the test tries something; drafts chosen without chance from a flat target are seldom kept)
     assert taken > 0 or not (drafted or greedy)
+
+
+@pytest.mark.parametrize("T,vocab", [(T32, 4001), (T16, 4001), (T32, 70000), (T16, 65541)])
+def test_rows_of_two_alignments(V, T, vocab):
+    """The draft's rows need not lie as the target's do."""
+    say(f"verify alignments {T} vocab={vocab}")
+    rng = np.random.default_rng(vocab)
+    n = 24
+    p, q = (torch.from_numpy(softmax(2 * rng.standard_normal((n, vocab)))).to(T).to(torch.float64).numpy() for _ in range(2))
+    parent = [-1, 0, 0, 0, 1, 2, 3, 3] * 3
+    tokens, u = rng.integers(0, vocab, n), rng.random(n).astype(np.float32)
+    got = [run(V, T, p, q, tokens, parent, u, [0, 8, 16, 24], [0, 1, 2], 3, pad, skew)
+           for pad, skew in ((0, 0), (0, 1), (3, 2), (1, 7))]
+    for g in got[1:]:
+        assert all(np.array_equal(x, y) for x, y in zip(g, got[0]))
+    for e in range(3):
+        path, after, _ = walk(p[8 * e:8 * e + 8], q[8 * e:8 * e + 8], tokens[8 * e:8 * e + 8], parent[:8],
+                              u[8 * e:8 * e + 8].astype(np.float64))
+        assert got[0][1][e] == len(path) and got[0][2][e] == after
 
 
 def test_edges(V):
