@@ -630,7 +630,7 @@ int vla_attention_mass(const vla_pages* c, int32_t layer, const vla_rows* r, con
 /* Bytes of scratch (may be 0; host only, but depends on the current device). */
 int vla_attention_mass_scratch(const vla_pages* c, const vla_rows* r, int32_t nq, int64_t* bytes);
 
-/* Drafted tokens and what they are judged by. A step's entry has its decided
+/* Drafted tokens and what they are measured against. A step's entry has its decided
  * token in its first row and its drafts behind it; probs' row t is the target's
  * distribution of what follows row t's token. */
 typedef struct vla_drafts {

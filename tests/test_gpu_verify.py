@@ -193,7 +193,7 @@ def test_rows_of_two_alignments(V, T, vocab):
 
 
 def test_edges(V):
-    """Ties, drafts that cannot be judged, nothing left of a target, no target."""
+    """Ties, drafts that cannot be tried, nothing left of a target, no target."""
     say("verify edges")
     f = lambda *x: np.array(x, np.float64)  # noqa: E731
     nan, inf = float("nan"), float("inf")
