@@ -1,7 +1,7 @@
 // Kernels of the paged KV cache: per-head norms and rotation with the store
 // into pages, and the pages' own book-keeping (who holds which page, copies
 // on a fork, accepted drafts moved together). Attention over it is in
-// tree.hip.
+// tree_dev.h.
 #include <algorithm>
 
 #include "paged_dev.h"
