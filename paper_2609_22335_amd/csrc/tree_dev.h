@@ -335,6 +335,7 @@ __device__ __forceinline__ Bounds bounds_of(const Tile& t) {
     x.last = t.kend;
     if (a.span || (a.window && a.depth)) {
       int own = 0x7FFFFFFF, lo = 0, first = 0x7FFFFFFF, last = 0;
+      bool far = false;  // a draft may lie `window` or more places before a row (none lies before t.len)
 #pragma unroll
       for (int i = 0; i < (BM + 63) / 64; ++i) {
         const int m = t.rt * BM + 64 * i + (int)(threadIdx.x & (BM < 64 ? BM - 1 : 63)), mc = m < t.M ? m : t.M - 1;
@@ -343,6 +344,7 @@ __device__ __forceinline__ Bounds bounds_of(const Tile& t) {
         lo = r.lo > lo ? r.lo : lo;
         first = r.lo < first ? r.lo : first;
         last = r.own > last ? r.own : last;
+        far = far || r.place - t.len >= a.window;
       }
 #pragma unroll
       for (int d = 1; d < 64; d *= 2) {
@@ -354,6 +356,8 @@ __device__ __forceinline__ Bounds bounds_of(const Tile& t) {
       x.low = uni(lo), x.first = uni(first), x.last = uni(last);
       own = uni(own);
       x.safe = a.span && !a.mask ? own : own < x.safe ? own : x.safe;
+      // (lo does not pass t.len: those drafts are looked at one by one)
+      if (a.window && a.depth && __any(far)) x.safe = min(x.safe, t.len);
     } else if (a.window) {
       const int m1 = (t.rt + 1) * BM < t.M ? (t.rt + 1) * BM - 1 : t.M - 1;
       const int w1 = t.len + m1 / t.group - a.window + 1, w0 = t.len + t.rt * BM / t.group - a.window + 1;
