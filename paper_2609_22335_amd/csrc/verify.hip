@@ -22,6 +22,10 @@ __device__ __forceinline__ float value(const T* p) {
   else return *p;
 }
 
+// A probability as it counts: 0 where it is negative or not a number. (Where
+// max(p - S q, 0) is worked out q alone needs it: that is 0 for every such p.)
+__device__ __forceinline__ float some(float x) { return fmaxf(x, 0.f); }
+
 // A row's elements t0 .. t0 + VEC - 1, t0 from -VEC + 1 on: one load where all
 // of them are the row's and aligned; others are 0.
 template <typename T>
@@ -35,8 +39,9 @@ __device__ __forceinline__ void load_some(const T* row, int t0, int V, bool alig
   }
 }
 
-// What is left of a node's target: max(p - sub q, 0) (drafts drawn from q), or
-// p without the tokens that were refused (drafts chosen without chance).
+// What is left of a node's target: max(p - sub q, 0) (drafts drawn from q, of
+// which a negative one or NaN is 0), or p without the tokens that were refused
+// (drafts chosen without chance).
 template <typename T>
 struct Left {
   const T *p, *q;  // q null: `gone` counts
@@ -65,7 +70,7 @@ struct Left {
     constexpr int N = El<T>::VEC;
     if (q) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) r[i] = fmax((double)x[i] - sub * (double)y[i], 0.0);
+      for (int i = 0; i < N; ++i) r[i] = fmax((double)x[i] - sub * (double)some(y[i]), 0.0);
     } else {
 #pragma unroll
       for (int i = 0; i < N; ++i) r[i] = fmax((double)x[i], 0.0);
@@ -373,8 +378,8 @@ __global__ __launch_bounds__(NT) void k_verify(DraftsDesc d) {
         sP[k] = in && d.best[row0 + par] == tok ? 1.f : 0.f;
       } else {
         sU[k] = d.uniform[row];
-        sP[k] = in ? value(P + (size_t)par * d.ldp + tok) : 0.f;
-        sQ[k] = in && Q ? value(Q + (size_t)par * d.ldq + tok) : 0.f;
+        sP[k] = in ? some(value(P + (size_t)par * d.ldp + tok)) : 0.f;
+        sQ[k] = in && Q ? some(value(Q + (size_t)par * d.ldq + tok)) : 0.f;
       }
       if (part == 0 && (PRE || !pre || at == 1)) kept[i] = -1;
     }
@@ -389,7 +394,7 @@ __global__ __launch_bounds__(NT) void k_verify(DraftsDesc d) {
         mine = fmax((double)sP[k] - left.sub * (double)sQ[k], 0.0);
         yes = (double)sU[k] * (double)sQ[k] * z < mine;
       } else {
-        mine = fmax((double)sP[k], 0.0);
+        mine = sP[k];
         for (int j = 0; j < left.n_gone; ++j) mine = left.refused(j) == sTok[k] ? 0.0 : mine;
         yes = (double)sU[k] * z < mine;
       }

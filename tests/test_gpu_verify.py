@@ -253,3 +253,72 @@ def test_answers_are_distributed_as_the_target(V):
         share = np.bincount(first, minlength=vocab) / n
         assert np.all(np.abs(share - p / p.sum()) < 5 * np.sqrt(p * (1 - p) / n)), (share, p)
         assert got[3] == 0
+
+
+ODD = [
+    # T, vocab, rows, tree width: one workgroup an entry, and several at first
+    (T32, 5, 40, 6), (T32, 3001, 24, 4), (T16, 2050, 17, 3), (T32, 300, 9, 0), (T32, 66001, 30, 4), (T16, 80003, 12, 2),
+]
+
+
+@pytest.mark.parametrize("T,vocab,rows,width", ODD)
+def test_odd_values_of_the_drafts(V, T, vocab, rows, width):
+    """Negative probabilities and NaN count as 0 in the drafts' distributions as
+    in the target's: the answers are those of the clean ones."""
+    say(f"verify odd drafted {T} vocab={vocab} rows={rows}")
+    for seed in range(4):
+        rng = np.random.default_rng(vocab + rows + 1000 * seed)
+        n = 3 * rows
+        p, q = (torch.from_numpy(softmax(2 * rng.standard_normal((n, vocab)))).to(T).to(torch.float64).numpy() for _ in range(2))
+        for x in (p, q):
+            at = rng.random(x.shape)
+            at[:, 0] = 0.5  # (something is left of every row)
+            x[at < 0.15] = np.nan
+            x[(at >= 0.15) & (at < 0.35)] *= -1
+            x[at > 0.9] = 0
+        clean = np.where(q > 0, q, 0)
+        parent = np.concatenate([tree(rng, rows, width) if width else np.arange(-1, rows - 1) for _ in range(3)])
+        tokens, u = rng.integers(0, vocab, n), rng.random(n).astype(np.float32)
+        u[rng.random(n) < 0.2] = 0
+        # (tokens whose q is odd among those that are tried)
+        for i in range(n):
+            row = i // rows * rows + max(0, int(parent[i]))
+            odd = np.flatnonzero(~(q[row] >= 0))
+            if len(odd) and rng.random() < 0.5:
+                tokens[i] = rng.choice(odd)
+        start = [0, rows, 2 * rows, n]
+        got = run(V, T, p, q, tokens, parent if width else None, u, start, [0, 1, 2], 3)
+        near = []
+        for e in range(3):
+            s = slice(e * rows, (e + 1) * rows)
+            path, after, bad = walk(p[s], clean[s], tokens[s], parent[s] if width else None, u[s].astype(np.float64), near)
+            assert got[1][e] == len(path) and got[2][e] == after and not bad
+            assert list(got[0][s]) == path + [-1] * (rows - len(path))
+        assert all(x > 1e-11 for x in near)
+        assert got[3] == 0
+
+
+@pytest.mark.parametrize("T", [T32, T16])
+def test_odd_drafted_one_by_one(V, T):
+    """A token whose target is 0 is not kept for a negative q, nor refused for a
+    NaN; what is left of a target never passes it."""
+    say(f"verify odd drafted one by one {T}")
+    nan = float("nan")
+    P = np.array([[0.0, 0.5, 0.25, 0.25]] * 2)
+    half = np.array([0.5, 0.5], np.float32)
+
+    def answer(q, token, u=half):
+        got = run(V, T, P, np.array([q] * 2, np.float64), [0, token], None, u, [0, 2], [0], 1)
+        assert got[3] == 0
+        return int(got[1][0]), int(got[2][0])
+
+    # p = 0: refused whatever q is; all of the target is left (q is 0 elsewhere): sums 0.5, 0.75, 1
+    for x in (-0.5, nan, 0.0):
+        assert answer([x, 0, 0, 0], 0, np.array([0.6, 0.5], np.float32)) == (1, 2)
+    # p > 0 and q 0: kept
+    for x in (-0.5, nan, 0.0):
+        assert answer([0, x, 0, 0], 1)[0] == 2
+    # token 2 is refused (u q = 0.5 > 0.25) and leaves max(p - q, 0) = 0, 0.5, 0, 0.25 beside a q of 0, negative or NaN
+    for x in (-1.0, nan, 0.0):
+        for u0, want in ((0.3, 1), (0.9, 3)):
+            assert answer([x, x, 1, x], 2, np.array([u0, 0.5], np.float32)) == (1, want)
