@@ -668,8 +668,9 @@ typedef struct vla_drafts {
  * n_kept and next: int32 [n_entries]. A draft whose parent does not stand before
  * it or whose token is outside the vocabulary is passed over, and next is -1
  * where p has no sum or an infinite one, or no likeliest token (VLA_PAGES_BAD
- * each). An entry without rows has n_kept 0 and next -1. Of c the sequences
- * (which entries are padding) and the status count. scratch:
+ * each). An entry without rows has n_kept 0 and next -1; of a batch without any
+ * (n_rows 0) that is all that is written, and start and seqs all that is read.
+ * Of c the sequences (which entries are padding) and the status count. scratch:
  * vla_verify_drafts_scratch bytes, 16-byte aligned, contents of no matter; calls
  * that may overlap need their own. kept, n_kept, next and scratch overlap nothing
  * else of the call. */

@@ -3631,18 +3631,26 @@ int vla_verify_drafts(const vla_pages* p, const vla_rows* rows, const vla_drafts
     VLA_TRY(drafts_size(p, rows, x->vocab, &d));
     if (x->dtype != VLA_F32 && x->dtype != VLA_BF16) return fail(VLA_EINVAL, "drafts: dtype");
     if (x->drafted && !x->uniform) return fail(VLA_EINVAL, "drafts: drafted needs uniform");
-    if (d.r.n_rows == 0 || d.r.n_ent == 0) return VLA_OK;  // nothing is read or written
-    if (!x->tokens || !x->probs || !kept || !n_kept || !next) return fail(VLA_EINVAL, "NULL argument");
+    if (d.r.n_ent == 0) return VLA_OK;  // nothing is read or written
+    if (!n_kept || !next) return fail(VLA_EINVAL, "NULL argument");
     const int64_t esz = x->dtype == VLA_BF16 ? 2 : 4, n = d.r.n_rows;
+    const size_t need = verify_scratch(d);
+    const ByteRows out[4] = {{n_kept, 0, (int64_t)d.r.n_ent * 4, 1}, {next, 0, (int64_t)d.r.n_ent * 4, 1},
+                             {kept, 0, n * 4, 1}, {scratch, 0, (int64_t)need, 1}};
+    d.dtype = x->dtype == VLA_BF16 ? DT_BF16 : DT_F32;
+    d.n_kept = n_kept;
+    d.next = next;
+    if (n == 0) {  // (every entry is answered; nothing else is read or written)
+      if (meet(out[0], out[1])) return fail(VLA_EINVAL, "kept, n_kept, next and scratch must not overlap");
+      return paged_launch("verify drafts", launch_verify(d, (hipStream_t)stream));
+    }
+    if (!x->tokens || !x->probs || !kept) return fail(VLA_EINVAL, "NULL argument");
     if (x->ld_probs < x->vocab || x->ld_probs > ((int64_t)1 << 31) || (uintptr_t)x->probs % esz)
       return fail(VLA_EINVAL, "drafts: probs' row stride or alignment");
     if (x->drafted && (x->ld_drafted < x->vocab || x->ld_drafted > ((int64_t)1 << 31) || (uintptr_t)x->drafted % esz))
       return fail(VLA_EINVAL, "drafts: drafted's row stride or alignment");
-    const size_t need = verify_scratch(d);
     if (!scratch || !aligned16(scratch) || scratch_bytes < 0 || (size_t)scratch_bytes < need)
       return fail(VLA_EINVAL, "scratch: needs " + std::to_string(need) + " bytes, 16-byte aligned");
-    const ByteRows out[4] = {{kept, 0, n * 4, 1}, {n_kept, 0, (int64_t)d.r.n_ent * 4, 1},
-                             {next, 0, (int64_t)d.r.n_ent * 4, 1}, {scratch, 0, (int64_t)need, 1}};
     const ByteRows in[5] = {{x->tokens, 0, n * 4, 1}, {x->parent, 0, x->parent ? n * 4 : 0, x->parent ? 1 : 0},
                             {x->uniform, 0, n * 4, x->uniform ? 1 : 0},
                             {x->probs, x->ld_probs * esz, x->vocab * esz, n},
@@ -3653,7 +3661,6 @@ int vla_verify_drafts(const vla_pages* p, const vla_rows* rows, const vla_drafts
       for (int j = 0; j < i; ++j)
         if (meet(out[i], out[j])) return fail(VLA_EINVAL, "kept, n_kept, next and scratch must not overlap");
     }
-    d.dtype = x->dtype == VLA_BF16 ? DT_BF16 : DT_F32;
     d.tokens = x->tokens;
     d.parent = x->parent;
     d.probs = x->probs;
@@ -3662,8 +3669,6 @@ int vla_verify_drafts(const vla_pages* p, const vla_rows* rows, const vla_drafts
     d.ldq = x->ld_drafted;
     d.uniform = x->uniform;
     d.kept = kept;
-    d.n_kept = n_kept;
-    d.next = next;
     d.scratch = scratch;
     return paged_launch("verify drafts", launch_verify(d, (hipStream_t)stream));
   })

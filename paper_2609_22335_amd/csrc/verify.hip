@@ -460,7 +460,7 @@ __global__ __launch_bounds__(NT) void k_verify(DraftsDesc d) {
 
 template <typename T>
 hipError_t verify(const DraftsDesc& d, hipStream_t st) {
-  if (!d.uniform) {
+  if (!d.uniform && d.r.n_rows > 0) {
     hipLaunchKernelGGL(k_likeliest<T>, dim3(d.r.n_rows), dim3(256), 0, st, d);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
@@ -486,10 +486,11 @@ size_t verify_scratch(const DraftsDesc& d) {
 bool verify_fits(const DraftsDesc& d) { return launchable(d.r.n_rows, 256) && launchable(d.r.n_ent, VT); }
 
 hipError_t launch_verify(const DraftsDesc& x, hipStream_t st) {
-  if (x.r.n_ent <= 0 || x.r.n_rows <= 0) return hipSuccess;
+  if (x.r.n_ent <= 0) return hipSuccess;
   DraftsDesc d = x;
   d.best = (int32_t*)d.scratch;
-  if (d.uniform && verify_pre(d)) d.pre = (void*)((char*)d.scratch + best_bytes(d));
+  // (a batch without rows has entries to answer all the same, and no scratch)
+  if (d.uniform && d.r.n_rows > 0 && verify_pre(d)) d.pre = (void*)((char*)d.scratch + best_bytes(d));
   return d.dtype == DT_BF16 ? verify<uint16_t>(d, st) : verify<float>(d, st);
 }
 

@@ -322,3 +322,16 @@ def test_odd_drafted_one_by_one(V, T):
     for x in (-1.0, nan, 0.0):
         for u0, want in ((0.3, 1), (0.9, 3)):
             assert answer([x, x, 1, x], 2, np.array([u0, 0.5], np.float32)) == (1, want)
+
+
+@pytest.mark.parametrize("kind", ["greedy", "chosen", "drawn"])
+@pytest.mark.parametrize("vocab", [50, 70000])
+def test_a_batch_without_rows(V, kind, vocab):
+    """Entries without rows are answered where the whole batch has none, too;
+    padding is left as it was."""
+    say(f"verify no rows {kind} vocab={vocab}")
+    probs = np.zeros((0, vocab))
+    none = np.zeros(0, np.float32)
+    got = run(V, T32, probs, probs if kind == "drawn" else None, none, None, None if kind == "greedy" else none,
+              [0, 0, 0, 0, 0], [1, -1, 0, 7], 2)
+    assert list(got[1]) == [0, -7, 0, -7] and list(got[2]) == [-1, -7, -1, -7] and got[3] == 0

@@ -140,6 +140,23 @@ def test_verify_refuses():
     refused("vocab", V.vla_verify_drafts_scratch, p, r, 2 ** 28 + 1)
 
 
+def test_verify_without_rows_refuses():
+    """Entries of a batch without rows are answered, so what the answers go to is
+    looked at, and nothing else."""
+    p, r = cache(), V.make_rows(Dev((3,)), 0)
+    none, nk, nx, scr = Dev((0,), ptr=None), far((2,), torch.int32, 4), far((2,), torch.int32, 5), far((16,), U8, 8)
+    call = V.vla_verify_drafts
+    refused("n_kept holds 1", call, p, r, none, Dev((0, 9), F), none, far((1,), torch.int32), nx, scr)
+    refused("next must have shape", call, p, r, none, Dev((0, 9), F), none, nk, far((3,), torch.int32), scr)
+    refused("must not overlap", call, p, r, none, Dev((0, 9), F), none, nk, Dev((2,), ptr=nk.data_ptr() + 4), scr)
+    refused("drafted needs uniform", call, p, r, none, Dev((0, 9), F), none, nk, nx, scr, drafted=Dev((0, 9), F))
+    x, d = C.c_void_p(0x10000), V.vla_drafts(0, 9, None, None, None, 0, None, 0, None)
+    lib, args = V._lib.vla_verify_drafts, (C.byref(p), C.byref(r), C.byref(d), None)
+    for out in ((None, x), (x, None)):
+        assert lib(*args, *out, None, 0, None) == -1
+        assert "NULL" in V.vla_last_error()
+
+
 @pytest.mark.parametrize("field,value,msg", [
     ("dtype", 2, "dtype"), ("head_dim", 48, "head_dim"), ("page_len", 24, "page_len"), ("k", None, "NULL"),
 ])
