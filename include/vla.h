@@ -660,8 +660,10 @@ typedef struct vla_drafts {
  * token t for which r(0) + ... + r(t) passes u times the sum of r, u the first
  * row's number; of p, where r is 0 everywhere. With uniform NULL a draft is kept
  * when it is the likeliest token of the row that it follows (the lowest of
- * several), and next is the last row's. All of it is computed in 64 bits;
- * probabilities are taken as they are given, negative ones and NaN as 0.
+ * several), and next is the last row's; values are compared as they are then,
+ * NaN and minus infinity left out, so that probs may be logits. Otherwise all of
+ * it is computed in 64 bits, and probabilities are taken as they are given,
+ * negative ones and NaN as 0.
  *
  * kept[start[e] + j] gets, for j < n_kept[e], the rows (of the entry, ascending,
  * 0 first) that are kept, and -1 behind them, as vla_pages_commit takes it.

@@ -335,3 +335,17 @@ def test_a_batch_without_rows(V, kind, vocab):
     got = run(V, T32, probs, probs if kind == "drawn" else None, none, None, None if kind == "greedy" else none,
               [0, 0, 0, 0, 0], [1, -1, 0, 7], 2)
     assert list(got[1]) == [0, -7, 0, -7] and list(got[2]) == [-1, -7, -1, -7] and got[3] == 0
+
+
+def test_likeliest_of_odd_rows(V):
+    """The likeliest token is looked for among the values as they are, NaN left
+    out, so that logits will do."""
+    say("verify likeliest of odd rows")
+    nan, inf = float("nan"), float("inf")
+    rows = [([-3, -1, -2, nan], 1), ([-1, 0, -1, 0], 1), ([nan, -inf, -5, -5], 2), ([-inf] * 4, -1), ([nan] * 4, -1),
+            ([0, inf, 1, inf], 1), ([nan, 0, 0, 0], 1)]
+    for T in (T32, T16):
+        for row, best in rows:
+            got = run(V, T, np.array([row, [0, 0, 0, 1]], np.float64), None, [0, max(best, 0)], None, None, [0, 2], [0], 1)
+            assert got[1][0] == (2 if best >= 0 else 1) and got[2][0] == (3 if best >= 0 else -1)
+            assert got[3] == (0 if best >= 0 else V.PAGES_BAD)
