@@ -378,10 +378,16 @@ hipError_t launch_pages_evict(const EvictDesc& d, hipStream_t st) {
   e.fresh = (int32_t*)p;
   p += up16((size_t)d.n * c.max_pages * 4);
   e.score = (double*)p;
+  // (each works on what the one before left)
+  hipError_t err;
   hipLaunchKernelGGL(k_evict_score, dim3((e.slots + 255) / 256, d.n), dim3(256), 0, st, e);
+  if ((err = hipGetLastError()) != hipSuccess) return err;
   hipLaunchKernelGGL(k_evict_pick, dim3(d.n), dim3(PICK), 0, st, e);
+  if ((err = hipGetLastError()) != hipSuccess) return err;
   hipLaunchKernelGGL(k_evict_pages, dim3(1), dim3(PICK), 0, st, e);
+  if ((err = hipGetLastError()) != hipSuccess) return err;
   hipLaunchKernelGGL(k_evict_move, dim3((unsigned)(d.n * movers(c))), dim3(MOVE), 0, st, e, width_of(c));
+  if ((err = hipGetLastError()) != hipSuccess) return err;
   hipLaunchKernelGGL(k_evict_done, dim3(d.n), dim3(256), 0, st, e);
   return hipGetLastError();
 }
