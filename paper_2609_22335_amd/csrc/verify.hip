@@ -351,8 +351,13 @@ __global__ __launch_bounds__(NT) void k_verify(DraftsDesc d) {
     left.set(P, Q, d.vocab);
     if (part == 0 && tid == 0) kept[0] = 0;
   }
+  // Where no draft was refused (S is 0) all of the target is left, whatever q holds.
+  auto untouched = [&] {
+    if (!(left.sub > 0)) left.q = nullptr;
+  };
   // PRE: this wave's part of what is left, and where the walk is
   auto leave = [&](int next) {
+    untouched();
     const int wv = tid >> 6, mine = part * 4 + wv, groups = left.groups(), per = part_of(groups, PARTS);
     const int a = min(mine * per, groups), b = min(a + per, groups);
     const double s = wave_sum(a < b ? left.sum(a, b) : 0.0);
@@ -445,6 +450,7 @@ __global__ __launch_bounds__(NT) void k_verify(DraftsDesc d) {
     token = d.best[row0 + node];
   } else {
     const double u = d.uniform[row0];
+    untouched();
     if (!summed) z = sum_parts(left, 0, left.groups(), sPart), parts = VW;
     token = draw(left, u, z, parts, sPart, sOut);
     if (token < 0 && (left.sub > 0 || left.n_gone)) {  // nothing is left: all of the target

@@ -324,6 +324,27 @@ def test_odd_drafted_one_by_one(V, T):
             assert answer([x, x, 1, x], 2, np.array([u0, 0.5], np.float32)) == (1, want)
 
 
+@pytest.mark.parametrize("T,vocab", [(T32, 9), (T16, 4001), (T32, 70001)])
+def test_infinite_drafted(V, T, vocab):
+    """All of a target is left where no draft of it was refused, whatever q holds;
+    of a token whose q is infinite nothing is left where one was."""
+    say(f"verify infinite drafted {T} vocab={vocab}")
+    P = np.zeros((3, vocab))
+    P[:, [1, vocab - 2, vocab - 1]] = 0.5, 0.25, 0.25
+    q = np.zeros((3, vocab))
+    q[:, 1] = np.inf
+    for u0, want in ((0.25, 1), (0.625, vocab - 2), (0.875, vocab - 1)):
+        u = np.array([u0, 0.5, 0.5], np.float32)
+        # no draft; one that is kept (its q is 0)
+        got = run(V, T, P[:1], q[:1], [0], None, u[:1], [0, 1], [0], 1)
+        assert got[1][0] == 1 and got[2][0] == want and got[3] == 0
+        got = run(V, T, P[:2], q[:2], [0, vocab - 1], None, u[:2], [0, 2], [0], 1)
+        assert got[1][0] == 2 and got[2][0] == want and got[3] == 0
+        # token 0 (p = 0) is refused first: half of the rest to each of the last two
+        got = run(V, T, P, q, [0, 0, 1], [-1, 0, 0], u, [0, 3], [0], 1)
+        assert got[1][0] == 1 and got[2][0] == (vocab - 2 if u0 < 0.5 else vocab - 1) and got[3] == 0
+
+
 @pytest.mark.parametrize("kind", ["greedy", "chosen", "drawn"])
 @pytest.mark.parametrize("vocab", [50, 70000])
 def test_a_batch_without_rows(V, kind, vocab):
