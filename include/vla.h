@@ -496,10 +496,13 @@ typedef struct vla_pages {
 } vla_pages;
 
 /* status bits: what a call found on the device and left undone */
-#define VLA_PAGES_OUT 1 /* a page was missing: the pool or a table was full, or a slot */
-                        /*   without a page was to be written                       */
-#define VLA_PAGES_BAD 2 /* a position outside the rotation table, or an accepted list  */
-                        /*   that does not ascend within its drafts                 */
+#define VLA_PAGES_OUT 1 /* a page was missing: the pool or a table was full, a slot    */
+                        /*   without a page was to be written or moved, or a        */
+                        /*   sequence stayed as it was for want of a free page      */
+#define VLA_PAGES_BAD 2 /* a position outside the rotation table, an accepted list     */
+                        /*   that does not ascend within its drafts, a draft that   */
+                        /*   was passed over, probabilities without a next token,   */
+                        /*   or a negative number of slots to keep                  */
 
 /* The rows of one step: entry e's are start[e] .. start[e + 1] - 1 of the row
  * buffers, row start[e] + i being draft i of sequence seqs[e] (slot

@@ -50,8 +50,10 @@ __global__ __launch_bounds__(256) void k_evict_score(Ev e) {
   const float* p = e.d.mass + (size_t)x.seq * c.nkv * e.slots + slot;
   const size_t layer = (size_t)c.n_seqs * c.nkv * e.slots;
   // (eight loads of the inner loop are out together: heads where there are as
-  // many, whose rows are neighbours; 28 layers of 8 heads, 57 MB, 22 us so and 34
-  // the other way round; 18 layers of one 5 and 9)
+  // many, whose rows are neighbours, else layers if there are more of them. 16
+  // sequences of 3,000 slots, 28 layers: of 8 heads 27 us so and 39 the other way
+  // round, of 1, 4 and 7 heads 8, 21 and 35 us, and 16, 52 and 87; 4 layers of 4
+  // heads 9 and 10)
   const bool deep = c.nkv < 8 && c.layers > c.nkv;
   const int n0 = deep ? c.nkv : c.layers, n1 = deep ? c.layers : c.nkv;
   const size_t s0 = deep ? (size_t)e.slots : layer, s1 = deep ? layer : (size_t)e.slots;

@@ -307,9 +307,11 @@ struct Pre {
 // One CU reads 50 GB/s from the HBM, so where rows are long and entries few,
 // PARTS / 4 workgroups of four waves (PRE) walk an entry up to the first sum
 // over a row that it needs and work out a part of it with each wave; the walk
-// proper goes on from there. 64 chains over 131,072 tokens: 19 us (4 TB/s) and 8
-// in turn, against 33 without; over 50,001 tokens a CU's pass takes 3 us, no more
-// than the second launch.
+// proper goes on from there. 64 chains over 131,072 tokens: 19 us (67 MB, 3.5
+// TB/s) and 8 in turn, against 33 without; over 50,001 tokens a CU's pass takes 3
+// us, no more than the second launch. Later sums of an entry are one CU's however
+// long the rows are: eight trees of 24 to 40 drafts take 33 us over 50,001 tokens
+// and 59 over 131,072.
 template <typename T, int NT, bool PRE>
 __global__ __launch_bounds__(NT) void k_verify(DraftsDesc d) {
   __shared__ int sPar[ROWS], sTok[ROWS];
@@ -482,7 +484,7 @@ hipError_t verify(const DraftsDesc& d, hipStream_t st) {
 
 }  // namespace
 
-// Where VW workgroups to an entry begin the walk: rows too long for one CU, and
+// Where PARTS / 4 workgroups to an entry begin the walk: rows too long for one CU, and
 // CUs that would be idle.
 static bool verify_pre(const DraftsDesc& d) { return d.vocab >= 65536 && d.r.n_ent <= 128; }
 static size_t best_bytes(const DraftsDesc& d) { return ((size_t)d.r.n_rows * 4 + 15) & ~(size_t)15; }
